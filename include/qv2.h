@@ -54,7 +54,9 @@ enum {
   QV2_ERR_NONFINITE = -5,   /* reported by qv2_sweep_model_host when an input held NaN or Inf */
   QV2_ERR_CUDA = -6,        /* a CUDA runtime call failed; see qv2_last_cuda_error */
   QV2_ERR_NOMEM = -7,       /* scratch allocation failed */
-  QV2_ERR_UNSUPPORTED = -8  /* a combination the library does not implement */
+  QV2_ERR_UNSUPPORTED = -8, /* a combination the library does not implement */
+  QV2_ERR_TIMEOUT = -9      /* a kernel of an earlier call gave up waiting for its own copies: the
+                               results of that call are not valid */
 };
 
 enum { QV2_PER_TENSOR = 0, QV2_PER_CHANNEL = 1 };            /* granularity */
@@ -506,6 +508,105 @@ int qv2_quant_metrics_noalloc(int device, void* stream, const qv2_tensor_desc* d
  * Returns the number of tiles, or a negative status; at most max_tiles are written.
  */
 int64_t qv2_debug_plan_tiles(const qv2_tensor_desc* descs, uint32_t n, uint64_t* out, uint64_t max_tiles);
+
+/*
+ * ---- Microscaled 4-bit floating point ------------------------------------------------------------
+ *
+ * What a layer that leaves FP32 for 4 bits runs on.  A row is held in blocks of QV2_MX_BLOCK = 32
+ * consecutive elements with one power-of-two scale each (the OCP MXFP4 format):
+ *
+ *   A = max |x| over the block (columns past the row's end count as 0)
+ *   e = clamp(floor(log2 A) - 2, -127, 127), scale byte = e + 127 (byte 0 when A = 0)
+ *   code = sign and nearest of {0, 0.5, 1, 1.5, 2, 3, 4, 6} to |x| 2^-e, ties to the even code,
+ *          magnitudes above 6 become 6; 4 bits, sign in bit 3 (a negative value that rounds to zero
+ *          keeps its sign), element 2j of a row in the low half of byte j, 2j+1 in the high half
+ *   value = code's number * 2^e
+ *
+ * A block that holds a NaN or an infinity has scale byte 255 and zero codes, and all its values
+ * are NaN: a poisoned block stays visible in everything computed from it.  With a power-of-two
+ * scale every step of the rounding is exact in binary32, so codes and scales are a fixed function
+ * of the inputs.  Element types are named by QV2_IN_F32 / QV2_IN_F16 / QV2_IN_BF16.
+ */
+#define QV2_MX_BLOCK 32
+#define QV2_MX_MAX_GROUPS 1024u
+
+/* `groups` matrices of [rows][cols] elements (the weights of the experts of a layer; 1 for an
+ * ordinary matrix) in packed form, all on the device. */
+typedef struct {
+  void* codes;               /* row r of group g at codes + g*codes_gs + r*codes_ld, 16*ceil(cols/32) bytes;
+                                the base and both strides are multiples of 16 bytes */
+  void* scales;              /* row r of group g at scales + g*scales_gs + r*scales_ld, ceil(cols/32) bytes;
+                                any alignment (rows that are multiples of 16 bytes load fastest) */
+  uint64_t groups, rows, cols;
+  uint64_t codes_ld, scales_ld;      /* bytes between rows */
+  uint64_t codes_gs, scales_gs;      /* bytes between groups; not read when groups <= 1 */
+} qv2_mx_matrix;
+
+/* Rounds x[rows][cols] (row r at x + r*x_ld elements) to 4 bits: rows and cols are those of `out`,
+ * whose groups must be 1.  values, nullable: the dequantized copy, element type x_type, rows
+ * values_ld elements apart.  No output may overlap x.  cols <= 2^26, rows <= 2^40.
+ * Errors: _NULL, _ARG (x_type, groups, a row stride shorter than the row), _ALIGN, _SIZE, _CUDA. */
+int qv2_mx_quantize(qv2_ctx* ctx, const void* x, uint32_t x_type, uint64_t x_ld, const qv2_mx_matrix* out,
+                    void* values, uint64_t values_ld);
+
+/* The values that m stands for, rounded to y_type; y[groups*rows][cols], rows y_ld elements apart.
+ * rows of a group <= 2^30, groups <= 2^20. */
+int qv2_mx_dequantize(qv2_ctx* ctx, const qv2_mx_matrix* m, void* y, uint32_t y_type, uint64_t y_ld);
+
+/* y[i][j] = sum_k a[i][k] w_g[j][k] + bias_g[j], products exact, sums in binary32, rounded once to
+ * y_type.  y has a->rows rows, y_ld elements apart, of w->rows elements.
+ * offsets == NULL: one weight (w->groups == 1) for every row.  Otherwise a device array of
+ * w->groups + 1 non-decreasing row numbers: rows offsets[g] .. offsets[g+1]-1 meet weight g (a
+ * group may be empty), and rows before offsets[0] or from offsets[groups] on are not written.
+ * Entries outside 0..a->rows are clamped to it, a decreasing one counts as its predecessor.
+ * bias, nullable: binary32 [groups][w->rows].  Inner sizes must agree, a->groups is 1,
+ * w->groups <= QV2_MX_MAX_GROUPS, cols <= 2^26, rows of a and of a group of w <= 2^30.
+ * The order of the sums depends on the sizes only: the same inputs give the same bits.
+ * y must not overlap a, w, bias or offsets. */
+int qv2_mx_matmul(qv2_ctx* ctx, const qv2_mx_matrix* a, const qv2_mx_matrix* w, const float* bias,
+                  const int64_t* offsets, void* y, uint32_t y_type, uint64_t y_ld);
+
+/* qv2_mx_quantize of x[rows][w->cols] into context scratch followed by qv2_mx_matmul: a layer of
+ * 4-bit weights applied to activations as they come.  The scratch grows on demand (the first call
+ * of a new largest size allocates, later ones do not). */
+int qv2_mx_linear(qv2_ctx* ctx, const void* x, uint32_t x_type, uint64_t x_ld, uint64_t rows,
+                  const qv2_mx_matrix* w, const float* bias, const int64_t* offsets, void* y, uint32_t y_type,
+                  uint64_t y_ld);
+
+/*
+ * ---- Quantized key / value cache ------------------------------------------------------------------
+ *
+ * A paged cache of the keys and values of an attention layer.  Token slot s = page * page_size + place;
+ * per slot and head one row of head_dim elements, dense arrays [pages][page_size][heads][...]:
+ *   QV2_KV_MX4: codes 16*ceil(head_dim/32) bytes, scales ceil(head_dim/32) bytes, the format above
+ *   QV2_KV_I8:  codes head_dim signed bytes, scales one binary32: the symmetric 8-bit quantizer of
+ *               qv2_calibrate with a group per row: step = R/127 (stored), q = clamp(round(x * (127/R)),
+ *               -127, 127), value = q * step; R = max |x|; step 1 and codes 0 when R = 0 or 127/R
+ *               overflows; a row with a NaN or an infinity has step NaN and codes 0, and reads back
+ *               as NaN
+ */
+enum { QV2_KV_MX4 = 0, QV2_KV_I8 = 1 };
+typedef struct {
+  void *k_codes, *k_scales, *v_codes, *v_scales;   /* device; MX4 codes 16-byte, I8 scales 4-byte aligned */
+  uint64_t pages;
+  uint32_t page_size, heads, head_dim, format;     /* head_dim <= 4096 */
+} qv2_kv_cache;
+
+/* Writes `tokens` new keys and values: element (t, h, d) of k at k + t*k_token_ld + h*k_head_ld + d
+ * (strides in elements, any values; likewise v).  slots: device, one slot number per token; a token
+ * whose slot is negative or past the cache is skipped.  Two tokens of a call must not name the same
+ * slot. */
+int qv2_kv_write(qv2_ctx* ctx, const qv2_kv_cache* cache, const void* k, uint64_t k_token_ld, uint64_t k_head_ld,
+                 const void* v, uint64_t v_token_ld, uint64_t v_head_ld, uint32_t type, uint64_t tokens,
+                 const int64_t* slots);
+
+/* Reads whole sequences back: starts is a device array of seqs + 1 non-decreasing numbers, sequence s
+ * fills rows starts[s] .. starts[s+1]-1 of k and v ([total][heads][head_dim], dense, element type
+ * `type`; either may be NULL), and its token i lies in page table[s*table_ld + i/page_size].  Rows
+ * outside every sequence, and tokens whose page number is out of range or past the table's row,
+ * are written as zeros. */
+int qv2_kv_read(qv2_ctx* ctx, const qv2_kv_cache* cache, const int32_t* table, uint64_t table_ld, uint32_t seqs,
+                const int64_t* starts, uint64_t total, void* k, void* v, uint32_t type);
 
 #ifdef __cplusplus
 }

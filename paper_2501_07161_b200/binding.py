@@ -5,6 +5,7 @@ CUDA kernels.  There is no CPU fallback: if the library cannot be built or loade
 from __future__ import annotations
 
 import ctypes as C
+import math
 import os
 from dataclasses import dataclass
 from typing import List, Optional, Sequence
@@ -32,7 +33,10 @@ EXPORTS = ["qv2_create", "qv2_destroy", "qv2_status_string", "qv2_last_cuda_erro
            "qv2_debug_plan_tiles", "qv2_quant_metrics_noalloc", "qv2_quant_metrics_ex", "qv2_rank_layers_ex", "qv2_kl_divergence", "qv2_fold_batchnorm", "qv2_sweep_graph_create", "qv2_sweep_graph_launch",
            "qv2_sweep_graph_destroy", "qv2_check_nonfinite", "qv2_calibrate_ex", "qv2_group_hist_count",
            "qv2_sync_count", "qv2_set_schedule", "qv2_stage_count", "qv2_set_fold_mode",
-           "qv2_set_phase_timing", "qv2_calibrate_phase_ms", "qv2_set_dependent_launch"]
+           "qv2_set_phase_timing", "qv2_calibrate_phase_ms", "qv2_set_dependent_launch",
+           "qv2_mx_quantize", "qv2_mx_dequantize", "qv2_mx_matmul", "qv2_mx_linear", "qv2_kv_write", "qv2_kv_read"]
+MX_BLOCK, MX_MAX_GROUPS = 32, 1024
+KV_MX4, KV_I8 = 0, 1
 KL_BINS = 128
 NO_GROUP = 0xFFFFFFFF
 NOALLOC_MAX_ELEMS = 1 << 27
@@ -61,6 +65,16 @@ class SweepBuffers(C.Structure):
 class HostResults(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in
                 ("mse", "sqnr_db", "nonfinite", "order", "keep_fp32", "n_keep")]
+
+
+class MxMatrixC(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p)] + \
+               [(n, C.c_uint64) for n in ("groups", "rows", "cols", "codes_ld", "scales_ld", "codes_gs", "scales_gs")]
+
+
+class KvCacheC(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("k_codes", "k_scales", "v_codes", "v_scales")] + \
+               [("pages", C.c_uint64)] + [(n, C.c_uint32) for n in ("page_size", "heads", "head_dim", "format")]
 
 
 _lib = None
@@ -120,6 +134,13 @@ def lib() -> C.CDLL:
     L.qv2_debug_plan_tiles.argtypes = [dp, u32, vp, u64]; L.qv2_debug_plan_tiles.restype = C.c_int64
     L.qv2_quant_metrics_noalloc.argtypes = [i32, vp, dp, vp, vp, vp, vp]
     L.qv2_quant_metrics_noalloc.restype = i32
+    mp, kp = C.POINTER(MxMatrixC), C.POINTER(KvCacheC)
+    L.qv2_mx_quantize.argtypes = [vp, vp, u32, u64, mp, vp, u64]; L.qv2_mx_quantize.restype = i32
+    L.qv2_mx_dequantize.argtypes = [vp, mp, vp, u32, u64]; L.qv2_mx_dequantize.restype = i32
+    L.qv2_mx_matmul.argtypes = [vp, mp, mp, vp, vp, vp, u32, u64]; L.qv2_mx_matmul.restype = i32
+    L.qv2_mx_linear.argtypes = [vp, vp, u32, u64, u64, mp, vp, vp, vp, u32, u64]; L.qv2_mx_linear.restype = i32
+    L.qv2_kv_write.argtypes = [vp, kp, vp, u64, u64, vp, u64, u64, u32, u64, vp]; L.qv2_kv_write.restype = i32
+    L.qv2_kv_read.argtypes = [vp, kp, vp, u64, u32, vp, u64, vp, vp, u32]; L.qv2_kv_read.restype = i32
     _lib = L
     return L
 
@@ -193,6 +214,77 @@ class MetricsOut:
     sqnr_db: torch.Tensor
     codes: Optional[List[Optional[torch.Tensor]]] = None
     cosine: Optional[torch.Tensor] = None
+
+
+@dataclass(frozen=True)
+class MxMatrix:
+    """A matrix (or, with a leading dimension, one per expert) in the microscaled 4-bit format:
+    codes uint8 [(groups,) rows, 16 * ceil(cols / 32)], scales uint8 [(groups,) rows, ceil(cols / 32)].
+    Rows may be strided; bytes of a row are consecutive.  Rows of scales that are multiples of 16
+    bytes apart load fastest (mx_empty allocates them so)."""
+    codes: torch.Tensor
+    scales: torch.Tensor
+    cols: int
+    values: Optional[torch.Tensor] = None          # the dequantized copy, where mx_quantize was asked for it
+
+    def __post_init__(self):
+        c, s, blocks = self.codes, self.scales, -(-self.cols // MX_BLOCK)
+        if c.dtype != torch.uint8 or s.dtype != torch.uint8:
+            raise TypeError("codes and scales must be uint8")
+        if c.dim() not in (2, 3) or s.dim() != c.dim() or s.shape[:-1] != c.shape[:-1]:
+            raise ValueError("codes and scales must both be [(groups,) rows, bytes]")
+        if c.shape[-1] != 16 * blocks or s.shape[-1] != blocks:
+            raise ValueError(f"{self.cols} columns take {16 * blocks} bytes of codes and {blocks} of scales per row")
+        if blocks and (c.stride(-1) != 1 or s.stride(-1) != 1) and c.numel():
+            raise ValueError("the bytes of a row must be consecutive")
+        if c.device != s.device:
+            raise ValueError("codes and scales must be on one device")
+        groups, rows = (c.shape[0], c.shape[1]) if c.dim() == 3 else (1, c.shape[0])
+        one = rows <= 1
+        object.__setattr__(self, "_c", MxMatrixC(
+            c.data_ptr(), s.data_ptr(), groups, rows, self.cols, 16 * blocks if one else c.stride(-2),
+            blocks if one else s.stride(-2), c.stride(0) if c.dim() == 3 else 0, s.stride(0) if c.dim() == 3 else 0))
+
+    @property
+    def groups(self) -> int:
+        return self._c.groups
+
+    @property
+    def rows(self) -> int:
+        return self._c.rows
+
+
+@dataclass(frozen=True)
+class KvCache:
+    """A paged cache of quantized keys and values, dense arrays [pages, page_size, heads, ...]:
+    KV_MX4 holds codes uint8 [..., 16 * ceil(dim / 32)] and scales uint8 [..., ceil(dim / 32)], KV_I8
+    holds codes int8 [..., dim] and scales float32 [...]."""
+    format: int
+    head_dim: int
+    k_codes: torch.Tensor
+    k_scales: torch.Tensor
+    v_codes: torch.Tensor
+    v_scales: torch.Tensor
+
+    def __post_init__(self):
+        if self.format not in (KV_MX4, KV_I8):
+            raise ValueError("format must be KV_MX4 or KV_I8")
+        mx, blocks = self.format == KV_MX4, -(-self.head_dim // MX_BLOCK)
+        shape = tuple(self.k_codes.shape[:3])
+        if len(shape) != 3:
+            raise ValueError("cache arrays are [pages, page_size, heads, ...]")
+        for codes, scales in ((self.k_codes, self.k_scales), (self.v_codes, self.v_scales)):
+            if codes.dtype != (torch.uint8 if mx else torch.int8) or scales.dtype != (torch.uint8 if mx else torch.float32):
+                raise TypeError("KV_MX4 holds uint8 codes and scales, KV_I8 int8 codes and float32 scales")
+            if tuple(codes.shape) != shape + (16 * blocks if mx else self.head_dim,) or \
+                    tuple(scales.shape) != shape + ((blocks,) if mx else ()):
+                raise ValueError("cache arrays do not have the shapes of this format")
+            if not codes.is_contiguous() or not scales.is_contiguous() or codes.device != scales.device or \
+                    codes.device != self.k_codes.device:
+                raise ValueError("cache arrays must be dense and on one device")
+        object.__setattr__(self, "_c", KvCacheC(
+            self.k_codes.data_ptr(), self.k_scales.data_ptr(), self.v_codes.data_ptr(), self.v_scales.data_ptr(),
+            shape[0], shape[1], shape[2], self.head_dim, self.format))
 
 
 class Context:
@@ -379,6 +471,170 @@ class Context:
         if st not in (OK, -5):
             raise Qv2Error(st, "qv2_sweep_model_host")
         return st
+
+
+    # -- microscaled 4-bit floating point ----------------------------------------------------
+    def _on_stream(self, *used: Optional[torch.Tensor]) -> bool:
+        """Checks the device of the tensors of a call.  When torch's current stream is not this
+        context's, marks them as used on the context's stream, so that their memory is not handed
+        out again before the call has read it (waiting for whoever wrote them is the caller's part,
+        as for every call)."""
+        for t in used:
+            if t is not None and t.device != self.device:
+                raise ValueError(f"a tensor is on {t.device}, the context on {self.device}")
+        if torch.cuda.current_stream(self.device).cuda_stream == self.stream.cuda_stream:
+            return True
+        for t in used:
+            if t is not None:
+                t.record_stream(self.stream)
+        return False
+
+    def _new(self, same: bool, shape, dtype) -> torch.Tensor:
+        """Memory that belongs to the context's stream."""
+        if same:
+            return torch.empty(shape, dtype=dtype, device=self.device)
+        with torch.cuda.stream(self.stream):
+            return torch.empty(shape, dtype=dtype, device=self.device)
+
+    @staticmethod
+    def _rows(x: torch.Tensor, cols: int) -> torch.Tensor:
+        """x [..., cols] as [rows, cols] with consecutive elements."""
+        if x.dtype not in _DTYPE_FLAG:
+            raise TypeError("activations must be float32, float16 or bfloat16")
+        if x.dim() < 1 or x.shape[-1] != cols:
+            raise ValueError(f"the last dimension must be {cols}")
+        if x.dim() != 2:
+            x = x.reshape(x.numel() // cols if cols else math.prod(x.shape[:-1]), cols)
+        if cols > 1 and x.stride(1) != 1:
+            raise ValueError("the elements of a row must be consecutive")
+        if x.shape[0] > 1 and x.stride(0) < cols:
+            raise ValueError("rows may not overlap")
+        return x
+
+    def mx_empty(self, rows: int, cols: int, groups: int = 0, values: Optional[torch.Tensor] = None, same: Optional[bool] = None) -> MxMatrix:
+        """An uninitialised matrix (groups > 0: one per expert), scale rows 16 bytes aligned."""
+        same = self._on_stream() if same is None else same
+        blocks, lead = -(-cols // MX_BLOCK), ((groups,) if groups else ())
+        codes = self._new(same, (*lead, rows, 16 * blocks), torch.uint8)
+        scales = self._new(same, (*lead, rows, (blocks + 15) // 16 * 16), torch.uint8)
+        return MxMatrix(codes, scales if scales.shape[-1] == blocks else scales[..., :blocks], cols, values)
+
+    def mx_quantize(self, x: torch.Tensor, want_values: bool = False) -> MxMatrix:
+        """x [..., cols] rounded to 4 bits, rows flattened; with want_values also its dequantized copy,
+        of x's shape and type."""
+        shape, x = x.shape, self._rows(x, x.shape[-1])
+        same = self._on_stream(x)
+        values = self._new(same, shape, x.dtype) if want_values else None
+        m = self.mx_empty(x.shape[0], x.shape[1], values=values, same=same)
+        _check(lib().qv2_mx_quantize(self._h, x.data_ptr(), _DTYPE_FLAG[x.dtype], x.stride(0), m._c, _ptr(values), x.shape[1]),
+               "qv2_mx_quantize")
+        return m
+
+    def mx_dequantize(self, m: MxMatrix, dtype: torch.dtype = torch.float32) -> torch.Tensor:
+        """-> [(groups,) rows, cols]"""
+        same = self._on_stream(m.codes, m.scales)
+        y = self._new(same, (*m.codes.shape[:-1], m.cols), dtype)
+        _check(lib().qv2_mx_dequantize(self._h, m._c, y.data_ptr(), _DTYPE_FLAG[dtype], m.cols), "qv2_mx_dequantize")
+        return y
+
+    def _product_args(self, w: MxMatrix, bias, offsets, grouped: bool):
+        if grouped != (w.codes.dim() == 3):
+            raise ValueError("a dense product takes codes [rows, bytes], a grouped one [groups, rows, bytes]")
+        if bias is not None and (bias.dtype != torch.float32 or not bias.is_contiguous() or bias.shape != w.codes.shape[:-1]):
+            raise ValueError("bias must be dense float32 [(groups,) rows of the weight]")
+        if grouped and (offsets.dtype != torch.int64 or offsets.shape != (w.groups + 1,) or not offsets.is_contiguous()):
+            raise ValueError("offsets must be dense int64 [groups + 1]")
+
+    def _out(self, out, same, shape, dtype):
+        if out is None:
+            return self._new(same, shape, dtype)
+        if out.dtype != dtype or tuple(out.shape) != tuple(shape) or (out.dim() and out.shape[-1] > 1 and out.stride(-1) != 1):
+            raise ValueError("out must have the result's shape and type, its rows consecutive")
+        if out.dim() != 2 and not out.is_contiguous():
+            raise ValueError("out must be dense unless it is a matrix")
+        return out
+
+    def _mx_apply(self, x, w, bias, offsets, out_dtype, out, grouped):
+        self._product_args(w, bias, offsets, grouped)
+        dtype = out_dtype or (out.dtype if out is not None else x.dtype)
+        if dtype not in _DTYPE_FLAG:
+            raise TypeError("results are float32, float16 or bfloat16")
+        shape = (*x.shape[:-1], w.rows)
+        x = self._rows(x, w.cols)
+        same = self._on_stream(x, w.codes, w.scales, bias, offsets, out)
+        y = self._out(out, same, shape, dtype)
+        _check(lib().qv2_mx_linear(self._h, x.data_ptr(), _DTYPE_FLAG[x.dtype], x.stride(0), x.shape[0], w._c, _ptr(bias), _ptr(offsets),
+                                   y.data_ptr(), _DTYPE_FLAG[dtype], y.stride(0) if y.dim() == 2 else w.rows), "qv2_mx_linear")
+        return y
+
+    def mx_linear(self, x: torch.Tensor, w: MxMatrix, bias: Optional[torch.Tensor] = None, out_dtype: Optional[torch.dtype] = None,
+                  out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """y = q(x) w^T + bias: x [..., cols] is rounded to 4 bits on the way; -> [..., w.rows], x's type
+        unless out_dtype says otherwise."""
+        return self._mx_apply(x, w, bias, None, out_dtype, out, False)
+
+    def mx_linear_grouped(self, x: torch.Tensor, offsets: torch.Tensor, w: MxMatrix, bias: Optional[torch.Tensor] = None,
+                          out_dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Rows offsets[g] .. offsets[g+1]-1 of x meet weight g of w [groups, rows, ...]; offsets int64
+        [groups + 1] on the device.  Rows of no group are left as they were in `out` (undefined in a
+        new result)."""
+        return self._mx_apply(x, w, bias, offsets, out_dtype, out, True)
+
+    def mx_matmul(self, a: MxMatrix, w: MxMatrix, bias: Optional[torch.Tensor] = None, offsets: Optional[torch.Tensor] = None,
+                  out_dtype: torch.dtype = torch.float32, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """The product of packed matrices: a [rows, cols] against w [n, cols] (offsets None) or [groups, n, cols]."""
+        self._product_args(w, bias, offsets, offsets is not None)
+        if a.codes.dim() != 2:
+            raise ValueError("the left matrix has no groups")
+        if out_dtype not in _DTYPE_FLAG:
+            raise TypeError("results are float32, float16 or bfloat16")
+        same = self._on_stream(a.codes, a.scales, w.codes, w.scales, bias, offsets, out)
+        y = self._out(out, same, (a.rows, w.rows), out_dtype)
+        _check(lib().qv2_mx_matmul(self._h, a._c, w._c, _ptr(bias), _ptr(offsets), y.data_ptr(), _DTYPE_FLAG[out_dtype], y.stride(0)),
+               "qv2_mx_matmul")
+        return y
+
+    # -- quantized key / value cache ---------------------------------------------------------
+    def kv_empty(self, pages: int, page_size: int, heads: int, head_dim: int, format: int = KV_I8) -> KvCache:
+        """A cache whose slots hold nothing yet."""
+        same, shape, blocks = self._on_stream(), (pages, page_size, heads), -(-head_dim // MX_BLOCK)
+        parts = []
+        for _ in "kv":
+            if format == KV_MX4:
+                parts += [self._new(same, (*shape, 16 * blocks), torch.uint8), self._new(same, (*shape, blocks), torch.uint8)]
+            else:
+                parts += [self._new(same, (*shape, head_dim), torch.int8), self._new(same, shape, torch.float32)]
+        return KvCache(format, head_dim, *parts)
+
+    def kv_write(self, cache: KvCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor):
+        """Rounds keys and values [tokens, heads, dim] (any strides of tokens and heads) into their
+        slots (int64 [tokens], page * page_size + place; negative: skipped)."""
+        if k.dtype not in _DTYPE_FLAG or v.dtype != k.dtype:
+            raise TypeError("keys and values must both be float32, float16 or bfloat16")
+        shape = (slots.numel(), cache._c.heads, cache.head_dim)
+        if k.shape != shape or v.shape != shape or (shape[2] > 1 and (k.stride(2) != 1 or v.stride(2) != 1)):
+            raise ValueError("keys and values must be [tokens, heads, dim] of the cache, rows consecutive")
+        if slots.dtype != torch.int64 or slots.dim() != 1 or not slots.is_contiguous():
+            raise ValueError("slots must be dense int64 [tokens]")
+        self._on_stream(k, v, slots, cache.k_codes, cache.k_scales, cache.v_codes, cache.v_scales)
+        _check(lib().qv2_kv_write(self._h, cache._c, k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0), v.stride(1),
+                                  _DTYPE_FLAG[k.dtype], shape[0], slots.data_ptr()), "qv2_kv_write")
+
+    def kv_read(self, cache: KvCache, table: torch.Tensor, starts: torch.Tensor, total: int, dtype: torch.dtype = torch.bfloat16):
+        """Whole sequences: starts int64 [seqs + 1] (the host knows its last entry, `total`), table int32
+        [seqs, pages of the longest] -> keys, values [total, heads, dim]."""
+        if dtype not in _DTYPE_FLAG:
+            raise TypeError("results are float32, float16 or bfloat16")
+        if table.dtype != torch.int32 or table.dim() != 2 or not table.is_contiguous():
+            raise ValueError("table must be dense int32 [seqs, pages]")
+        if starts.dtype != torch.int64 or starts.shape != (table.shape[0] + 1,) or not starts.is_contiguous():
+            raise ValueError("starts must be dense int64 [seqs + 1]")
+        same = self._on_stream(table, starts, cache.k_codes, cache.k_scales, cache.v_codes, cache.v_scales)
+        shape = (total, cache._c.heads, cache.head_dim)
+        k, v = self._new(same, shape, dtype), self._new(same, shape, dtype)
+        _check(lib().qv2_kv_read(self._h, cache._c, table.data_ptr(), table.shape[1], table.shape[0], starts.data_ptr(), total,
+                                 k.data_ptr(), v.data_ptr(), _DTYPE_FLAG[dtype]), "qv2_kv_read")
+        return k, v
 
 
 def quant_metrics_noalloc(desc: TensorDesc, step: torch.Tensor, inv: torch.Tensor, offset: torch.Tensor,
