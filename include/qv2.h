@@ -528,7 +528,7 @@ int64_t qv2_debug_plan_tiles(const qv2_tensor_desc* descs, uint32_t n, uint64_t*
  * of the inputs.  Element types are named by QV2_IN_F32 / QV2_IN_F16 / QV2_IN_BF16.
  */
 #define QV2_MX_BLOCK 32
-#define QV2_MX_MAX_GROUPS 1024u
+#define QV2_MX_MAX_GROUPS 512u
 
 /* `groups` matrices of [rows][cols] elements (the weights of the experts of a layer; 1 for an
  * ordinary matrix) in packed form, all on the device. */

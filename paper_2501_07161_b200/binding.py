@@ -35,7 +35,7 @@ EXPORTS = ["qv2_create", "qv2_destroy", "qv2_status_string", "qv2_last_cuda_erro
            "qv2_sync_count", "qv2_set_schedule", "qv2_stage_count", "qv2_set_fold_mode",
            "qv2_set_phase_timing", "qv2_calibrate_phase_ms", "qv2_set_dependent_launch",
            "qv2_mx_quantize", "qv2_mx_dequantize", "qv2_mx_matmul", "qv2_mx_linear", "qv2_kv_write", "qv2_kv_read"]
-MX_BLOCK, MX_MAX_GROUPS = 32, 1024
+MX_BLOCK, MX_MAX_GROUPS = 32, 512
 KV_MX4, KV_I8 = 0, 1
 KL_BINS = 128
 NO_GROUP = 0xFFFFFFFF

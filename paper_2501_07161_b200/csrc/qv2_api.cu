@@ -245,7 +245,14 @@ extern "C" int qv2_create(qv2_ctx** out, int device, void* stream) {
   int sms = 0;
   cudaError_t e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
   if (e == cudaSuccess) e = cudaMalloc((void**)&c->d_rank, kRankScratchDoubles * sizeof(double));
-  if (e != cudaSuccess) { delete c; return e == cudaErrorMemoryAllocation ? QV2_ERR_NOMEM : QV2_ERR_CUDA; }
+  if (e == cudaSuccess) e = cudaHostAlloc((void**)&c->h_fault, sizeof(uint32_t), cudaHostAllocMapped);
+  if (e == cudaSuccess) { *c->h_fault = 0; e = cudaHostGetDevicePointer((void**)&c->d_fault, c->h_fault, 0); }
+  if (e != cudaSuccess) {
+    cudaFree(c->d_rank);
+    if (c->h_fault) cudaFreeHost(c->h_fault);
+    delete c;
+    return e == cudaErrorMemoryAllocation ? QV2_ERR_NOMEM : QV2_ERR_CUDA;
+  }
   c->sm_count = sms > 0 ? sms : 1;
   // occupancy of each persistent kernel on THIS device (two contexts on different GPUs differ)
   c->caps.range = range_grid_cap(c->sm_count, false);
@@ -272,6 +279,7 @@ extern "C" int qv2_destroy(qv2_ctx* c) {
   cudaFree(c->d_nf_acc); cudaFree(c->d_hist_acc); cudaFree(c->d_tickets); cudaFree(c->d_codes);
   cudaFree(c->d_rank); cudaFree(c->d_mx_codes); cudaFree(c->d_mx_scales);
   if (c->h_pinned) cudaFreeHost(c->h_pinned);
+  cudaFreeHost(c->h_fault);
   for (int i = 0; i < kCodeRing; ++i) {
     if (c->h_codes[i]) cudaFreeHost(c->h_codes[i]);
     if (c->code_ev[i]) cudaEventDestroy(c->code_ev[i]);

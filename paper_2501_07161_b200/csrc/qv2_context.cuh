@@ -65,6 +65,8 @@ struct qv2_ctx {
   // qv2_mx_linear: the activations of the current call in packed form
   uint8_t* d_mx_codes = nullptr;  size_t cap_mx_codes = 0;
   uint8_t* d_mx_scales = nullptr; size_t cap_mx_scales = 0;
+  uint32_t* h_fault = nullptr;    // host-mapped word and its device address: a kernel that gave up waiting sets it
+  uint32_t* d_fault = nullptr;
   // pinned host staging for the plan upload
   uint8_t* h_pinned = nullptr;    size_t cap_pinned = 0;
   // pinned ring for the code-pointer table: a call fills the next area and copies it on the

@@ -186,6 +186,8 @@ struct MxProduct {
   const float* bias; const int64_t* offsets;
   void* y; uint64_t y_ld;
   uint32_t dtype, m, n, k, groups;
+  uint32_t early;        // only `a` may still be on its way when the launch begins (see mx_matmul_kernel)
+  uint32_t* fault;       // host-mapped word, set when a kernel gave up waiting
 };
 cudaError_t launch_mx_matmul(const Launch& l, const MxProduct& p, uint64_t* launches);
 

@@ -61,10 +61,17 @@ int check_product(const qv2_mx_matrix* w, uint64_t rows, const float* bias, cons
   return check_dense(y, dtype, y_ld, rows, w->rows);
 }
 
+// Whether a kernel of an earlier call gave up waiting; asking clears it.
+int take_fault(qv2_ctx* c) {
+  if (!*(volatile uint32_t*)c->h_fault) return QV2_OK;
+  *(volatile uint32_t*)c->h_fault = 0;
+  return QV2_ERR_TIMEOUT;
+}
+
 int run_product(qv2_ctx* c, const MxView& a, uint64_t rows, const qv2_mx_matrix* w, const float* bias, const int64_t* offsets, void* y,
-                int dtype, uint64_t y_ld) {
-  if (rows == 0 || w->rows == 0) return QV2_OK;
+                int dtype, uint64_t y_ld, bool early) {
   MxProduct p;
+  p.early = early && c->dependent_launch; p.fault = c->d_fault;
   p.a = a; p.w = view_of(w);
   p.bias = bias; p.offsets = offsets; p.y = y; p.y_ld = y_ld;
   p.dtype = (uint32_t)dtype; p.m = (uint32_t)rows; p.n = (uint32_t)w->rows; p.k = (uint32_t)w->cols; p.groups = (uint32_t)w->groups;
@@ -147,8 +154,10 @@ extern "C" int qv2_mx_matmul(qv2_ctx* c, const qv2_mx_matrix* a, const qv2_mx_ma
     if (st != QV2_OK) return st;
     if ((st = check_product(w, a->rows, bias, offsets, y, dtype, y_ld)) != QV2_OK) return st;
     if (a->cols != w->cols) return QV2_ERR_ARG;
+    if ((st = take_fault(c)) != QV2_OK) return st;
+    if (a->rows == 0 || w->rows == 0) return QV2_OK;
     DeviceGuard guard(c->device);
-    return run_product(c, view_of(a), a->rows, w, bias, offsets, y, dtype, y_ld);
+    return run_product(c, view_of(a), a->rows, w, bias, offsets, y, dtype, y_ld, false);
   };
   return logged(c, "qv2_mx_matmul", before, run());
 }
@@ -163,6 +172,7 @@ extern "C" int qv2_mx_linear(qv2_ctx* c, const void* x, uint32_t x_type, uint64_
     int st = check_product(w, rows, bias, offsets, y, yt, y_ld);
     if (st != QV2_OK) return st;
     if ((st = check_dense(x, xt, x_ld, rows, w->cols)) != QV2_OK) return st;
+    if ((st = take_fault(c)) != QV2_OK) return st;
     if (rows == 0 || w->rows == 0) return QV2_OK;
     DeviceGuard guard(c->device);
     const uint64_t blocks = (w->cols + QV2_MX_BLOCK - 1) / QV2_MX_BLOCK;
@@ -172,7 +182,9 @@ extern "C" int qv2_mx_linear(qv2_ctx* c, const void* x, uint32_t x_type, uint64_
     if ((st = grow(c, &c->d_mx_scales, &c->cap_mx_scales, rows * a.scales_ld, false)) != QV2_OK) return st;
     a.codes = c->d_mx_codes; a.scales = c->d_mx_scales;
     if (w->cols) QV2_CUDA(c, launch_mx_quantize(launch_of(c), x, (uint32_t)xt, x_ld, rows, (uint32_t)w->cols, a, nullptr, 0, &c->launches));
-    return run_product(c, a, rows, w, bias, offsets, y, yt, y_ld);
+    // The kernel that rounds x waits for all work before it and only then lets the product begin, so
+    // weights, bias and offsets are complete when the product starts to fetch them.
+    return run_product(c, a, rows, w, bias, offsets, y, yt, y_ld, w->cols != 0);
   };
   return logged(c, "qv2_mx_linear", before, run());
 }
