@@ -6,8 +6,8 @@
 //   warp 0       fetches code tiles by TMA (128 bytes = 256 columns per row and step, 128-byte swizzle),
 //   warp 1       copies the scales from shared to tensor memory and issues the products,
 //   warp 2       owns the tensor memory,
-//   warps 4-7    move finished accumulators out (one warp per quarter of the 128 accumulator rows),
-//   warps 8-11   bring the scales: they lie row by row in memory, the tensor core wants them four to a
+//   warps 4-11   move finished accumulators out (two warps per quarter of the 128 accumulator rows),
+//   warps 12-15  bring the scales: they lie row by row in memory, the tensor core wants them four to a
 //                word and 32 rows to a column, so they pass through registers, 16 bytes per row and two
 //                steps, fetched four steps ahead.
 // A ring of shared-memory stages decouples them; accumulators are double-buffered.
@@ -25,7 +25,7 @@ namespace qv2 {
 
 namespace {
 
-constexpr int kProductThreads = 384;
+constexpr int kProductThreads = 512;
 constexpr uint32_t kStepCols = 256;              // columns per stage: 128 bytes of codes
 constexpr uint64_t kWaitLimitNs = 2000000000ull; // a wait that lasts this long gives up
 constexpr uint32_t kMaxGroups = QV2_MX_MAX_GROUPS;
@@ -33,7 +33,6 @@ constexpr uint32_t kMaxGroups = QV2_MX_MAX_GROUPS;
 // ------------------------------------------------------------------------------------ PTX wrappers
 __device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory"); }
-__device__ __forceinline__ void bar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
 __device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
   asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
@@ -45,39 +44,84 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
 }
 __device__ __forceinline__ uint64_t now_ns() { uint64_t t; asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t)); return t; }
 
-// Waits for the phase of `parity` to complete.  false: this wait or another of the CTA has given up.
-__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile uint32_t* failed) {
-  if (bar_try(bar, parity)) return true;
-  uint64_t begin = 0;
-  for (uint32_t i = 1;; ++i) {
-    if (bar_try(bar, parity)) return true;
-    if ((i & 255u) == 0) {
-      if (*failed) return false;
-      const uint64_t t = now_ns();
-      if (!begin) begin = t;
-      else if (t - begin > kWaitLimitNs) { *failed = 1; return false; }
-    }
-  }
+// One lane of the warp, the same each time.  Work issued by one thread stands behind this test and not behind a
+// lane number: the values it needs are then known to be the warp's own and are kept in uniform registers (with
+// `lane == 0` a step of the product took 950 cycles to issue).
+__device__ __forceinline__ bool elect_one() {
+  uint32_t ok;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok));
+  return ok != 0;
 }
 
-__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y, int z) {
-  asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
-               ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z) : "memory");
+// The warp waits for the phase of `parity` to complete.  false, for all of its lanes: this wait or another of the
+// CTA has given up.
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile uint32_t* failed) {
+  bool ok = bar_try(bar, parity);
+  if (__all_sync(0xffffffffu, ok)) return true;
+  uint64_t begin = 0;
+  for (uint32_t i = 1; !ok; ++i) {
+    ok = bar_try(bar, parity);
+    if (!ok && (i & 255u) == 0) {
+      if (*failed) break;
+      const uint64_t t = now_ns();
+      if (!begin) begin = t;
+      else if (t - begin > kWaitLimitNs) { *failed = 1; break; }
+    }
+  }
+  return __all_sync(0xffffffffu, ok);
 }
+
+// PAIR: the two CTAs of a cluster work on one tile; copies of either report to the first one's barrier.
+template <bool PAIR>
+__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y, int z) {
+  if constexpr (PAIR)
+    asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+                 ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z) : "memory");
+  else
+    asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+                 ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z) : "memory");
+}
+// Arrives at `bar` (PAIR: at the same place in both CTAs) when the tensor work issued so far is done.
+template <bool PAIR>
 __device__ __forceinline__ void tc_commit(uint32_t bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+  if constexpr (PAIR)
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)3) : "memory");
+  else
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ uint32_t at_rank(uint32_t addr, uint32_t rank) {      // the same place in another CTA of the cluster
+  uint32_t r;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+  return r;
+}
+// Arrives at a barrier of this CTA, or (PAIR) at one given by at_rank.  What has to be seen with the arrival is shared
+// memory of the arriving CTA, read by its own tensor core after fence.proxy.async, and tensor memory, ordered by
+// tcgen05.fence; a release to the whole cluster would besides wait for all global traffic that the thread has in
+// flight, and took 1500 to 2200 cycles a step.
+template <bool PAIR>
+__device__ __forceinline__ void bar_arrive_at(uint32_t bar) {
+  if constexpr (PAIR) asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+  else asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 // Scales of 128 rows by 4 blocks: 512 consecutive bytes, 16 for each of 32 lanes, into 4 columns of all
-// four lane quarters.
+// four lane quarters.  (PAIR: each CTA from its own shared to its own tensor memory.)
+template <bool PAIR>
 __device__ __forceinline__ void tc_copy_scales(uint32_t column, uint64_t desc) {
-  asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(column), "l"(desc) : "memory");
+  if constexpr (PAIR) asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(column), "l"(desc) : "memory");
+  else asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(column), "l"(desc) : "memory");
 }
+template <bool PAIR>
 __device__ __forceinline__ void tc_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb, uint32_t accumulate) {
-  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
-               "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
-               ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate) : "memory");
+  if constexpr (PAIR)
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+                 "tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate) : "memory");
+  else
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+                 "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate) : "memory");
 }
 __device__ __forceinline__ void tc_load32(uint32_t taddr, uint32_t (&r)[32]) {
   asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 "
@@ -111,10 +155,13 @@ template <int BN_, bool TOKENS_X_, int STAGES_>
 struct Shape {
   static constexpr int BN = BN_, STAGES = STAGES_;
   static constexpr bool TOKENS_X = TOKENS_X_;              // X are the tokens (else the weights)
-  static constexpr int ROW_TILE = TOKENS_X ? 128 : BN;     // tokens per tile
+  static constexpr bool PAIR = TOKENS_X;                   // two CTAs per tile: each has half of X's and of Y's rows
+  static constexpr int CTAS = PAIR ? 2 : 1;
+  static constexpr int ROW_TILE = TOKENS_X ? 128 * CTAS : BN;     // tokens per tile
   static constexpr int W_TILE = TOKENS_X ? BN : 128;       // weight rows per tile
+  static constexpr int Y_ROWS = BN / CTAS;                 // rows of Y's codes that a CTA holds; it holds the scales of all
   static constexpr int YB = (BN + 127) / 128;              // 128-row groups of Y's scales
-  static constexpr uint32_t X_BYTES = 128 * 128, Y_BYTES = BN * 128;
+  static constexpr uint32_t X_BYTES = 128 * 128, Y_BYTES = Y_ROWS * 128;
   static constexpr uint32_t SF_BYTES = 2 * 512 * (1 + YB);
   static constexpr uint32_t STAGE = X_BYTES + Y_BYTES + SF_BYTES;
   // Two accumulators of 256 columns and the scales do not fit 512 columns: the second one begins 64
@@ -124,11 +171,15 @@ struct Shape {
   static constexpr uint32_t SF_COL = OVERLAP ? 448 : 2 * BN;
   static constexpr uint32_t SF_SET = 8 + 8 * YB;           // columns of one step's scales; two sets alternate
   static_assert(SF_COL + 2 * SF_SET <= 512, "tensor memory");
-  static constexpr uint32_t STAGING = TOKENS_X ? 4 * 4096 : 0;
+  static constexpr uint32_t AHEAD = 4;                     // pairs of steps whose scales are on their way
+  static constexpr uint32_t RAW_SLOT = 128 * 16 * (1 + YB), RAW = AHEAD * RAW_SLOT;
+  static constexpr uint32_t STAGING = TOKENS_X ? 8 * 2048 : 0;    // per result warp: 32 rows of 64 bytes
+  static constexpr uint32_t BIAS = TOKENS_X ? 8 * (BN / 2) * 4 : 0;
   static constexpr uint32_t TABLES = 2 * 4 * (kMaxGroups + 2);
-  static constexpr uint32_t SMEM = 1024 + STAGES * STAGE + STAGING + TABLES + 512;
+  static constexpr uint32_t SMEM = 1024 + STAGES * STAGE + RAW + STAGING + BIAS + TABLES + 512;
   static_assert(SMEM <= 232448, "shared memory");
-  static constexpr uint32_t IDESC = (1u << 7) | (1u << 10) | ((uint32_t)(BN / 8) << 17) | (1u << 23) | (8u << 24);   // E2M1 x E2M1, E8M0 scales, 128 x BN
+  // E2M1 x E2M1, E8M0 scales, 128 (PAIR: 256) x BN
+  static constexpr uint32_t IDESC = (1u << 7) | (1u << 10) | ((uint32_t)(BN / 8) << 17) | (1u << 23) | ((8u * CTAS) << 24);
 };
 
 struct ProductArgs {
@@ -177,21 +228,27 @@ __device__ __forceinline__ bool find_tile(const uint32_t* lo, const uint32_t* cu
   return true;
 }
 
-// Scale bytes 16*v .. 16*v+15 of a row, zeros behind the last block.
-__device__ __forceinline__ uint4 load_scales(const uint8_t* row, uint32_t v, uint32_t blocks, bool vec) {
-  const uint32_t at = 16 * v;
-  if (vec && at + 16 <= blocks) return __ldg(reinterpret_cast<const uint4*>(row + at));
-  uint32_t w[4] = {0, 0, 0, 0};
-#pragma unroll
-  for (uint32_t i = 0; i < 16; ++i)
-    if (at + i < blocks) w[i / 4] |= (uint32_t)__ldg(row + at + i) << (8 * (i % 4));
-  return make_uint4(w[0], w[1], w[2], w[3]);
+// n <= 16 scale bytes into this thread's 16 bytes of shared memory, zeros behind them.  Aligned ones are fetched
+// in the background (cp.async, completed by its group).
+__device__ __noinline__ void bring_bytes(uint8_t* dst, const uint8_t* src, uint32_t n) {
+  for (uint32_t i = 0; i < 16; ++i) dst[i] = i < n ? __ldg(src + i) : (uint8_t)0;
+}
+__device__ __forceinline__ void bring_scales(uint8_t* dst, const uint8_t* src, uint32_t n, bool vec) {
+  if (vec) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_addr(dst)), "l"(src), "r"(n) : "memory");
+  else bring_bytes(dst, src, n);
 }
 
 __device__ __forceinline__ void store_as(void* y, uint64_t at, uint32_t dtype, float v) {
   if (dtype == kBF16) ((__nv_bfloat16*)y)[at] = __float2bfloat16_rn(v);
   else if (dtype == kF16) ((__half*)y)[at] = __float2half_rn(v);
   else ((float*)y)[at] = v;
+}
+// 16 results that lie `ld` apart.
+template <class T>
+__device__ __forceinline__ void store_column(T* y, uint64_t ld, const uint32_t (&v)[16], float bias, uint32_t n) {
+#pragma unroll
+  for (uint32_t j = 0; j < 16; ++j)
+    if (j < n) y[j * ld] = Chunk8<T>::narrow(__uint_as_float(v[j]) + bias);
 }
 __device__ __forceinline__ uint32_t pack2(uint32_t dtype, float a, float b) {
   if (dtype == kBF16) { __nv_bfloat162 h = __floats2bfloat162_rn(a, b); return *reinterpret_cast<uint32_t*>(&h); }
@@ -207,30 +264,33 @@ __device__ __forceinline__ void cluster_sync() {
 template <class S>
 __global__ void __launch_bounds__(kProductThreads, 1)
 mx_matmul_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_y, const ProductArgs p) {
+  constexpr bool PAIR = S::PAIR;
   extern __shared__ uint8_t raw[];
   const uint32_t raw_addr = smem_addr(raw);
   uint8_t* const base = raw + ((1024u - (raw_addr & 1023u)) & 1023u);     // swizzled tiles start at multiples of 1024
   const uint32_t base_addr = smem_addr(base);
-  // codes of all stages, then scales of all stages, then the rest
+  // codes of all stages, scales of all stages, scales as they lie in memory, then the rest
   constexpr uint32_t CODES = S::X_BYTES + S::Y_BYTES;
   uint8_t* const sf = base + S::STAGES * CODES;
   const uint32_t sf_addr = base_addr + S::STAGES * CODES;
-  uint8_t* const staging = sf + S::STAGES * S::SF_BYTES;
-  uint32_t* const lo = reinterpret_cast<uint32_t*>(staging + S::STAGING);
+  uint8_t* const bytes_ring = sf + S::STAGES * S::SF_BYTES;
+  uint8_t* const staging = bytes_ring + S::RAW;
+  float* const bias_rows = reinterpret_cast<float*>(staging + S::STAGING);
+  uint32_t* const lo = reinterpret_cast<uint32_t*>(staging + S::STAGING + S::BIAS);
   uint32_t* const cum = lo + kMaxGroups + 2;
   uint64_t* const bars = reinterpret_cast<uint64_t*>(cum + kMaxGroups + 2);
   const uint32_t bar0 = smem_addr(bars);
-  auto full_codes = [&](uint32_t s) { return bar0 + 8 * s; };
-  auto full_scales = [&](uint32_t s) { return bar0 + 8 * (S::STAGES + s); };
-  auto empty = [&](uint32_t s) { return bar0 + 8 * (2 * S::STAGES + s); };
-  auto acc_full = [&](uint32_t b) { return bar0 + 8 * (3 * S::STAGES + b); };
-  auto acc_free = [&](uint32_t b) { return bar0 + 8 * (3 * S::STAGES + 2 + b); };
-  const uint32_t drained = bar0 + 8 * (3 * S::STAGES + 4);
-  static_assert(8 * (3 * S::STAGES + 5) + 8 <= 512, "barriers");
-  uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(bars + 3 * S::STAGES + 5);
+  const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const uint32_t half = PAIR ? blockIdx.x % 2 : 0;                         // place in the pair; the first one issues the products
+  auto full = [&](uint32_t s) { return bar0 + 8 * s; };                    // codes and scales of a stage are there (first CTA's counts)
+  auto empty = [&](uint32_t s) { return bar0 + 8 * (S::STAGES + s); };
+  auto acc_full = [&](uint32_t b) { return bar0 + 8 * (2 * S::STAGES + b); };
+  auto acc_free = [&](uint32_t b) { return bar0 + 8 * (2 * S::STAGES + 2 + b); };   // (first CTA's counts)
+  const uint32_t drained = bar0 + 8 * (2 * S::STAGES + 4);
+  static_assert(8 * (2 * S::STAGES + 5) + 8 <= 512, "barriers");
+  uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * S::STAGES + 5);
   volatile uint32_t* const failed = tmem_slot + 1;
 
-  const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   if (!p.early) dependency_wait();
   allow_dependents();
 
@@ -239,307 +299,386 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constan
     int64_t o = p.offsets ? __ldg(p.offsets + g) : (g ? (int64_t)p.m : 0);
     lo[g] = (uint32_t)(o < 0 ? 0 : o > (int64_t)p.m ? (int64_t)p.m : o);
   }
-  if (threadIdx.x == 0) {
-    for (uint32_t s = 0; s < S::STAGES; ++s) { bar_init(full_codes(s), 1); bar_init(full_scales(s), 4); bar_init(empty(s), 1); }
-    for (uint32_t b = 0; b < 2; ++b) { bar_init(acc_full(b), 1); bar_init(acc_free(b), 4); }
-    bar_init(drained, 1);
-    *failed = 0;
-    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    asm volatile("prefetch.tensormap [%0];" ::"l"(&map_x) : "memory");
-    asm volatile("prefetch.tensormap [%0];" ::"l"(&map_y) : "memory");
-  }
-  if (warp == 2) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(tmem_slot)) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-  }
-  tc_fence_before();
-  __syncthreads();
-  tc_fence_after();
-  if (warp == 0) {
-    uint32_t carry = 0;
-    for (uint32_t g0 = 0; g0 <= p.groups; g0 += 32) {      // running maximum
-      uint32_t v = g0 + lane <= p.groups ? lo[g0 + lane] : 0;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) { const uint32_t u = __shfl_up_sync(0xffffffffu, v, o); if (lane >= o) v = max(v, u); }
-      v = max(v, carry);
-      if (g0 + lane <= p.groups) lo[g0 + lane] = v;
-      carry = __shfl_sync(0xffffffffu, v, 31);
+  if (warp == 3) {
+    if (elect_one()) {
+#pragma unroll 1
+      for (uint32_t s = 0; s < S::STAGES; ++s) { bar_init(full(s), 1 + 4 * S::CTAS); bar_init(empty(s), 1); }
+#pragma unroll 1
+      for (uint32_t b = 0; b < 2; ++b) { bar_init(acc_full(b), 1); bar_init(acc_free(b), 8 * S::CTAS); }
+      bar_init(drained, 1);
+      *failed = 0;
+      asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     __syncwarp();
-    carry = 0;
-    for (uint32_t g0 = 0; g0 < p.groups; g0 += 32) {       // running sum of row tiles
-      const uint32_t g = g0 + lane;
-      uint32_t v = g < p.groups ? (lo[g + 1] - lo[g] + S::ROW_TILE - 1) / S::ROW_TILE : 0;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) { const uint32_t u = __shfl_up_sync(0xffffffffu, v, o); if (lane >= o) v += u; }
-      v += carry;
-      if (g < p.groups) cum[g + 1] = v;
-      carry = __shfl_sync(0xffffffffu, v, 31);
+  } else if (warp == 2) {
+    if constexpr (PAIR) {
+      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(tmem_slot)) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    } else {
+      asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(tmem_slot)) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
-    if (lane == 0) cum[0] = 0;
+  } else if (warp == 0) {
+    if (elect_one()) {
+      asm volatile("prefetch.tensormap [%0];" ::"l"(&map_x) : "memory");
+      asm volatile("prefetch.tensormap [%0];" ::"l"(&map_y) : "memory");
+    }
+    __syncwarp();
   }
-  __syncthreads();
+  if (p.groups > 1) {
+    __syncthreads();
+    if (warp == 4) {
+      uint32_t carry = 0;
+#pragma unroll 1
+      for (uint32_t g0 = 0; g0 <= p.groups; g0 += 32) {      // running maximum
+        uint32_t v = g0 + lane <= p.groups ? lo[g0 + lane] : 0;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) { const uint32_t u = __shfl_up_sync(0xffffffffu, v, o); if (lane >= o) v = max(v, u); }
+        v = max(v, carry);
+        if (g0 + lane <= p.groups) lo[g0 + lane] = v;
+        carry = __shfl_sync(0xffffffffu, v, 31);
+      }
+      __syncwarp();
+      carry = 0;
+#pragma unroll 1
+      for (uint32_t g0 = 0; g0 < p.groups; g0 += 32) {       // running sum of row tiles
+        const uint32_t g = g0 + lane;
+        uint32_t v = g < p.groups ? (lo[g + 1] - lo[g] + S::ROW_TILE - 1) / S::ROW_TILE : 0;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) { const uint32_t u = __shfl_up_sync(0xffffffffu, v, o); if (lane >= o) v += u; }
+        v += carry;
+        if (g < p.groups) cum[g + 1] = v;
+        carry = __shfl_sync(0xffffffffu, v, 31);
+      }
+      if (lane == 0) cum[0] = 0;
+    }
+  } else if (threadIdx.x == 128) {
+    const int64_t m = p.m, first = p.offsets ? min(max(__ldg(p.offsets), (int64_t)0), m) : 0, last = p.offsets ? min(max(__ldg(p.offsets + 1), first), m) : m;
+    lo[0] = (uint32_t)first; lo[1] = (uint32_t)last;
+    cum[0] = 0; cum[1] = (uint32_t)(last - first + S::ROW_TILE - 1) / S::ROW_TILE;
+  }
+  __syncwarp();
+  tc_fence_before();
+  if constexpr (PAIR) cluster_sync(); else __syncthreads();
+  tc_fence_after();
   const uint32_t tmem = *tmem_slot;
 
-  // this CTA's tiles: tile0, tile0 + stride, ...; the steps of a tile are cut over the cluster in pairs
-  const uint32_t rank = p.splits > 1 ? blockIdx.x % p.splits : 0;
-  const uint32_t tile0 = blockIdx.x / p.splits, stride = gridDim.x / p.splits;
-  const uint32_t pairs = (p.steps + 1) / 2;
-  const uint32_t step_begin = 2 * (uint32_t)((uint64_t)pairs * rank / p.splits);
-  const uint32_t step_end = min(p.steps, 2 * (uint32_t)((uint64_t)pairs * (rank + 1) / p.splits));
+  // this CTA's (pair's) tiles: tile0, tile0 + stride, ...; the steps of a tile are cut over the cluster in twos
+  const uint32_t rank = PAIR ? 0 : blockIdx.x % p.splits, width = PAIR ? 2 : p.splits;
+  const uint32_t tile0 = blockIdx.x / width, stride = gridDim.x / width;
+  const uint32_t twos = (p.steps + 1) / 2;
+  const uint32_t step_begin = 2 * (uint32_t)((uint64_t)twos * rank / p.splits);
+  const uint32_t step_end = min(p.steps, 2 * (uint32_t)((uint64_t)twos * (rank + 1) / p.splits));
   Where at;
 
   if (warp == 0) {
     // ---------------------------------------------------------------------------------- codes
-    if (lane == 0) {
-      uint32_t it = 0;                        // fills so far
-      auto fetch_w = [&](uint32_t s, uint32_t step) {
-        if (S::TOKENS_X) tma_load(base_addr + s * CODES + S::X_BYTES, &map_y, full_codes(s), step * 128, at.w0, at.group);
-        else tma_load(base_addr + s * CODES, &map_x, full_codes(s), step * 128, at.w0, at.group);
-      };
-      auto fetch_a = [&](uint32_t s, uint32_t step) {
-        if (S::TOKENS_X) tma_load(base_addr + s * CODES, &map_x, full_codes(s), step * 128, at.token0, 0);
-        else tma_load(base_addr + s * CODES + S::X_BYTES, &map_y, full_codes(s), step * 128, at.token0, 0);
-      };
-      bool first = p.early != 0;
-      for (uint32_t tile = tile0; find_tile<S>(lo, cum, p.groups, p.w_tiles, tile, &at); tile += stride) {
-        uint32_t step = step_begin;
-        if (first) {
-          // the weights of the first stages do not depend on the kernel that is rounding the activations
-          const uint32_t n = min(step_end - step, (uint32_t)S::STAGES);
-          for (uint32_t i = 0; i < n; ++i) { bar_expect(full_codes(i), CODES); fetch_w(i, step + i); }
-          dependency_wait();
-          for (uint32_t i = 0; i < n; ++i) fetch_a(i, step + i);
-          step += n; it = n;
-          first = false;
+    uint32_t s = 0, phase = 1, fills = 0;     // the first wait for an empty stage is for the phase before the first
+    const uint32_t full0 = PAIR ? at_rank(full(0), 0) : full(0);
+    auto fetch = [&](uint32_t stage, uint32_t step, bool weights) {
+      const bool x = weights != S::TOKENS_X;
+      const int row = (int)(weights ? at.w0 + (x ? 0 : S::Y_ROWS * half) : at.token0 + (x ? 128 * half : 0));
+      tma_load<PAIR>(base_addr + stage * CODES + (x ? 0 : S::X_BYTES), x ? &map_x : &map_y, full0 + 8 * stage, (int)step * 128, row, weights ? (int)at.group : 0);
+    };
+    bool first = p.early != 0, ok = true;
+#pragma unroll 1
+    for (uint32_t tile = tile0; ok && find_tile<S>(lo, cum, p.groups, p.w_tiles, tile, &at); tile += stride) {
+      uint32_t step = step_begin;
+      if (first) {
+        // the weights of the first stages do not depend on the kernel that is rounding the activations
+        const uint32_t n = min(step_end - step, (uint32_t)S::STAGES);
+        if (elect_one()) {
+#pragma unroll 1
+          for (uint32_t i = 0; i < n; ++i) {
+            if (half == 0) bar_expect(full(i), S::CTAS * CODES);
+            fetch(i, step + i, true);
+          }
         }
-        for (; step < step_end; ++step, ++it) {
-          const uint32_t s = it % S::STAGES;
-          if (it >= S::STAGES && !bar_wait(empty(s), (it / S::STAGES - 1) & 1, failed)) goto out;
-          bar_expect(full_codes(s), CODES);
-          fetch_w(s, step);
-          fetch_a(s, step);
+        __syncwarp();
+        dependency_wait();
+        if (elect_one()) {
+#pragma unroll 1
+          for (uint32_t i = 0; i < n; ++i) fetch(i, step + i, false);
         }
+        __syncwarp();
+        step += n; fills = n; s = n;
+        if (s == S::STAGES) { s = 0; phase = 0; }
+        first = false;
       }
-    out:
-      if (*failed)                            // leave no copy in flight
-        for (uint32_t i = it > S::STAGES ? it - S::STAGES : 0; i < it; ++i) {
-          const uint64_t begin = now_ns();
-          while (!bar_try(full_codes(i % S::STAGES), (i / S::STAGES) & 1) && now_ns() - begin < kWaitLimitNs) {}
+#pragma unroll 1
+      for (; step < step_end; ++step) {
+        if (!bar_wait(empty(s), phase, failed)) { ok = false; break; }
+        if (elect_one()) {
+          if (half == 0) bar_expect(full(s), S::CTAS * CODES);
+          fetch(s, step, true);
+          fetch(s, step, false);
         }
+        __syncwarp();
+        ++fills;
+        if (++s == S::STAGES) { s = 0; phase ^= 1; }
+      }
     }
-  } else if (warp == 1) {
+    if (*failed) {                            // leave no copy in flight: what was asked for last has landed long before the limit passes
+      const uint64_t begin = now_ns();
+      for (uint32_t i = fills > S::STAGES ? fills - S::STAGES : 0; i < fills; ++i)
+        while (!bar_try(full(i % S::STAGES), (i / S::STAGES) & 1) && now_ns() - begin < kWaitLimitNs / 20) {}
+    }
+  } else if (warp == 1 && half == 0) {
     // ---------------------------------------------------------------------------------- products
-    if (lane == 0) {
-      uint32_t it = 0, done = 0;              // steps and tiles so far
-      for (uint32_t tile = tile0; find_tile<S>(lo, cum, p.groups, p.w_tiles, tile, &at); tile += stride, ++done) {
-        const uint32_t b = done & 1;
-        // OVERLAP: the predecessor has left the shared columns; else: the tile before it has left this buffer
-        if (S::OVERLAP ? done >= 1 && !bar_wait(acc_free(b ^ 1), ((done - 1) / 2) & 1, failed)
-                       : done >= 2 && !bar_wait(acc_free(b), (done / 2 - 1) & 1, failed)) break;
+    uint32_t s = 0, phase = 0, set = 0, done = 0;
+#pragma unroll 1
+    for (uint32_t tile = tile0; find_tile<S>(lo, cum, p.groups, p.w_tiles, tile, &at); tile += stride, ++done) {
+      const uint32_t b = done & 1;
+      // OVERLAP: the predecessor has left the shared columns; else: the tile before it has left this buffer
+      if (S::OVERLAP ? done >= 1 && !bar_wait(acc_free(b ^ 1), ((done - 1) / 2) & 1, failed)
+                     : done >= 2 && !bar_wait(acc_free(b), (done / 2 - 1) & 1, failed)) break;
+      tc_fence_after();
+      const uint32_t acc = tmem + b * S::ACC_STEP;
+      bool ok = true;
+#pragma unroll 1
+      for (uint32_t step = step_begin; step < step_end; ++step) {
+        if (!bar_wait(full(s), phase, failed)) { ok = false; break; }
         tc_fence_after();
-        const uint32_t acc = tmem + b * S::ACC_STEP;
-        bool ok = true;
-        for (uint32_t step = step_begin; step < step_end; ++step, ++it) {
-          const uint32_t s = it % S::STAGES, phase = (it / S::STAGES) & 1;
-          if (!bar_wait(full_scales(s), phase, failed) || !bar_wait(full_codes(s), phase, failed)) { ok = false; break; }
-          tc_fence_after();
-          const uint32_t sfx = tmem + S::SF_COL + (it & 1) * S::SF_SET, sfy = sfx + 8;
-          const uint32_t src = sf_addr + s * S::SF_BYTES;
+        if (elect_one()) {
+          const uint32_t sfx = tmem + S::SF_COL + set, sfy = sfx + 8;
+          const uint64_t src = scales_desc(sf_addr + s * S::SF_BYTES);
 #pragma unroll
           for (uint32_t h = 0; h < 2; ++h) {
-            tc_copy_scales(sfx + 4 * h, scales_desc(src + 512 * h));
+            tc_copy_scales<PAIR>(sfx + 4 * h, src + 32 * h);
 #pragma unroll
-            for (uint32_t y = 0; y < S::YB; ++y)
-              tc_copy_scales(sfy + 4 * (h * S::YB + y), scales_desc(src + 1024 + 512 * (h * S::YB + y)));
+            for (uint32_t y = 0; y < S::YB; ++y) tc_copy_scales<PAIR>(sfy + 4 * (h * S::YB + y), src + 64 + 32 * (h * S::YB + y));
           }
           const uint64_t dx = codes_desc(base_addr + s * CODES), dy = codes_desc(base_addr + s * CODES + S::X_BYTES);
 #pragma unroll
           for (uint32_t k = 0; k < 4; ++k) {  // 64 columns each: 32 bytes along the row, two of the word's four scales
             const uint32_t id = 2 * (k & 1);
-            tc_mma(acc, dx + 2 * k, dy + 2 * k, S::IDESC | (id << 29) | (id << 4), sfx + 4 * (k / 2), sfy + 4 * S::YB * (k / 2),
-                   step > step_begin || k > 0);
+            tc_mma<PAIR>(acc, dx + 2 * k, dy + 2 * k, S::IDESC | (id << 29) | (id << 4), sfx + 4 * (k / 2), sfy + 4 * S::YB * (k / 2),
+                         step > step_begin || k > 0);
           }
-          tc_commit(empty(s));
+          tc_commit<PAIR>(empty(s));
         }
-        if (!ok) break;
-        tc_commit(acc_full(b));
+        __syncwarp();
+        set ^= S::SF_SET;
+        if (++s == S::STAGES) { s = 0; phase ^= 1; }
       }
-      if (*failed) {                          // leave no product in flight
-        tc_commit(drained);
-        const uint64_t begin = now_ns();
-        while (!bar_try(drained, 0) && now_ns() - begin < kWaitLimitNs) {}
-      }
+      if (!ok) break;
+      if (elect_one()) tc_commit<PAIR>(acc_full(b));
+      __syncwarp();
     }
-  } else if (warp >= 8) {
+    if (*failed) {                            // leave no product in flight
+      if (elect_one()) tc_commit<PAIR>(drained);
+      __syncwarp();
+      const uint64_t begin = now_ns();
+      while (!bar_try(drained, 0) && now_ns() - begin < kWaitLimitNs) {}
+    }
+  } else if (warp >= 12) {
     // ---------------------------------------------------------------------------------- scales
-    const uint32_t t = threadIdx.x - 256;
+    const uint32_t t = threadIdx.x - 384;
     if (p.early) dependency_wait();
-    constexpr int AHEAD = 4;                  // pairs of steps in flight
-    constexpr int YV = S::YB;
-    struct Pair { uint4 x, y[YV]; uint32_t n; } ring[AHEAD];
-    // the sequence of pairs to fetch
-    uint32_t tile = tile0, pair = 0;
-    const uint8_t *px = nullptr, *py[YV];
-    bool live = true, begun = false;
-    auto fetch = [&](Pair& r) {
-      r.n = 0; r.x = make_uint4(0, 0, 0, 0);
+    const uint32_t full0 = PAIR ? at_rank(full(0), 0) : full(0);
+    const bool vec_x = p.x_vec != 0, vec_y = p.y_vec != 0;
+    uint8_t* const mine = bytes_ring + 16 * t;     // of slot i: + i * RAW_SLOT; X's row, then 2048 bytes on Y's, and its row 128 below
+    // The sequence of pairs of steps, fetched AHEAD of the one that is unpacked.  Rows past the end of a matrix take
+    // the scales of its last row: they scale results that nobody stores.
+    uint32_t tile = tile0, two = 0, slot_in = 0;
+    const uint8_t *px = nullptr, *py[S::YB];
+    bool live = find_tile<S>(lo, cum, p.groups, p.w_tiles, tile, &at);
+    auto enter = [&] {
+      two = step_begin / 2;
+      const uint32_t xr = min((S::TOKENS_X ? at.token0 + 128 * half : at.w0) + t, p.x_rows - 1);
+      px = p.x_scales + (S::TOKENS_X ? 0 : at.group * p.x_sgs) + xr * p.x_sld + 16ull * two;
 #pragma unroll
-      for (int i = 0; i < YV; ++i) r.y[i] = make_uint4(0, 0, 0, 0);
-      if (!live) return;
-      if (!begun || 2 * pair >= step_end) {
-        if (begun) tile += stride;
-        begun = true;
-        if (!find_tile<S>(lo, cum, p.groups, p.w_tiles, tile, &at)) { live = false; return; }
-        pair = step_begin / 2;
-        const uint32_t xr = (S::TOKENS_X ? at.token0 : at.w0) + t;
-        px = xr < p.x_rows ? p.x_scales + (S::TOKENS_X ? 0 : at.group * p.x_sgs) + xr * p.x_sld : nullptr;
+      for (int i = 0; i < S::YB; ++i) {
+        const uint32_t yr = min((S::TOKENS_X ? at.w0 : at.token0) + t + 128 * i, p.y_rows - 1);
+        py[i] = p.y_scales + (S::TOKENS_X ? at.group * p.y_sgs : 0) + yr * p.y_sld + 16ull * two;
+      }
+    };
+    auto fetch = [&] {                             // one pair of steps into the next slot, or nothing; always one group
+      if (live) {
+        uint8_t* dst = mine + slot_in * S::RAW_SLOT;
+        const uint32_t n = min(p.blocks - 16 * two, 16u);
+        bring_scales(dst, px, n, vec_x);
+        px += 16;
 #pragma unroll
-        for (int i = 0; i < YV; ++i) {
-          const uint32_t yr = (S::TOKENS_X ? at.w0 : at.token0) + t + 128 * i;
-          py[i] = t + 128 * i < S::BN && yr < p.y_rows ? p.y_scales + (S::TOKENS_X ? at.group * p.y_sgs : 0) + yr * p.y_sld : nullptr;
+        for (int i = 0; i < S::YB; ++i) {
+          if (t + 128 * i < S::BN) bring_scales(dst + 2048 * (1 + i), py[i], n, vec_y);
+          py[i] += 16;
+        }
+        if (2 * ++two >= step_end) {
+          tile += stride;
+          live = find_tile<S>(lo, cum, p.groups, p.w_tiles, tile, &at);
+          if (live) enter();
         }
       }
-      if (px) r.x = load_scales(px, pair, p.blocks, p.x_vec);
-#pragma unroll
-      for (int i = 0; i < YV; ++i)
-        if (py[i]) r.y[i] = load_scales(py[i], pair, p.blocks, p.y_vec);
-      r.n = min(2u, step_end - 2 * pair);
-      ++pair;
+      slot_in = slot_in + 1 == S::AHEAD ? 0 : slot_in + 1;
+      asm volatile("cp.async.commit_group;" ::: "memory");
     };
-#pragma unroll
-    for (int i = 0; i < AHEAD; ++i) fetch(ring[i]);
-    uint32_t it = 0;
+    if (live) enter();
+#pragma unroll 1
+    for (uint32_t i = 0; i + 1 < S::AHEAD; ++i) fetch();
+    uint32_t s = 0, phase = 1, slot = 0;
     const uint32_t word = (t % 32) * 16 + (t / 32) * 4;
-    for (bool more = true; more;) {
+    Where now;
+    bool ok = true;
+#pragma unroll 1
+    for (uint32_t tile_now = tile0; ok && find_tile<S>(lo, cum, p.groups, p.w_tiles, tile_now, &now); tile_now += stride) {
+#pragma unroll 1
+      for (uint32_t step = step_begin; step < step_end; step += 2) {
+        fetch();
+        asm volatile("cp.async.wait_group %0;" ::"n"(S::AHEAD - 1) : "memory");
+        // both steps at once
+        const bool both = step + 1 < step_end;
+        const uint32_t s1 = s + 1 == S::STAGES ? 0 : s + 1, phase1 = s + 1 == S::STAGES ? phase ^ 1 : phase;
+        if (!bar_wait(empty(s), phase, failed) || (both && !bar_wait(empty(s1), phase1, failed))) { ok = false; break; }
+        const uint8_t* src = mine + slot * S::RAW_SLOT;
+        uint8_t *d0 = sf + s * S::SF_BYTES + word, *d1 = sf + s1 * S::SF_BYTES + word;
 #pragma unroll
-      for (int i = 0; i < AHEAD; ++i) {
-        if (!more) break;
-        Pair& r = ring[i];
-        if (r.n == 0) { more = false; break; }
-#pragma unroll
-        for (uint32_t h = 0; h < 2; ++h) {
-          if (h >= r.n) break;
-          const uint32_t s = it % S::STAGES;
-          if (it >= S::STAGES && !bar_wait(empty(s), (it / S::STAGES - 1) & 1, failed)) { more = false; break; }
-          uint8_t* dst = sf + s * S::SF_BYTES + word;
-          *reinterpret_cast<uint32_t*>(dst) = h ? r.x.z : r.x.x;
-          *reinterpret_cast<uint32_t*>(dst + 512) = h ? r.x.w : r.x.y;
-#pragma unroll
-          for (int y = 0; y < YV; ++y) {
-            *reinterpret_cast<uint32_t*>(dst + 1024 + 512 * y) = h ? r.y[y].z : r.y[y].x;
-            *reinterpret_cast<uint32_t*>(dst + 1024 + 512 * (YV + y)) = h ? r.y[y].w : r.y[y].y;
+        for (int i = 0; i <= S::YB; ++i) {         // X, then Y's groups of 128 rows
+          const uint4 v = *reinterpret_cast<const uint4*>(src + 2048 * i);
+          const uint32_t at0 = i == 0 ? 0 : 1024 + 512 * (i - 1), at1 = i == 0 ? 512 : 1024 + 512 * (S::YB + i - 1);
+          *reinterpret_cast<uint32_t*>(d0 + at0) = v.x;
+          *reinterpret_cast<uint32_t*>(d0 + at1) = v.y;
+          if (both) {
+            *reinterpret_cast<uint32_t*>(d1 + at0) = v.z;
+            *reinterpret_cast<uint32_t*>(d1 + at1) = v.w;
           }
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-          __syncwarp();
-          if (lane == 0) bar_arrive(full_scales(s));
-          ++it;
         }
-        if (more) fetch(r);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) {
+          bar_arrive_at<PAIR>(full0 + 8 * s);
+          if (both) bar_arrive_at<PAIR>(full0 + 8 * s1);
+        }
+        slot = slot + 1 == S::AHEAD ? 0 : slot + 1;
+        s = s1; phase = phase1;
+        if (both && ++s == S::STAGES) { s = 0; phase ^= 1; }
       }
     }
+    asm volatile("cp.async.wait_all;" ::: "memory");
   } else if (warp >= 4) {
     // ---------------------------------------------------------------------------------- results
-    const uint32_t quarter = warp - 4;        // warp w may read lanes 32 * (w % 4) and up
+    const uint32_t quarter = warp % 4;        // the lanes that a warp may read follow from its number
+    const uint32_t side = (warp - 4) / 4;     // which half of the columns
     const uint32_t lanes = (quarter * 32) << 16;
     if (p.early) dependency_wait();
+    const uint32_t free0 = PAIR ? at_rank(acc_free(0), 0) : acc_free(0);
     uint32_t done = 0;
+#pragma unroll 1
     for (uint32_t tile = tile0; find_tile<S>(lo, cum, p.groups, p.w_tiles, tile, &at); tile += stride, ++done) {
       const uint32_t b = done & 1;
-      if (!bar_wait(acc_full(b), (done / 2) & 1, failed)) break;
-      tc_fence_after();
-      const uint32_t acc = tmem + b * S::ACC_STEP + lanes;
       if constexpr (S::TOKENS_X) {
-        // lane = token, columns = weight rows: 64 columns at a time, the ones shared with the next tile first
-        uint8_t* const mine = staging + quarter * 4096;
-        const uint32_t esz = p.dtype == kF32 ? 4 : 2;
-        const float* bias = p.bias ? p.bias + (uint64_t)at.group * p.n : nullptr;
-        const uint32_t row0 = at.token0 + quarter * 32;
+        constexpr uint32_t COLS = S::BN / 2;  // columns of this warp
+        const uint32_t w0 = at.w0 + side * COLS;
+        float* const bias_row = bias_rows + (warp - 4) * COLS;
+        if (p.bias) {                         // the warp's part of the bias, while the products are at work
+          for (uint32_t i = lane; i < COLS; i += 32) bias_row[i] = w0 + i < p.n ? __ldg(p.bias + (uint64_t)at.group * p.n + w0 + i) : 0.f;
+          __syncwarp();
+        }
+        if (!bar_wait(acc_full(b), (done / 2) & 1, failed)) break;
+        tc_fence_after();
+        const uint32_t acc = tmem + b * S::ACC_STEP + side * COLS + lanes;
+        // The columns shared with the next tile are the last 64 of the first buffer and the first 64 of the second:
+        // they go first, and a warp that has none of them lets the next tile in at once.
+        const bool shares = side != b;
+        if (!shares && lane == 0) bar_arrive_at<PAIR>(free0 + 8 * b);
+        // lane = token, columns = weight rows, 32 at a time
+        uint8_t* const mine = staging + (warp - 4) * 2048;
+        const bool wide = p.dtype == kF32;
+        const uint32_t row0 = at.token0 + 128 * half + quarter * 32;
         const uint32_t rows = row0 < at.token_end ? min(32u, at.token_end - row0) : 0;
 #pragma unroll 1
-        for (uint32_t c = 0; c < S::BN / 64; ++c) {
-          const uint32_t cc = b == 0 ? (c + S::BN / 64 - 1) % (S::BN / 64) : c;
-          uint32_t v[2][32];
-          tc_load32(acc + 64 * cc, v[0]);
-          tc_load32(acc + 64 * cc + 32, v[1]);
+        for (uint32_t c = 0; c < COLS / 32; ++c) {
+          const uint32_t cc = b == 0 ? c ^ 2 : c;
+          uint32_t v[32];
+          tc_load32(acc + 32 * cc, v);
           tc_load_wait();
-          if (c == 0) {
+          if (c == 1 && shares) {
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) bar_arrive(acc_free(b));
+            if (lane == 0) bar_arrive_at<PAIR>(free0 + 8 * b);
           }
-          const uint32_t col0 = at.w0 + 64 * cc;
-          if (col0 >= p.n) continue;
+          if (p.bias) {
 #pragma unroll
-          for (uint32_t h = 0; h < 2; ++h) {
-            const uint32_t col = col0 + 32 * h;
-            if (bias) {
-#pragma unroll
-              for (uint32_t j = 0; j < 32; ++j)
-                if (col + j < p.n) v[h][j] = __float_as_uint(__uint_as_float(v[h][j]) + __ldg(bias + col + j));
+            for (uint32_t j = 0; j < 32; j += 4) {
+              const float4 f = *reinterpret_cast<const float4*>(bias_row + 32 * cc + j);
+              v[j] = __float_as_uint(__uint_as_float(v[j]) + f.x); v[j + 1] = __float_as_uint(__uint_as_float(v[j + 1]) + f.y);
+              v[j + 2] = __float_as_uint(__uint_as_float(v[j + 2]) + f.z); v[j + 3] = __float_as_uint(__uint_as_float(v[j + 3]) + f.w);
             }
-            // rows of 128 bytes, 16-byte pieces swizzled by the row so that neither side meets bank conflicts
-            if (esz == 2) {
+          }
+          if (p.dtype == kBF16) {
 #pragma unroll
-              for (uint32_t j = 0; j < 4; ++j) {
-                uint32_t o[4];
+            for (uint32_t j = 0; j < 16; ++j) v[j] = pack2(kBF16, __uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1]));
+          } else if (p.dtype == kF16) {
 #pragma unroll
-                for (uint32_t e = 0; e < 4; ++e)
-                  o[e] = pack2(p.dtype, __uint_as_float(v[h][8 * j + 2 * e]), __uint_as_float(v[h][8 * j + 2 * e + 1]));
-                *reinterpret_cast<uint4*>(mine + lane * 128 + (((4 * h + j) ^ (lane & 7)) * 16)) = make_uint4(o[0], o[1], o[2], o[3]);
-              }
-              if (h == 0) continue;
-            } else {
+            for (uint32_t j = 0; j < 16; ++j) v[j] = pack2(kF16, __uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1]));
+          }
+          // Staged as rows of 64 bytes (32 results of 16 bits; 16 of 32 bits, in two rounds) whose four 16-byte pieces
+          // are swizzled by the row so that neither side meets bank conflicts.
+          const uint32_t shift = wide ? 2 : 1, most = 64u >> shift;
+#pragma unroll 1
+          for (uint32_t round = 0; round < (wide ? 2u : 1u); ++round) {
+            uint8_t* const row = mine + lane * 64;
+            const uint32_t sw = (lane >> 1) & 3;
 #pragma unroll
-              for (uint32_t j = 0; j < 8; ++j)
-                *reinterpret_cast<uint4*>(mine + lane * 128 + ((j ^ (lane & 7)) * 16)) = make_uint4(v[h][4 * j], v[h][4 * j + 1], v[h][4 * j + 2], v[h][4 * j + 3]);
+            for (uint32_t j = 0; j < 4; ++j) {
+              const bool hi = round != 0;
+              *reinterpret_cast<uint4*>(row + ((j ^ sw) * 16)) =
+                  make_uint4(hi ? v[16 + 4 * j] : v[4 * j], hi ? v[17 + 4 * j] : v[4 * j + 1], hi ? v[18 + 4 * j] : v[4 * j + 2], hi ? v[19 + 4 * j] : v[4 * j + 3]);
             }
             __syncwarp();
-            const uint32_t begin = esz == 2 ? col0 : col;          // first column of the staged rows
-            const uint32_t bytes = min((p.n - begin) * esz, 128u); // (col0 < n; the second half may lie behind the end)
-            if (begin < p.n) {
+            const uint32_t col = w0 + 32 * cc + 16 * round;                      // first column of the staged rows
+            const uint32_t cols = col < p.n ? min(p.n - col, most) : 0;
+            uint8_t* const out = (uint8_t*)p.out + (((uint64_t)row0 * p.out_ld + col) << shift);
+            if (p.out_vec && cols == most) {
+              const uint32_t r = lane / 4, piece = lane % 4;
+              uint8_t* dst = out + ((r * p.out_ld) << shift) + 16 * piece;
+              const uint8_t* from = mine + r * 64 + ((piece ^ ((r >> 1) & 3)) * 16);
 #pragma unroll
-              for (uint32_t i = 0; i < 8; ++i) {
-                const uint32_t r = 4 * i + lane / 8, piece = lane % 8;
-                if (r >= rows || 16 * piece >= bytes) continue;
-                const uint4 o = *reinterpret_cast<const uint4*>(mine + r * 128 + ((piece ^ (r & 7)) * 16));
-                uint8_t* dst = (uint8_t*)p.out + ((uint64_t)(row0 + r) * p.out_ld + begin) * esz + 16 * piece;
-                if (p.out_vec && 16 * piece + 16 <= bytes) {
-                  *reinterpret_cast<uint4*>(dst) = o;
-                } else {
-                  const uint32_t w[4] = {o.x, o.y, o.z, o.w};
-#pragma unroll
-                  for (uint32_t e = 0; e < 8; ++e) {
-                    if (esz == 2) { if (16 * piece + 2 * e < bytes) reinterpret_cast<uint16_t*>(dst)[e] = (uint16_t)(w[e / 2] >> (16 * (e % 2))); }
-                    else if (e < 4 && 16 * piece + 4 * e < bytes) reinterpret_cast<uint32_t*>(dst)[e] = w[e];
-                  }
-                }
+              for (uint32_t i = 0; i < 4; ++i) {
+                if (8 * i + r < rows) *reinterpret_cast<uint4*>(dst) = *reinterpret_cast<const uint4*>(from + 512 * i);
+                dst += (8 * p.out_ld) << shift;
+              }
+            } else {
+#pragma unroll 1
+              for (uint32_t i = lane; i < rows * 32; i += 32) {                  // 32 places a row, the columns that exist
+                const uint32_t r = i / 32, e = i % 32;
+                if (e >= cols) continue;
+                const uint8_t* from = mine + r * 64 + ((((e << shift) / 16) ^ ((r >> 1) & 3)) * 16) + ((e << shift) % 16);
+                uint8_t* dst = out + ((r * p.out_ld + e) << shift);
+                if (wide) *reinterpret_cast<uint32_t*>(dst) = *reinterpret_cast<const uint32_t*>(from);
+                else *reinterpret_cast<uint16_t*>(dst) = *reinterpret_cast<const uint16_t*>(from);
               }
             }
             __syncwarp();
           }
         }
       } else {
+        if (!bar_wait(acc_full(b), (done / 2) & 1, failed)) break;
+        tc_fence_after();
+        const uint32_t acc = tmem + b * S::ACC_STEP + lanes;
         // lane = weight row, columns = tokens: 32 lanes write neighbouring results
         const uint32_t n = at.w0 + quarter * 32 + lane;
         const float bias = p.bias && n < p.n ? __ldg(p.bias + (uint64_t)at.group * p.n + n) : 0.f;
         const uint32_t tokens = min((uint32_t)S::BN, at.token_end - at.token0);
         float* part = reinterpret_cast<float*>(base) + quarter * 32 + lane;     // [token][128], over stages that are done with
 #pragma unroll 1
-        for (uint32_t c = 0; c < S::BN; c += 16) {
-          if (c >= tokens) break;
+        for (uint32_t c = 16 * side; c < tokens; c += 32) {
           uint32_t v[16];
           tc_load16(acc + c, v);
           tc_load_wait();
+          if (p.splits > 1) {
 #pragma unroll
-          for (uint32_t j = 0; j < 16; ++j) {
-            if (p.splits > 1) part[(c + j) * 128] = __uint_as_float(v[j]);
-            else if (c + j < tokens && n < p.n) store_as(p.out, (uint64_t)(at.token0 + c + j) * p.out_ld + n, p.dtype, __uint_as_float(v[j]) + bias);
+            for (uint32_t j = 0; j < 16; ++j) part[(c + j) * 128] = __uint_as_float(v[j]);
+          } else if (n < p.n) {
+            const uint64_t to = (uint64_t)(at.token0 + c) * p.out_ld + n;
+            if (p.dtype == kBF16) store_column<__nv_bfloat16>((__nv_bfloat16*)p.out + to, p.out_ld, v, bias, tokens - c);
+            else if (p.dtype == kF16) store_column<__half>((__half*)p.out + to, p.out_ld, v, bias, tokens - c);
+            else store_column<float>((float*)p.out + to, p.out_ld, v, bias, tokens - c);
           }
         }
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) bar_arrive(acc_free(b));
+        if (lane == 0) bar_arrive_at<false>(free0 + 8 * b);
       }
     }
   }
@@ -548,29 +687,38 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constan
   if (!S::TOKENS_X && p.splits > 1) {
     // One tile per cluster: each rank adds up its share of the tokens over all ranks, in their order.
     cluster_sync();
-    if (warp >= 4 && warp < 8 && find_tile<S>(lo, cum, p.groups, p.w_tiles, tile0, &at)) {
-      const uint32_t col = threadIdx.x - 128, n = at.w0 + col;
+    if (find_tile<S>(lo, cum, p.groups, p.w_tiles, tile0, &at)) {
+      const uint32_t col = threadIdx.x % 128, n = at.w0 + col;
       const uint32_t tokens = min((uint32_t)S::BN, at.token_end - at.token0);
       const float bias = p.bias && n < p.n ? __ldg(p.bias + (uint64_t)at.group * p.n + n) : 0.f;
-      for (uint32_t tok = rank; tok < tokens; tok += p.splits) {
-        float sum = 0.f;
-        for (uint32_t r = 0; r < p.splits; ++r) {
-          uint32_t remote;
-          float v;
-          asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(base_addr + (tok * 128 + col) * 4), "r"(r));
-          asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(remote) : "memory");
-          sum += v;
+      uint32_t from[8];
+#pragma unroll
+      for (uint32_t r = 0; r < 8; ++r) from[r] = at_rank(base_addr + col * 4, r < p.splits ? r : 0);
+#pragma unroll 1
+      for (uint32_t tok = rank + p.splits * (threadIdx.x / 128); tok < tokens; tok += 4 * p.splits) {
+        float v[8], sum = 0.f;
+#pragma unroll
+        for (uint32_t r = 0; r < 8; ++r) {
+          v[r] = 0.f;
+          if (r < p.splits) asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v[r]) : "r"(from[r] + tok * 512));
         }
+#pragma unroll
+        for (uint32_t r = 0; r < 8; ++r)
+          if (r < p.splits) sum += v[r];
         if (n < p.n) store_as(p.out, (uint64_t)(at.token0 + tok) * p.out_ld + n, p.dtype, sum + bias);
       }
     }
-    cluster_sync();
   }
+  __syncwarp();
   tc_fence_before();
-  __syncthreads();
+  // no CTA of a cluster leaves while another may still read its memory or arrive at its barriers
+  if (PAIR || p.splits > 1) cluster_sync(); else __syncthreads();
   tc_fence_after();
   if (threadIdx.x == 0 && *failed) { *p.fault = 1; __threadfence_system(); }
-  if (warp == 2) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+  if (warp == 2) {
+    if constexpr (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+    else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+  }
 }
 
 // Products over no columns: the bias, or zero.
@@ -628,7 +776,7 @@ cudaError_t launch_shape(const Launch& l, const MxProduct& q, ProductArgs p, uin
   p.x_vec = vec16(x); p.y_vec = vec16(y);
   CUtensorMap mx, my;
   const uint64_t xg = S::TOKENS_X ? 1 : q.groups, yg = S::TOKENS_X ? q.groups : 1;
-  if (!make_map(&mx, x, p.blocks, p.x_rows, xg, 128) || !make_map(&my, y, p.blocks, p.y_rows, yg, S::BN)) return cudaErrorNotSupported;
+  if (!make_map(&mx, x, p.blocks, p.x_rows, xg, 128) || !make_map(&my, y, p.blocks, p.y_rows, yg, S::Y_ROWS)) return cudaErrorNotSupported;
   p.w_tiles = (q.n + S::W_TILE - 1) / S::W_TILE;
   // no more row tiles than this, whatever the offsets say: every group has at most one tile that is not full
   uint64_t row_tiles = (q.m + S::ROW_TILE - 1) / S::ROW_TILE;
@@ -640,7 +788,9 @@ cudaError_t launch_shape(const Launch& l, const MxProduct& q, ProductArgs p, uin
     const uint32_t pairs = (p.steps + 1) / 2;
     while (p.splits < 8 && p.splits * 2 <= pairs && tiles * p.splits * 2 <= (uint64_t)l.sm_count) p.splits *= 2;
   }
-  const uint32_t grid = p.splits > 1 ? (uint32_t)tiles * p.splits : (uint32_t)(tiles < (uint64_t)l.sm_count ? tiles : l.sm_count);
+  const uint32_t width = S::PAIR ? 2 : p.splits;           // CTAs of a cluster
+  const uint64_t most = p.splits > 1 ? tiles : (uint64_t)l.sm_count / width;
+  const uint32_t grid = (uint32_t)(tiles < most ? tiles : most) * width;
   static bool ready[64] = {};                // per device
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
@@ -655,9 +805,9 @@ cudaError_t launch_shape(const Launch& l, const MxProduct& q, ProductArgs p, uin
   cudaLaunchAttribute attr[2];
   uint32_t na = 0;
   if (l.pdl) { attr[na].id = cudaLaunchAttributeProgrammaticStreamSerialization; attr[na++].val.programmaticStreamSerializationAllowed = 1; }
-  if (p.splits > 1) {
+  if (width > 1) {
     attr[na].id = cudaLaunchAttributeClusterDimension;
-    attr[na].val.clusterDim.x = p.splits; attr[na].val.clusterDim.y = 1; attr[na++].val.clusterDim.z = 1;
+    attr[na].val.clusterDim.x = width; attr[na].val.clusterDim.y = 1; attr[na++].val.clusterDim.z = 1;
   }
   cfg.attrs = attr; cfg.numAttrs = na;
   e = cudaLaunchKernelEx(&cfg, mx_matmul_kernel<S>, mx, my, p);
@@ -665,11 +815,11 @@ cudaError_t launch_shape(const Launch& l, const MxProduct& q, ProductArgs p, uin
   return e;
 }
 
-using ManyRows = Shape<256, true, 4>;
-using Few16 = Shape<16, false, 10>;
-using Few32 = Shape<32, false, 9>;
-using Few64 = Shape<64, false, 8>;
-using Few128 = Shape<128, false, 6>;
+using ManyRows = Shape<256, true, 5>;
+using Few16 = Shape<16, false, 9>;
+using Few32 = Shape<32, false, 8>;
+using Few64 = Shape<64, false, 7>;
+using Few128 = Shape<128, false, 5>;
 
 }  // namespace
 
@@ -686,8 +836,8 @@ cudaError_t launch_mx_matmul(const Launch& l, const MxProduct& q, uint64_t* laun
     return e;
   }
   const uint32_t per_weight = (q.m + q.groups - 1) / q.groups;     // average rows that meet one weight
-  const uint64_t many_tiles = (uint64_t)((q.m + 127) / 128) * ((q.n + 255) / 256);
-  if (per_weight > 64 && 2 * many_tiles > (uint64_t)l.sm_count) return launch_shape<ManyRows>(l, q, p, launches);
+  const uint64_t many_tiles = (uint64_t)((q.m + 255) / 256) * ((q.n + 255) / 256);
+  if (per_weight > 64 && 4 * many_tiles > (uint64_t)l.sm_count) return launch_shape<ManyRows>(l, q, p, launches);
   if (per_weight <= 16) return launch_shape<Few16>(l, q, p, launches);
   if (per_weight <= 32) return launch_shape<Few32>(l, q, p, launches);
   if (per_weight <= 64) return launch_shape<Few64>(l, q, p, launches);
