@@ -81,6 +81,9 @@ __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, u
     asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
                  ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z) : "memory");
 }
+__device__ __forceinline__ void tma_store(uint32_t src, const CUtensorMap* map, int x, int y) {
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%2, %3}], [%1];" ::"l"(map), "r"(src), "r"(x), "r"(y) : "memory");
+}
 // Arrives at `bar` (PAIR: at the same place in both CTAs) when the tensor work issued so far is done.
 template <bool PAIR>
 __device__ __forceinline__ void tc_commit(uint32_t bar) {
@@ -191,7 +194,7 @@ struct ProductArgs {
   const int64_t* offsets;
   void* out;
   uint64_t out_ld;
-  uint32_t dtype, out_vec;                   // out_vec: 16-byte stores of whole rows are aligned
+  uint32_t dtype, out_tma;                   // out_tma: the rows of the result are aligned for TMA
   uint32_t m, n, blocks, steps, groups, w_tiles, splits;
   uint32_t early;                            // everything but `a` was complete before this launch could begin
   uint32_t* fault;
@@ -263,7 +266,8 @@ __device__ __forceinline__ void cluster_sync() {
 // ------------------------------------------------------------------------------------ the kernel
 template <class S>
 __global__ void __launch_bounds__(kProductThreads, 1)
-mx_matmul_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_y, const ProductArgs p) {
+mx_matmul_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_y, const __grid_constant__ CUtensorMap map_out,
+                 const ProductArgs p) {
   constexpr bool PAIR = S::PAIR;
   extern __shared__ uint8_t raw[];
   const uint32_t raw_addr = smem_addr(raw);
@@ -581,26 +585,39 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constan
         // they go first, and a warp that has none of them lets the next tile in at once.
         const bool shares = side != b;
         if (!shares && lane == 0) bar_arrive_at<PAIR>(free0 + 8 * b);
-        // lane = token, columns = weight rows, 32 at a time
+        // lane = token, columns = weight rows, 32 at a time.  32 whole rows leave as a tile by TMA, by way of 2 KB of shared
+        // memory (rows of 64 bytes: 32 results of 16 bits, or in two rounds 16 of 32 bits).  Stores by the warp itself, 4096
+        // or more cycles of the load/store unit a tile, held up the products: their barriers and operands share that unit.
+        const uint32_t row0 = at.token0 + 128 * half + quarter * 32, row = row0 + lane;
+        const bool by_tma = p.out_tma && row0 + 32 <= at.token_end;
+        const uint32_t shift = p.dtype == kF32 ? 2 : 1;
         uint8_t* const mine = staging + (warp - 4) * 2048;
-        const bool wide = p.dtype == kF32;
-        const uint32_t row0 = at.token0 + 128 * half + quarter * 32;
-        const uint32_t rows = row0 < at.token_end ? min(32u, at.token_end - row0) : 0;
+        uint8_t* const put = mine + lane * 64;
+        const uint32_t put_sw = ((lane >> 1) & 3) * 16;                          // the 64-byte swizzle
+        auto column = [&](uint32_t c) { return 32 * (b == 0 ? c ^ 2 : c); };
+        uint32_t next[32];
+        tc_load32(acc + column(0), next);
+        tc_load_wait();
 #pragma unroll 1
         for (uint32_t c = 0; c < COLS / 32; ++c) {
-          const uint32_t cc = b == 0 ? c ^ 2 : c;
           uint32_t v[32];
-          tc_load32(acc + 32 * cc, v);
-          tc_load_wait();
-          if (c == 1 && shares) {
+#pragma unroll
+          for (uint32_t j = 0; j < 32; ++j) v[j] = next[j];
+          if (c + 1 < COLS / 32) {
+            tc_load32(acc + column(c + 1), next);
+            tc_load_wait();
+          }
+          if (c == 0 && shares) {
             tc_fence_before();
             __syncwarp();
             if (lane == 0) bar_arrive_at<PAIR>(free0 + 8 * b);
           }
+          const uint32_t col = column(c), cols = w0 + col < p.n ? min(p.n - w0 - col, 32u) : 0;
+          if (cols == 0) continue;
           if (p.bias) {
 #pragma unroll
             for (uint32_t j = 0; j < 32; j += 4) {
-              const float4 f = *reinterpret_cast<const float4*>(bias_row + 32 * cc + j);
+              const float4 f = *reinterpret_cast<const float4*>(bias_row + col + j);
               v[j] = __float_as_uint(__uint_as_float(v[j]) + f.x); v[j + 1] = __float_as_uint(__uint_as_float(v[j + 1]) + f.y);
               v[j + 2] = __float_as_uint(__uint_as_float(v[j + 2]) + f.z); v[j + 3] = __float_as_uint(__uint_as_float(v[j + 3]) + f.w);
             }
@@ -612,46 +629,42 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constan
 #pragma unroll
             for (uint32_t j = 0; j < 16; ++j) v[j] = pack2(kF16, __uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1]));
           }
-          // Staged as rows of 64 bytes (32 results of 16 bits; 16 of 32 bits, in two rounds) whose four 16-byte pieces
-          // are swizzled by the row so that neither side meets bank conflicts.
-          const uint32_t shift = wide ? 2 : 1, most = 64u >> shift;
+          if (by_tma) {
 #pragma unroll 1
-          for (uint32_t round = 0; round < (wide ? 2u : 1u); ++round) {
-            uint8_t* const row = mine + lane * 64;
-            const uint32_t sw = (lane >> 1) & 3;
+            for (uint32_t round = 0; round < shift; ++round) {
+              if (elect_one()) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");   // the last tile has been read out
+              __syncwarp();
 #pragma unroll
-            for (uint32_t j = 0; j < 4; ++j) {
-              const bool hi = round != 0;
-              *reinterpret_cast<uint4*>(row + ((j ^ sw) * 16)) =
-                  make_uint4(hi ? v[16 + 4 * j] : v[4 * j], hi ? v[17 + 4 * j] : v[4 * j + 1], hi ? v[18 + 4 * j] : v[4 * j + 2], hi ? v[19 + 4 * j] : v[4 * j + 3]);
-            }
-            __syncwarp();
-            const uint32_t col = w0 + 32 * cc + 16 * round;                      // first column of the staged rows
-            const uint32_t cols = col < p.n ? min(p.n - col, most) : 0;
-            uint8_t* const out = (uint8_t*)p.out + (((uint64_t)row0 * p.out_ld + col) << shift);
-            if (p.out_vec && cols == most) {
-              const uint32_t r = lane / 4, piece = lane % 4;
-              uint8_t* dst = out + ((r * p.out_ld) << shift) + 16 * piece;
-              const uint8_t* from = mine + r * 64 + ((piece ^ ((r >> 1) & 3)) * 16);
-#pragma unroll
-              for (uint32_t i = 0; i < 4; ++i) {
-                if (8 * i + r < rows) *reinterpret_cast<uint4*>(dst) = *reinterpret_cast<const uint4*>(from + 512 * i);
-                dst += (8 * p.out_ld) << shift;
+              for (uint32_t j = 0; j < 4; ++j)
+                *reinterpret_cast<uint4*>(put + ((16 * j) ^ put_sw)) = make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+              asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+              __syncwarp();
+              if (elect_one()) {
+                tma_store(smem_addr(mine), &map_out, (int)(w0 + col + 16 * round), (int)row0);
+                asm volatile("cp.async.bulk.commit_group;" ::: "memory");
               }
+              __syncwarp();
+#pragma unroll
+              for (uint32_t j = 0; j < 16; ++j) v[j] = v[16 + j];
+            }
+          } else if (row < at.token_end) {
+            uint8_t* const to = (uint8_t*)p.out + (((uint64_t)row * p.out_ld + w0 + col) << shift);
+            if (p.out_tma && cols == 32) {
+#pragma unroll
+              for (uint32_t j = 0; j < 32; j += 4)
+                if (j < (16u << (shift - 1))) reinterpret_cast<uint4*>(to)[j / 4] = make_uint4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+            } else if (shift == 2) {
+#pragma unroll
+              for (uint32_t j = 0; j < 32; ++j)
+                if (j < cols) reinterpret_cast<uint32_t*>(to)[j] = v[j];
             } else {
-#pragma unroll 1
-              for (uint32_t i = lane; i < rows * 32; i += 32) {                  // 32 places a row, the columns that exist
-                const uint32_t r = i / 32, e = i % 32;
-                if (e >= cols) continue;
-                const uint8_t* from = mine + r * 64 + ((((e << shift) / 16) ^ ((r >> 1) & 3)) * 16) + ((e << shift) % 16);
-                uint8_t* dst = out + ((r * p.out_ld + e) << shift);
-                if (wide) *reinterpret_cast<uint32_t*>(dst) = *reinterpret_cast<const uint32_t*>(from);
-                else *reinterpret_cast<uint16_t*>(dst) = *reinterpret_cast<const uint16_t*>(from);
-              }
+#pragma unroll
+              for (uint32_t j = 0; j < 32; ++j)
+                if (j < cols) reinterpret_cast<uint16_t*>(to)[j] = (uint16_t)(v[j / 2] >> (16 * (j % 2)));
             }
-            __syncwarp();
           }
         }
+        __syncwarp();
       } else {
         if (!bar_wait(acc_full(b), (done / 2) & 1, failed)) break;
         tc_fence_after();
@@ -681,6 +694,9 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constan
         if (lane == 0) bar_arrive_at<false>(free0 + 8 * b);
       }
     }
+  }
+  if constexpr (S::TOKENS_X) {
+    if (warp >= 4 && warp < 12 && elect_one()) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
   }
   __syncwarp();
 
@@ -765,6 +781,15 @@ bool make_map(CUtensorMap* map, const MxView& m, uint32_t blocks, uint64_t rows,
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// The result as the many-row form stores it: boxes of 32 rows by 64 bytes.
+bool make_out_map(CUtensorMap* map, const MxProduct& q) {
+  const uint32_t esz = dtype_size(q.dtype);
+  const cuuint64_t dims[2] = {q.n, q.m}, strides[1] = {q.y_ld * esz};
+  const cuuint32_t box[2] = {64 / esz, 32}, ones[2] = {1, 1};
+  return encoder()(map, esz == 4 ? CU_TENSOR_MAP_DATA_TYPE_UINT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16, 2, q.y, dims, strides, box, ones,
+                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 bool vec16(const MxView& v) { return ((uintptr_t)v.scales | v.scales_ld | v.scales_gs) % 16 == 0; }
 
 template <class S>
@@ -774,9 +799,12 @@ cudaError_t launch_shape(const Launch& l, const MxProduct& q, ProductArgs p, uin
   p.x_sld = x.scales_ld; p.y_sld = y.scales_ld; p.x_sgs = x.scales_gs; p.y_sgs = y.scales_gs;
   p.x_rows = S::TOKENS_X ? q.m : q.n; p.y_rows = S::TOKENS_X ? q.n : q.m;
   p.x_vec = vec16(x); p.y_vec = vec16(y);
-  CUtensorMap mx, my;
+  CUtensorMap mx, my, mo = {};
   const uint64_t xg = S::TOKENS_X ? 1 : q.groups, yg = S::TOKENS_X ? q.groups : 1;
   if (!make_map(&mx, x, p.blocks, p.x_rows, xg, 128) || !make_map(&my, y, p.blocks, p.y_rows, yg, S::Y_ROWS)) return cudaErrorNotSupported;
+  const uint64_t row_bytes = q.y_ld * dtype_size(q.dtype);
+  p.out_tma = S::TOKENS_X && (uintptr_t)q.y % 16 == 0 && row_bytes % 16 == 0 && row_bytes < (1ull << 40);
+  if (p.out_tma && !make_out_map(&mo, q)) return cudaErrorNotSupported;
   p.w_tiles = (q.n + S::W_TILE - 1) / S::W_TILE;
   // no more row tiles than this, whatever the offsets say: every group has at most one tile that is not full
   uint64_t row_tiles = (q.m + S::ROW_TILE - 1) / S::ROW_TILE;
@@ -810,7 +838,7 @@ cudaError_t launch_shape(const Launch& l, const MxProduct& q, ProductArgs p, uin
     attr[na].val.clusterDim.x = width; attr[na].val.clusterDim.y = 1; attr[na++].val.clusterDim.z = 1;
   }
   cfg.attrs = attr; cfg.numAttrs = na;
-  e = cudaLaunchKernelEx(&cfg, mx_matmul_kernel<S>, mx, my, p);
+  e = cudaLaunchKernelEx(&cfg, mx_matmul_kernel<S>, mx, my, mo, p);
   if (e == cudaSuccess) ++*launches;
   return e;
 }
@@ -828,7 +856,6 @@ cudaError_t launch_mx_matmul(const Launch& l, const MxProduct& q, uint64_t* laun
   p.bias = q.bias; p.offsets = q.offsets; p.out = q.y; p.out_ld = q.y_ld; p.dtype = q.dtype;
   p.m = q.m; p.n = q.n; p.blocks = (q.k + 31) / 32; p.steps = (q.k + kStepCols - 1) / kStepCols; p.groups = q.groups;
   p.early = q.early; p.fault = q.fault;
-  p.out_vec = ((uintptr_t)q.y % 16 == 0) && (q.y_ld * dtype_size(q.dtype)) % 16 == 0;
   if (p.steps == 0) {
     const uint64_t want = ((uint64_t)q.m * q.n + 255) / 256;
     cudaError_t e = launch_kernel(l, mx_bias_kernel, (uint32_t)(want < 4096 ? want : 4096), 256, p);
