@@ -566,18 +566,33 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constan
     const uint32_t lanes = (quarter * 32) << 16;
     if (p.early) dependency_wait();
     const uint32_t free0 = PAIR ? at_rank(acc_free(0), 0) : acc_free(0);
+    constexpr uint32_t COLS = S::BN / 2;      // TOKENS_X: columns of this warp
+    float* const bias_row = bias_rows + (warp - 4) * COLS;
+    float ahead[COLS / 32 ? COLS / 32 : 1];   // TOKENS_X: this lane's part of the next tile's bias, fetched a tile ahead
+    auto fetch_bias = [&](const Where& w) {
+#pragma unroll
+      for (uint32_t i = 0; i < COLS / 32; ++i) {
+        const uint32_t n = w.w0 + side * COLS + 32 * i + lane;
+        ahead[i] = n < p.n ? __ldg(p.bias + (uint64_t)w.group * p.n + n) : 0.f;
+      }
+    };
     uint32_t done = 0;
+    Where then;
+    bool more = find_tile<S>(lo, cum, p.groups, p.w_tiles, tile0, &then);
+    if (S::TOKENS_X && p.bias && more) fetch_bias(then);
 #pragma unroll 1
-    for (uint32_t tile = tile0; find_tile<S>(lo, cum, p.groups, p.w_tiles, tile, &at); tile += stride, ++done) {
+    for (uint32_t tile = tile0; more; tile += stride, ++done) {
       const uint32_t b = done & 1;
+      at = then;
       if constexpr (S::TOKENS_X) {
-        constexpr uint32_t COLS = S::BN / 2;  // columns of this warp
         const uint32_t w0 = at.w0 + side * COLS;
-        float* const bias_row = bias_rows + (warp - 4) * COLS;
-        if (p.bias) {                         // the warp's part of the bias, while the products are at work
-          for (uint32_t i = lane; i < COLS; i += 32) bias_row[i] = w0 + i < p.n ? __ldg(p.bias + (uint64_t)at.group * p.n + w0 + i) : 0.f;
+        if (p.bias) {
+#pragma unroll
+          for (uint32_t i = 0; i < COLS / 32; ++i) bias_row[32 * i + lane] = ahead[i];
           __syncwarp();
         }
+        more = find_tile<S>(lo, cum, p.groups, p.w_tiles, tile + stride, &then);
+        if (p.bias && more) fetch_bias(then);
         if (!bar_wait(acc_full(b), (done / 2) & 1, failed)) break;
         tc_fence_after();
         const uint32_t acc = tmem + b * S::ACC_STEP + side * COLS + lanes;
@@ -666,6 +681,7 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constan
         }
         __syncwarp();
       } else {
+        more = find_tile<S>(lo, cum, p.groups, p.w_tiles, tile + stride, &then);
         if (!bar_wait(acc_full(b), (done / 2) & 1, failed)) break;
         tc_fence_after();
         const uint32_t acc = tmem + b * S::ACC_STEP + lanes;
