@@ -97,9 +97,10 @@ template <> struct Chunk8<__nv_bfloat16> : Chunk8Half {
   static __device__ __forceinline__ void store_vec(__nv_bfloat16* p, const float (&v)[8]) {
     uint32_t o[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) { __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]); o[i] = *reinterpret_cast<uint32_t*>(&h); }
+    for (int i = 0; i < 4; ++i) o[i] = pack(v[2 * i], v[2 * i + 1]);
     *reinterpret_cast<uint4*>(p) = make_uint4(o[0], o[1], o[2], o[3]);
   }
+  static __device__ __forceinline__ uint32_t pack(float a, float b) { __nv_bfloat162 h = __floats2bfloat162_rn(a, b); return *reinterpret_cast<uint32_t*>(&h); }
   static __device__ __forceinline__ __nv_bfloat16 narrow(float v) { return __float2bfloat16_rn(v); }
 };
 template <> struct Chunk8<__half> : Chunk8Half {
@@ -118,9 +119,10 @@ template <> struct Chunk8<__half> : Chunk8Half {
   static __device__ __forceinline__ void store_vec(__half* p, const float (&v)[8]) {
     uint32_t o[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) { __half2 h = __floats2half2_rn(v[2 * i], v[2 * i + 1]); o[i] = *reinterpret_cast<uint32_t*>(&h); }
+    for (int i = 0; i < 4; ++i) o[i] = pack(v[2 * i], v[2 * i + 1]);
     *reinterpret_cast<uint4*>(p) = make_uint4(o[0], o[1], o[2], o[3]);
   }
+  static __device__ __forceinline__ uint32_t pack(float a, float b) { __half2 h = __floats2half2_rn(a, b); return *reinterpret_cast<uint32_t*>(&h); }
   static __device__ __forceinline__ __half narrow(float v) { return __float2half_rn(v); }
 };
 template <class T>
@@ -128,6 +130,28 @@ __device__ __forceinline__ void store_some(T* p, const float (&v)[8], uint32_t n
 #pragma unroll
   for (uint32_t i = 0; i < 8; ++i)
     if (i < n) p[i] = Chunk8<T>::narrow(v[i]);
+}
+
+// Sixteen results as whole 32-byte sectors; p is 32-byte aligned.
+__device__ __forceinline__ void store_sector(void* p, const uint32_t (&w)[8]) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+               ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
+}
+template <class T>
+__device__ __forceinline__ void store_sectors(T* p, const float (&a)[8], const float (&b)[8]) {
+  uint32_t w[8];
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(a[i]);
+    store_sector(p, w);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(b[i]);
+    store_sector(p + 8, w);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { w[i] = Chunk8<T>::pack(a[2 * i], a[2 * i + 1]); w[4 + i] = Chunk8<T>::pack(b[2 * i], b[2 * i + 1]); }
+    store_sector(p, w);
+  }
 }
 
 // --- the 4-bit format ------------------------------------------------------------------------------
