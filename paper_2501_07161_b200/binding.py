@@ -295,6 +295,7 @@ class Context:
         self.device = torch.device("cuda", device)
         s = stream if stream is not None else torch.cuda.current_stream(self.device)
         self.stream = s
+        self._raw_stream = s.cuda_stream
         self._graphs = []          # captured passes must be destroyed before their context
         _check(lib().qv2_create(C.byref(self._h), device, C.c_void_p(s.cuda_stream)), "qv2_create")
 
@@ -479,10 +480,11 @@ class Context:
         context's, marks them as used on the context's stream, so that their memory is not handed
         out again before the call has read it (waiting for whoever wrote them is the caller's part,
         as for every call)."""
+        i = self.device.index
         for t in used:
-            if t is not None and t.device != self.device:
+            if t is not None and t.get_device() != i:
                 raise ValueError(f"a tensor is on {t.device}, the context on {self.device}")
-        if torch.cuda.current_stream(self.device).cuda_stream == self.stream.cuda_stream:
+        if torch.cuda.current_stream(i).cuda_stream == self._raw_stream:
             return True
         for t in used:
             if t is not None:
