@@ -67,6 +67,11 @@ class HostResults(C.Structure):
                 ("mse", "sqnr_db", "nonfinite", "order", "keep_fp32", "n_keep")]
 
 
+# The handle of torch's current stream on a device; the short way where this torch has it.
+_current_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+    (lambda device: torch.cuda.current_stream(device).cuda_stream)
+
+
 class MxMatrixC(C.Structure):
     _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p)] + \
                [(n, C.c_uint64) for n in ("groups", "rows", "cols", "codes_ld", "scales_ld", "codes_gs", "scales_gs")]
@@ -245,6 +250,13 @@ class MxMatrix:
             c.data_ptr(), s.data_ptr(), groups, rows, self.cols, 16 * blocks if one else c.stride(-2),
             blocks if one else s.stride(-2), c.stride(0) if c.dim() == 3 else 0, s.stride(0) if c.dim() == 3 else 0))
 
+    @classmethod
+    def _made(cls, codes, scales, cols, values, c) -> "MxMatrix":
+        """One whose parts this module has just allocated: nothing to check."""
+        m = object.__new__(cls)
+        m.__dict__.update(codes=codes, scales=scales, cols=cols, values=values, _c=c)
+        return m
+
     @property
     def groups(self) -> int:
         return self._c.groups
@@ -296,6 +308,7 @@ class Context:
         s = stream if stream is not None else torch.cuda.current_stream(self.device)
         self.stream = s
         self._raw_stream = s.cuda_stream
+        self._like = {}            # an empty tensor of each type on this device, which new ones are made after
         self._graphs = []          # captured passes must be destroyed before their context
         _check(lib().qv2_create(C.byref(self._h), device, C.c_void_p(s.cuda_stream)), "qv2_create")
 
@@ -484,7 +497,7 @@ class Context:
         for t in used:
             if t is not None and t.get_device() != i:
                 raise ValueError(f"a tensor is on {t.device}, the context on {self.device}")
-        if torch.cuda.current_stream(i).cuda_stream == self._raw_stream:
+        if _current_raw_stream(i) == self._raw_stream:
             return True
         for t in used:
             if t is not None:
@@ -493,43 +506,54 @@ class Context:
 
     def _new(self, same: bool, shape, dtype) -> torch.Tensor:
         """Memory that belongs to the context's stream."""
+        like = self._like.get(dtype)
+        if like is None:
+            like = self._like[dtype] = torch.empty(0, dtype=dtype, device=self.device)
         if same:
-            return torch.empty(shape, dtype=dtype, device=self.device)
+            return like.new_empty(shape)
         with torch.cuda.stream(self.stream):
-            return torch.empty(shape, dtype=dtype, device=self.device)
+            return like.new_empty(shape)
 
     @staticmethod
     def _rows(x: torch.Tensor, cols: int) -> torch.Tensor:
         """x [..., cols] as [rows, cols] with consecutive elements."""
         if x.dtype not in _DTYPE_FLAG:
             raise TypeError("activations must be float32, float16 or bfloat16")
-        if x.dim() < 1 or x.shape[-1] != cols:
+        shape = x.shape
+        if not shape or shape[-1] != cols:
             raise ValueError(f"the last dimension must be {cols}")
-        if x.dim() != 2:
-            x = x.reshape(x.numel() // cols if cols else math.prod(x.shape[:-1]), cols)
-        if cols > 1 and x.stride(1) != 1:
+        if len(shape) != 2:
+            x = x.reshape(math.prod(shape[:-1]), cols)
+        row, one = x.stride()
+        if one != 1 and cols > 1:
             raise ValueError("the elements of a row must be consecutive")
-        if x.shape[0] > 1 and x.stride(0) < cols:
+        if row < cols and x.shape[0] > 1:
             raise ValueError("rows may not overlap")
         return x
 
-    def mx_empty(self, rows: int, cols: int, groups: int = 0, values: Optional[torch.Tensor] = None, same: Optional[bool] = None) -> MxMatrix:
-        """An uninitialised matrix (groups > 0: one per expert), scale rows 16 bytes aligned."""
-        same = self._on_stream() if same is None else same
-        blocks, lead = -(-cols // MX_BLOCK), ((groups,) if groups else ())
+    def _mx_empty(self, same, rows, cols, groups=0, values=None) -> MxMatrix:
+        blocks = -(-cols // MX_BLOCK)
+        pitch, lead = (blocks + 15) // 16 * 16, ((groups,) if groups else ())
         codes = self._new(same, (*lead, rows, 16 * blocks), torch.uint8)
-        scales = self._new(same, (*lead, rows, (blocks + 15) // 16 * 16), torch.uint8)
-        return MxMatrix(codes, scales if scales.shape[-1] == blocks else scales[..., :blocks], cols, values)
+        scales = self._new(same, (*lead, rows, pitch), torch.uint8)
+        c = MxMatrixC(codes.data_ptr(), scales.data_ptr(), groups or 1, rows, cols, 16 * blocks, pitch, 16 * blocks * rows, pitch * rows)
+        return MxMatrix._made(codes, scales if pitch == blocks else scales[..., :blocks], cols, values, c)
+
+    def mx_empty(self, rows: int, cols: int, groups: int = 0) -> MxMatrix:
+        """An uninitialised matrix (groups > 0: one per expert), scale rows 16 bytes aligned."""
+        return self._mx_empty(self._on_stream(), rows, cols, groups)
 
     def mx_quantize(self, x: torch.Tensor, want_values: bool = False) -> MxMatrix:
         """x [..., cols] rounded to 4 bits, rows flattened; with want_values also its dequantized copy,
         of x's shape and type."""
-        shape, x = x.shape, self._rows(x, x.shape[-1])
+        shape = x.shape
+        x = self._rows(x, shape[-1] if shape else 0)
         same = self._on_stream(x)
         values = self._new(same, shape, x.dtype) if want_values else None
-        m = self.mx_empty(x.shape[0], x.shape[1], values=values, same=same)
-        _check(lib().qv2_mx_quantize(self._h, x.data_ptr(), _DTYPE_FLAG[x.dtype], x.stride(0), m._c, _ptr(values), x.shape[1]),
-               "qv2_mx_quantize")
+        rows, cols = x.shape
+        m = self._mx_empty(same, rows, cols, 0, values)
+        _check(lib().qv2_mx_quantize(self._h, x.data_ptr(), _DTYPE_FLAG[x.dtype], x.stride(0), m._c,
+                                     None if values is None else values.data_ptr(), cols), "qv2_mx_quantize")
         return m
 
     def mx_dequantize(self, m: MxMatrix, dtype: torch.dtype = torch.float32) -> torch.Tensor:
@@ -540,9 +564,10 @@ class Context:
         return y
 
     def _product_args(self, w: MxMatrix, bias, offsets, grouped: bool):
-        if grouped != (w.codes.dim() == 3):
+        shape = w.codes.shape
+        if grouped != (len(shape) == 3):
             raise ValueError("a dense product takes codes [rows, bytes], a grouped one [groups, rows, bytes]")
-        if bias is not None and (bias.dtype != torch.float32 or not bias.is_contiguous() or bias.shape != w.codes.shape[:-1]):
+        if bias is not None and (bias.dtype != torch.float32 or not bias.is_contiguous() or bias.shape != shape[:-1]):
             raise ValueError("bias must be dense float32 [(groups,) rows of the weight]")
         if grouped and (offsets.dtype != torch.int64 or offsets.shape != (w.groups + 1,) or not offsets.is_contiguous()):
             raise ValueError("offsets must be dense int64 [groups + 1]")
@@ -611,31 +636,41 @@ class Context:
     def kv_write(self, cache: KvCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor):
         """Rounds keys and values [tokens, heads, dim] (any strides of tokens and heads) into their
         slots (int64 [tokens], page * page_size + place; negative: skipped)."""
-        if k.dtype not in _DTYPE_FLAG or v.dtype != k.dtype:
+        type_ = _DTYPE_FLAG.get(k.dtype)
+        if type_ is None or v.dtype != k.dtype:
             raise TypeError("keys and values must both be float32, float16 or bfloat16")
-        shape = (slots.numel(), cache._c.heads, cache.head_dim)
-        if k.shape != shape or v.shape != shape or (shape[2] > 1 and (k.stride(2) != 1 or v.stride(2) != 1)):
-            raise ValueError("keys and values must be [tokens, heads, dim] of the cache, rows consecutive")
+        tokens, c = slots.numel(), cache._c
+        shape = (tokens, c.heads, c.head_dim)
+        if k.shape != shape or v.shape != shape:
+            raise ValueError("keys and values must be [tokens, heads, dim] of the cache")
+        (kt, kh, kd), (vt, vh, vd) = k.stride(), v.stride()
+        if (kd != 1 or vd != 1) and shape[2] > 1:
+            raise ValueError("the elements of a key or value must be consecutive")
         if slots.dtype != torch.int64 or slots.dim() != 1 or not slots.is_contiguous():
             raise ValueError("slots must be dense int64 [tokens]")
-        self._on_stream(k, v, slots, cache.k_codes, cache.k_scales, cache.v_codes, cache.v_scales)
-        _check(lib().qv2_kv_write(self._h, cache._c, k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0), v.stride(1),
-                                  _DTYPE_FLAG[k.dtype], shape[0], slots.data_ptr()), "qv2_kv_write")
+        if not self._on_stream(k, v, slots, cache.k_codes):
+            self._on_stream(cache.k_scales, cache.v_codes, cache.v_scales)
+        _check(lib().qv2_kv_write(self._h, c, k.data_ptr(), kt, kh, v.data_ptr(), vt, vh, type_, tokens, slots.data_ptr()), "qv2_kv_write")
 
     def kv_read(self, cache: KvCache, table: torch.Tensor, starts: torch.Tensor, total: int, dtype: torch.dtype = torch.bfloat16):
         """Whole sequences: starts int64 [seqs + 1] (the host knows its last entry, `total`), table int32
         [seqs, pages of the longest] -> keys, values [total, heads, dim]."""
-        if dtype not in _DTYPE_FLAG:
+        type_ = _DTYPE_FLAG.get(dtype)
+        if type_ is None:
             raise TypeError("results are float32, float16 or bfloat16")
         if table.dtype != torch.int32 or table.dim() != 2 or not table.is_contiguous():
             raise ValueError("table must be dense int32 [seqs, pages]")
-        if starts.dtype != torch.int64 or starts.shape != (table.shape[0] + 1,) or not starts.is_contiguous():
+        seqs, width = table.shape
+        if starts.dtype != torch.int64 or starts.shape != (seqs + 1,) or not starts.is_contiguous():
             raise ValueError("starts must be dense int64 [seqs + 1]")
-        same = self._on_stream(table, starts, cache.k_codes, cache.k_scales, cache.v_codes, cache.v_scales)
-        shape = (total, cache._c.heads, cache.head_dim)
+        same = self._on_stream(table, starts, cache.k_codes)
+        if not same:
+            self._on_stream(cache.k_scales, cache.v_codes, cache.v_scales)
+        c = cache._c
+        shape = (total, c.heads, c.head_dim)
         k, v = self._new(same, shape, dtype), self._new(same, shape, dtype)
-        _check(lib().qv2_kv_read(self._h, cache._c, table.data_ptr(), table.shape[1], table.shape[0], starts.data_ptr(), total,
-                                 k.data_ptr(), v.data_ptr(), _DTYPE_FLAG[dtype]), "qv2_kv_read")
+        _check(lib().qv2_kv_read(self._h, c, table.data_ptr(), width, seqs, starts.data_ptr(), total, k.data_ptr(), v.data_ptr(), type_),
+               "qv2_kv_read")
         return k, v
 
 
