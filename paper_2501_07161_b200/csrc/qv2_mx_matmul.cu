@@ -385,6 +385,7 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constan
       tma_load<PAIR>(base_addr + stage * CODES + (x ? 0 : S::X_BYTES), x ? &map_x : &map_y, full0 + 8 * stage, (int)step * 128, row, weights ? (int)at.group : 0);
     };
     bool first = p.early != 0, ok = true;
+    at = Where{};
 #pragma unroll 1
     for (uint32_t tile = tile0; ok && find_tile<S>(lo, cum, p.groups, p.w_tiles, tile, &at); tile += stride) {
       uint32_t step = step_begin;
@@ -482,18 +483,22 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constan
     const uint32_t full0 = PAIR ? at_rank(full(0), 0) : full(0);
     const bool vec_x = p.x_vec != 0, vec_y = p.y_vec != 0;
     uint8_t* const mine = bytes_ring + 16 * t;     // of slot i: + i * RAW_SLOT; X's row, then 2048 bytes on Y's, and its row 128 below
-    // The sequence of pairs of steps, fetched AHEAD of the one that is unpacked.  Rows past the end of a matrix take
-    // the scales of its last row: they scale results that nobody stores.
+    // The sequence of pairs of steps, fetched AHEAD of the one that is unpacked.  Rows past the end of a matrix keep what
+    // the slot held: they scale results that nobody stores.  (Fetching the last row's scales for them made a product
+    // of 333 rows take 41 us, one of 512 rows 19: hundreds of lanes asked for the same few bytes.)
     uint32_t tile = tile0, two = 0, slot_in = 0;
     const uint8_t *px = nullptr, *py[S::YB];
+    bool in_x = false, in_y[S::YB];
     bool live = find_tile<S>(lo, cum, p.groups, p.w_tiles, tile, &at);
     auto enter = [&] {
       two = step_begin / 2;
-      const uint32_t xr = min((S::TOKENS_X ? at.token0 + 128 * half : at.w0) + t, p.x_rows - 1);
+      const uint32_t xr = (S::TOKENS_X ? at.token0 + 128 * half : at.w0) + t;
+      in_x = xr < p.x_rows;
       px = p.x_scales + (S::TOKENS_X ? 0 : at.group * p.x_sgs) + xr * p.x_sld + 16ull * two;
 #pragma unroll
       for (int i = 0; i < S::YB; ++i) {
-        const uint32_t yr = min((S::TOKENS_X ? at.w0 : at.token0) + t + 128 * i, p.y_rows - 1);
+        const uint32_t yr = (S::TOKENS_X ? at.w0 : at.token0) + t + 128 * i;
+        in_y[i] = t + 128 * i < S::BN && yr < p.y_rows;
         py[i] = p.y_scales + (S::TOKENS_X ? at.group * p.y_sgs : 0) + yr * p.y_sld + 16ull * two;
       }
     };
@@ -501,11 +506,11 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constan
       if (live) {
         uint8_t* dst = mine + slot_in * S::RAW_SLOT;
         const uint32_t n = min(p.blocks - 16 * two, 16u);
-        bring_scales(dst, px, n, vec_x);
+        if (in_x) bring_scales(dst, px, n, vec_x);
         px += 16;
 #pragma unroll
         for (int i = 0; i < S::YB; ++i) {
-          if (t + 128 * i < S::BN) bring_scales(dst + 2048 * (1 + i), py[i], n, vec_y);
+          if (in_y[i]) bring_scales(dst + 2048 * (1 + i), py[i], n, vec_y);
           py[i] += 16;
         }
         if (2 * ++two >= step_end) {
@@ -717,27 +722,34 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constan
   __syncwarp();
 
   if (!S::TOKENS_X && p.splits > 1) {
-    // One tile per cluster: each rank adds up its share of the tokens over all ranks, in their order.
+    // One tile per cluster: each rank adds up its share of the tokens over all ranks, in their order.  A warp takes a
+    // token, a lane four weight rows of it: remote shared memory is bound by requests, 16 bytes a lane are the widest.
     cluster_sync();
     if (find_tile<S>(lo, cum, p.groups, p.w_tiles, tile0, &at)) {
-      const uint32_t col = threadIdx.x % 128, n = at.w0 + col;
+      const uint32_t n = at.w0 + 4 * lane;
       const uint32_t tokens = min((uint32_t)S::BN, at.token_end - at.token0);
-      const float bias = p.bias && n < p.n ? __ldg(p.bias + (uint64_t)at.group * p.n + n) : 0.f;
-      uint32_t from[8];
+      float bias[4];
 #pragma unroll
-      for (uint32_t r = 0; r < 8; ++r) from[r] = at_rank(base_addr + col * 4, r < p.splits ? r : 0);
+      for (uint32_t k = 0; k < 4; ++k) bias[k] = p.bias && n + k < p.n ? __ldg(p.bias + (uint64_t)at.group * p.n + n + k) : 0.f;
 #pragma unroll 1
-      for (uint32_t tok = rank + p.splits * (threadIdx.x / 128); tok < tokens; tok += 4 * p.splits) {
-        float v[8], sum = 0.f;
+      for (uint32_t tok = rank + p.splits * warp; tok < tokens; tok += p.splits * (kProductThreads / 32)) {
+        float4 v[8];
 #pragma unroll
         for (uint32_t r = 0; r < 8; ++r) {
-          v[r] = 0.f;
-          if (r < p.splits) asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v[r]) : "r"(from[r] + tok * 512));
+          v[r] = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (r < p.splits)
+            asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[r].x), "=f"(v[r].y), "=f"(v[r].z), "=f"(v[r].w)
+                         : "r"(at_rank(base_addr + tok * 512 + lane * 16, r)));
         }
+        float4 sum = v[0];
 #pragma unroll
-        for (uint32_t r = 0; r < 8; ++r)
-          if (r < p.splits) sum += v[r];
-        if (n < p.n) store_as(p.out, (uint64_t)(at.token0 + tok) * p.out_ld + n, p.dtype, sum + bias);
+        for (uint32_t r = 1; r < 8; ++r)
+          if (r < p.splits) { sum.x += v[r].x; sum.y += v[r].y; sum.z += v[r].z; sum.w += v[r].w; }
+        const uint64_t to = (uint64_t)(at.token0 + tok) * p.out_ld + n;
+        const float y[4] = {sum.x + bias[0], sum.y + bias[1], sum.z + bias[2], sum.w + bias[3]};
+#pragma unroll
+        for (uint32_t k = 0; k < 4; ++k)
+          if (n + k < p.n) store_as(p.out, to + k, p.dtype, y[k]);
       }
     }
   }
@@ -808,6 +820,43 @@ bool make_out_map(CUtensorMap* map, const MxProduct& q) {
 
 bool vec16(const MxView& v) { return ((uintptr_t)v.scales | v.scales_ld | v.scales_gs) % 16 == 0; }
 
+// No more tiles than this, whatever the offsets say: every group has at most one row tile that is not full.
+template <class S>
+uint64_t most_tiles(const MxProduct& q) {
+  uint64_t row_tiles = (q.m + S::ROW_TILE - 1) / S::ROW_TILE;
+  if (q.groups > 1) row_tiles += q.groups < q.m ? q.groups : q.m;
+  return row_tiles * ((q.n + S::W_TILE - 1) / S::W_TILE);
+}
+
+constexpr int kDevices = 64;                 // answers are kept for this many devices
+
+template <class S>
+cudaError_t allow_shared(int dev) {
+  static bool done[kDevices] = {};
+  if (dev < kDevices && done[dev]) return cudaSuccess;
+  cudaError_t e = cudaFuncSetAttribute(mx_matmul_kernel<S>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM);
+  if (e == cudaSuccess && dev < kDevices) done[dev] = true;
+  return e;
+}
+
+// Clusters of `width` CTAs that the device holds at one time (0: it could not be asked).
+template <class S>
+uint32_t resident_clusters(int dev, uint32_t width) {
+  static uint32_t known[kDevices][4] = {};   // per log2 of the width; stored plus one
+  const uint32_t w = width == 8 ? 3 : width == 4 ? 2 : 1;
+  if (dev < kDevices && known[dev][w]) return known[dev][w] - 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(width); cfg.blockDim = dim3(kProductThreads); cfg.dynamicSmemBytes = S::SMEM;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = width; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr; cfg.numAttrs = 1;
+  int n = 0;
+  if (cudaOccupancyMaxActiveClusters(&n, mx_matmul_kernel<S>, &cfg) != cudaSuccess) { cudaGetLastError(); n = 0; }
+  if (dev < kDevices) known[dev][w] = (uint32_t)n + 1;
+  return (uint32_t)n;
+}
+
 template <class S>
 cudaError_t launch_shape(const Launch& l, const MxProduct& q, ProductArgs p, uint64_t* launches) {
   const MxView &x = S::TOKENS_X ? q.a : q.w, &y = S::TOKENS_X ? q.w : q.a;
@@ -822,28 +871,22 @@ cudaError_t launch_shape(const Launch& l, const MxProduct& q, ProductArgs p, uin
   p.out_tma = S::TOKENS_X && (uintptr_t)q.y % 16 == 0 && row_bytes % 16 == 0 && row_bytes < (1ull << 40);
   if (p.out_tma && !make_out_map(&mo, q)) return cudaErrorNotSupported;
   p.w_tiles = (q.n + S::W_TILE - 1) / S::W_TILE;
-  // no more row tiles than this, whatever the offsets say: every group has at most one tile that is not full
-  uint64_t row_tiles = (q.m + S::ROW_TILE - 1) / S::ROW_TILE;
-  if (q.groups > 1) row_tiles += q.groups < q.m ? q.groups : q.m;
-  const uint64_t tiles = row_tiles * p.w_tiles;
+  const uint64_t tiles = most_tiles<S>(q);
   if (tiles > 0x7fffffffull) return cudaErrorInvalidValue;
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess) e = allow_shared<S>(dev);
+  if (e != cudaSuccess) return e;
   p.splits = 1;
   if (!S::TOKENS_X) {
-    const uint32_t pairs = (p.steps + 1) / 2;
+    const uint32_t pairs = (p.steps + 1) / 2;              // the steps are cut in twos
+    // as many as fill the SMs, as long as all clusters fit the device at once (16 of eight do not, on a B200)
     while (p.splits < 8 && p.splits * 2 <= pairs && tiles * p.splits * 2 <= (uint64_t)l.sm_count) p.splits *= 2;
+    while (p.splits > 1 && tiles > resident_clusters<S>(dev, p.splits)) p.splits /= 2;
   }
   const uint32_t width = S::PAIR ? 2 : p.splits;           // CTAs of a cluster
   const uint64_t most = p.splits > 1 ? tiles : (uint64_t)l.sm_count / width;
   const uint32_t grid = (uint32_t)(tiles < most ? tiles : most) * width;
-  static bool ready[64] = {};                // per device
-  int dev = 0;
-  cudaError_t e = cudaGetDevice(&dev);
-  if (e != cudaSuccess) return e;
-  if (dev < 0 || dev >= 64 || !ready[dev]) {
-    e = cudaFuncSetAttribute(mx_matmul_kernel<S>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM);
-    if (e != cudaSuccess) return e;
-    if (dev >= 0 && dev < 64) ready[dev] = true;
-  }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(grid); cfg.blockDim = dim3(kProductThreads); cfg.dynamicSmemBytes = S::SMEM; cfg.stream = l.stream;
   cudaLaunchAttribute attr[2];
@@ -878,13 +921,20 @@ cudaError_t launch_mx_matmul(const Launch& l, const MxProduct& q, uint64_t* laun
     if (e == cudaSuccess) ++*launches;
     return e;
   }
-  const uint32_t per_weight = (q.m + q.groups - 1) / q.groups;     // average rows that meet one weight
-  const uint64_t many_tiles = (uint64_t)((q.m + 255) / 256) * ((q.n + 255) / 256);
-  if (per_weight > 64 && 4 * many_tiles > (uint64_t)l.sm_count) return launch_shape<ManyRows>(l, q, p, launches);
+  // Rows that meet one weight, on average.  Up to 64 of them are one tile beside the weights (the next wider tile
+  // costs up to a fifth more: 16 rows x 4096 x 4096 6.7 us at 16, 7.1 at 64 and 7.9 at 128).  More rows take the
+  // narrowest tile whose count does not exceed the SMs: at 4096 x 4096, 128 rows 8.9 us at 64 and 13.1 at 16 wide,
+  // 256 rows 10.0 at 64, 13.4 at 32 and 12.5 in the many-row form.  Where 128 wide is too many tiles the many-row form
+  // is faster: 768 rows 13.9 us against 16.3, 2048 rows 20.6 against 27.1.
+  const uint32_t per_weight = (q.m + q.groups - 1) / q.groups;
+  const uint64_t sms = (uint64_t)l.sm_count;
   if (per_weight <= 16) return launch_shape<Few16>(l, q, p, launches);
   if (per_weight <= 32) return launch_shape<Few32>(l, q, p, launches);
   if (per_weight <= 64) return launch_shape<Few64>(l, q, p, launches);
-  return launch_shape<Few128>(l, q, p, launches);
+  if (most_tiles<Few32>(q) <= sms) return launch_shape<Few32>(l, q, p, launches);
+  if (most_tiles<Few64>(q) <= sms) return launch_shape<Few64>(l, q, p, launches);
+  if (most_tiles<Few128>(q) <= sms) return launch_shape<Few128>(l, q, p, launches);
+  return launch_shape<ManyRows>(l, q, p, launches);
 }
 
 }  // namespace qv2
