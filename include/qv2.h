@@ -560,7 +560,10 @@ int qv2_mx_dequantize(qv2_ctx* ctx, const qv2_mx_matrix* m, void* y, uint32_t y_
  * group may be empty), and rows before offsets[0] or from offsets[groups] on are not written.
  * Entries outside 0..a->rows are clamped to it, a decreasing one counts as its predecessor.
  * bias, nullable: binary32 [groups][w->rows].  Inner sizes must agree, a->groups is 1,
- * w->groups <= QV2_MX_MAX_GROUPS, cols <= 2^26, rows of a and of a group of w <= 2^30.
+ * w->groups <= QV2_MX_MAX_GROUPS, cols <= 2^26, rows of a and of a group of w <= 2^30, and
+ * (ceil(a->rows / 16) + groups) * ceil(w->rows / 128) < 2^31.
+ * Errors: _NULL, _ARG, _ALIGN, _SIZE, _CUDA, _NOMEM; QV2_ERR_TIMEOUT when an earlier product gave up
+ * waiting for its own copies (it had no valid result; this call has done nothing).
  * The order of the sums depends on the sizes only: the same inputs give the same bits.
  * y must not overlap a, w, bias or offsets. */
 int qv2_mx_matmul(qv2_ctx* ctx, const qv2_mx_matrix* a, const qv2_mx_matrix* w, const float* bias,

@@ -558,6 +558,8 @@ class Context:
 
     def mx_dequantize(self, m: MxMatrix, dtype: torch.dtype = torch.float32) -> torch.Tensor:
         """-> [(groups,) rows, cols]"""
+        if dtype not in _DTYPE_FLAG:
+            raise TypeError("values are float32, float16 or bfloat16")
         same = self._on_stream(m.codes, m.scales)
         y = self._new(same, (*m.codes.shape[:-1], m.cols), dtype)
         _check(lib().qv2_mx_dequantize(self._h, m._c, y.data_ptr(), _DTYPE_FLAG[dtype], m.cols), "qv2_mx_dequantize")

@@ -32,7 +32,7 @@ kv_write_mx4_kernel(KvView c, KvNew n, uint64_t token0, FastDiv cpr, FastDiv hea
     if (i < n_items) {
       slot[u] = __ldg(n.slots + token0 + t);
       const T* p = (const T*)n.x[which] + (token0 + t) * n.token_ld[which] + h[u] * n.head_ld[which] + 8ull * ch[u];
-      if (vec && ch[u] * 8 + 8 <= c.dim) e[u].load_vec(p);
+      if (ch[u] * 8 + 8 <= c.dim) { if (vec) e[u].load_vec(p); else e[u].load_any(p); }
       else if (ch[u] * 8 < c.dim) e[u].load_some(p, c.dim - ch[u] * 8);
     }
   }
@@ -81,7 +81,7 @@ kv_write_i8_kernel(KvView c, KvNew n, uint64_t token0, FastDiv heads, uint32_t n
     for (uint32_t g = 0; g < 2; ++g, d += 8) {
       e[g].zero();
       if (!p || d >= c.dim) continue;
-      if (vec && d + 8 <= c.dim) e[g].load_vec(p + d);
+      if (d + 8 <= c.dim) { if (vec) e[g].load_vec(p + d); else e[g].load_any(p + d); }
       else e[g].load_some(p + d, c.dim - d);
     }
   };

@@ -38,12 +38,40 @@ struct MxView {                  // qv2_mx_matrix as the kernels see it
   uint64_t codes_ld, scales_ld, codes_gs, scales_gs;
 };
 
+// NW words from p, whatever its alignment (a multiple of 2): aligned 16-byte loads, each of which holds at least one
+// of the wanted bytes, shifted into place.
+template <int NW>
+__device__ __forceinline__ void load_shifted(uint32_t (&out)[NW], const void* p) {
+  const uint32_t off = (uint32_t)((uintptr_t)p & 15u);
+  const uint4* q = reinterpret_cast<const uint4*>((uintptr_t)p & ~(uintptr_t)15u);
+  uint32_t w[NW + 4];
+#pragma unroll
+  for (int i = 0; i <= NW / 4; ++i) {
+    const uint4 v = i < NW / 4 || off ? __ldg(q + i) : make_uint4(0, 0, 0, 0);
+    w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
+  }
+  if (off & 8u)
+#pragma unroll
+    for (int i = 0; i < NW + 2; ++i) w[i] = w[i + 2];
+  if (off & 4u)
+#pragma unroll
+    for (int i = 0; i < NW + 1; ++i) w[i] = w[i + 1];
+#pragma unroll
+  for (int i = 0; i < NW; ++i) out[i] = __funnelshift_r(w[i], w[i + 1], 8 * (off & 3u));
+}
+
 // --- eight consecutive elements, as loaded ---------------------------------------------------------
 template <class T> struct Chunk8;
 template <> struct Chunk8<float> {
   float4 a, b;
   __device__ __forceinline__ void load_vec(const float* p) {
     a = ld_stream4(reinterpret_cast<const float4*>(p)); b = ld_stream4(reinterpret_cast<const float4*>(p) + 1);
+  }
+  __device__ __forceinline__ void load_any(const float* p) {
+    uint32_t w[8];
+    load_shifted<8>(w, p);
+    a = make_float4(__uint_as_float(w[0]), __uint_as_float(w[1]), __uint_as_float(w[2]), __uint_as_float(w[3]));
+    b = make_float4(__uint_as_float(w[4]), __uint_as_float(w[5]), __uint_as_float(w[6]), __uint_as_float(w[7]));
   }
   __device__ __forceinline__ void zero() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
   __device__ __forceinline__ void load_some(const float* p, uint32_t n) {
@@ -75,6 +103,7 @@ struct Chunk8Half {              // the two 16-bit types: four words of two elem
     asm("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
         : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "l"(p));
   }
+  __device__ __forceinline__ void load_any(const void* p) { load_shifted<4>(w, p); }
   __device__ __forceinline__ void zero() { w[0] = w[1] = w[2] = w[3] = 0; }
   __device__ __forceinline__ void load_halves(const unsigned short* p, uint32_t n) {
 #pragma unroll

@@ -42,7 +42,7 @@ int check_matrix(const qv2_mx_matrix* m, uint64_t max_groups, uint64_t max_rows)
   if (m->groups > 1) {
     // groups may not overlap, and their strides stay far from overflowing 64 bits
     if (m->codes_gs < (m->rows - 1) * m->codes_ld + 16 * blocks || m->scales_gs < (m->rows - 1) * m->scales_ld + blocks) return QV2_ERR_ARG;
-    if (m->codes_gs > (1ull << 40) || m->scales_gs > (1ull << 40)) return QV2_ERR_SIZE;
+    if (m->codes_gs >= (1ull << 40) || m->scales_gs >= (1ull << 40)) return QV2_ERR_SIZE;
     if (m->codes_gs % 16) return QV2_ERR_ALIGN;
   }
   return QV2_OK;
@@ -57,6 +57,8 @@ int check_product(const qv2_mx_matrix* w, uint64_t rows, const float* bias, cons
   if (st != QV2_OK) return st;
   if (!offsets && w->groups != 1) return QV2_ERR_ARG;
   if (rows > kMaxRows) return QV2_ERR_SIZE;
+  // tile numbers stay below 2^31, whichever of the product's shapes is taken (16 rows by 128 are its smallest tile)
+  if (((rows + 15) / 16 + w->groups) * ((w->rows + 127) / 128) > 0x7fffffffull) return QV2_ERR_SIZE;
   if ((uintptr_t)bias % 4 || (uintptr_t)offsets % 8) return QV2_ERR_ALIGN;
   return check_dense(y, dtype, y_ld, rows, w->rows);
 }

@@ -194,7 +194,7 @@ struct ProductArgs {
   const int64_t* offsets;
   void* out;
   uint64_t out_ld;
-  uint32_t dtype, out_tma;                   // out_tma: the rows of the result are aligned for TMA
+  uint32_t dtype, out_align;                 // out_align: rows of the result start at multiples of 16 (as TMA needs), 4 or 2 bytes
   uint32_t m, n, blocks, steps, groups, w_tiles, splits;
   uint32_t early;                            // everything but `a` was complete before this launch could begin
   uint32_t* fault;
@@ -299,8 +299,8 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constan
   allow_dependents();
 
   // group tables: lo[g] = first token of group g (clamped, never decreasing), cum[g] = row tiles before it
-  for (uint32_t g = threadIdx.x; g <= p.groups; g += kProductThreads) {
-    int64_t o = p.offsets ? __ldg(p.offsets + g) : (g ? (int64_t)p.m : 0);
+  for (uint32_t g = threadIdx.x; p.groups > 1 && g <= p.groups; g += kProductThreads) {
+    const int64_t o = __ldg(p.offsets + g);
     lo[g] = (uint32_t)(o < 0 ? 0 : o > (int64_t)p.m ? (int64_t)p.m : o);
   }
   if (warp == 3) {
@@ -605,11 +605,14 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constan
         // they go first, and a warp that has none of them lets the next tile in at once.
         const bool shares = side != b;
         if (!shares && lane == 0) bar_arrive_at<PAIR>(free0 + 8 * b);
-        // lane = token, columns = weight rows, 32 at a time.  32 whole rows leave as a tile by TMA, by way of 2 KB of shared
-        // memory (rows of 64 bytes: 32 results of 16 bits, or in two rounds 16 of 32 bits).  Stores by the warp itself, 4096
-        // or more cycles of the load/store unit a tile, held up the products: their barriers and operands share that unit.
-        const uint32_t row0 = at.token0 + 128 * half + quarter * 32, row = row0 + lane;
-        const bool by_tma = p.out_tma && row0 + 32 <= at.token_end;
+        // lane = token, columns = weight rows, 32 at a time.  They pass through 2 KB of shared memory (rows
+        // of 64 bytes: 32 results of 16 bits, or in two rounds 16 of 32 bits) and leave as a tile by TMA.  Where the result's
+        // rows are not aligned for TMA, or a group ends inside the tile, the warp stores the rows side by side itself.  (Every
+        // lane storing its own row took 4096 or more cycles of the load/store unit a tile and held up the products, whose
+        // barriers and operands share that unit; in single elements a product of 6385 x 3738 x 262 took 262 us.)
+        const uint32_t row0 = at.token0 + 128 * half + quarter * 32;
+        const uint32_t rows = row0 < at.token_end ? min(32u, at.token_end - row0) : 0;
+        const bool by_tma = p.out_align == 16 && rows == 32;
         const uint32_t shift = p.dtype == kF32 ? 2 : 1;
         uint8_t* const mine = staging + (warp - 4) * 2048;
         uint8_t* const put = mine + lane * 64;
@@ -633,7 +636,7 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constan
             if (lane == 0) bar_arrive_at<PAIR>(free0 + 8 * b);
           }
           const uint32_t col = column(c), cols = w0 + col < p.n ? min(p.n - w0 - col, 32u) : 0;
-          if (cols == 0) continue;
+          if (cols == 0 || rows == 0) continue;
           if (p.bias) {
 #pragma unroll
             for (uint32_t j = 0; j < 32; j += 4) {
@@ -649,39 +652,49 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constan
 #pragma unroll
             for (uint32_t j = 0; j < 16; ++j) v[j] = pack2(kF16, __uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1]));
           }
-          if (by_tma) {
 #pragma unroll 1
-            for (uint32_t round = 0; round < shift; ++round) {
-              if (elect_one()) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");   // the last tile has been read out
-              __syncwarp();
+          for (uint32_t round = 0; round < shift; ++round) {
+            if (elect_one()) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");     // the last tile has been read out
+            __syncwarp();
 #pragma unroll
-              for (uint32_t j = 0; j < 4; ++j)
-                *reinterpret_cast<uint4*>(put + ((16 * j) ^ put_sw)) = make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+            for (uint32_t j = 0; j < 4; ++j)
+              *reinterpret_cast<uint4*>(put + ((16 * j) ^ put_sw)) = make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+#pragma unroll
+            for (uint32_t j = 0; j < 16; ++j) v[j] = v[16 + j];
+            if (by_tma) {
               asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
               __syncwarp();
               if (elect_one()) {
                 tma_store(smem_addr(mine), &map_out, (int)(w0 + col + 16 * round), (int)row0);
                 asm volatile("cp.async.bulk.commit_group;" ::: "memory");
               }
-              __syncwarp();
-#pragma unroll
-              for (uint32_t j = 0; j < 16; ++j) v[j] = v[16 + j];
-            }
-          } else if (row < at.token_end) {
-            uint8_t* const to = (uint8_t*)p.out + (((uint64_t)row * p.out_ld + w0 + col) << shift);
-            if (p.out_tma && cols == 32) {
-#pragma unroll
-              for (uint32_t j = 0; j < 32; j += 4)
-                if (j < (16u << (shift - 1))) reinterpret_cast<uint4*>(to)[j / 4] = make_uint4(v[j], v[j + 1], v[j + 2], v[j + 3]);
-            } else if (shift == 2) {
-#pragma unroll
-              for (uint32_t j = 0; j < 32; ++j)
-                if (j < cols) reinterpret_cast<uint32_t*>(to)[j] = v[j];
             } else {
+              __syncwarp();
+              const uint32_t left = cols > 16 * round ? cols - 16 * round : 0, bytes = min(left << shift, 64u);
+              uint8_t* const to = (uint8_t*)p.out + (((uint64_t)row0 * p.out_ld + w0 + col + 16 * round) << shift);
+              const uint64_t pitch = p.out_ld << shift;
+              auto staged = [&](uint32_t r, uint32_t b) { return mine + r * 64 + (((b / 16) ^ ((r >> 1) & 3)) * 16) + b % 16; };
+              if (p.out_align == 16 && bytes == 64) {          // a row by four lanes
 #pragma unroll
-              for (uint32_t j = 0; j < 32; ++j)
-                if (j < cols) reinterpret_cast<uint16_t*>(to)[j] = (uint16_t)(v[j / 2] >> (16 * (j % 2)));
+                for (uint32_t i = 0; i < 4; ++i) {
+                  const uint32_t r = 8 * i + lane / 4, at_byte = 16 * (lane % 4);
+                  if (r < rows) *reinterpret_cast<uint4*>(to + r * pitch + at_byte) = *reinterpret_cast<const uint4*>(staged(r, at_byte));
+                }
+              } else if (p.out_align >= 4) {                   // by sixteen
+                const uint32_t at_byte = 4 * (lane % 16);
+#pragma unroll 4
+                for (uint32_t r = lane / 16; r < rows; r += 2) {
+                  if (at_byte + 4 <= bytes) *reinterpret_cast<uint32_t*>(to + r * pitch + at_byte) = *reinterpret_cast<const uint32_t*>(staged(r, at_byte));
+                  else if (at_byte < bytes) *reinterpret_cast<uint16_t*>(to + r * pitch + at_byte) = *reinterpret_cast<const uint16_t*>(staged(r, at_byte));
+                }
+              } else {                                         // by all (16-bit results on odd addresses of two bytes)
+                const uint32_t at_byte = 2 * lane;
+#pragma unroll 4
+                for (uint32_t r = 0; r < rows; ++r)
+                  if (at_byte < bytes) *reinterpret_cast<uint16_t*>(to + r * pitch + at_byte) = *reinterpret_cast<const uint16_t*>(staged(r, at_byte));
+              }
             }
+            __syncwarp();
           }
         }
         __syncwarp();
@@ -868,11 +881,11 @@ cudaError_t launch_shape(const Launch& l, const MxProduct& q, ProductArgs p, uin
   const uint64_t xg = S::TOKENS_X ? 1 : q.groups, yg = S::TOKENS_X ? q.groups : 1;
   if (!make_map(&mx, x, p.blocks, p.x_rows, xg, 128) || !make_map(&my, y, p.blocks, p.y_rows, yg, S::Y_ROWS)) return cudaErrorNotSupported;
   const uint64_t row_bytes = q.y_ld * dtype_size(q.dtype);
-  p.out_tma = S::TOKENS_X && (uintptr_t)q.y % 16 == 0 && row_bytes % 16 == 0 && row_bytes < (1ull << 40);
-  if (p.out_tma && !make_out_map(&mo, q)) return cudaErrorNotSupported;
+  const uint64_t where = (uintptr_t)q.y | row_bytes;
+  p.out_align = where % 16 == 0 && row_bytes < (1ull << 40) ? 16 : where % 4 == 0 ? 4 : 2;
+  if (S::TOKENS_X && p.out_align == 16 && !make_out_map(&mo, q)) return cudaErrorNotSupported;
   p.w_tiles = (q.n + S::W_TILE - 1) / S::W_TILE;
   const uint64_t tiles = most_tiles<S>(q);
-  if (tiles > 0x7fffffffull) return cudaErrorInvalidValue;
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e == cudaSuccess) e = allow_shared<S>(dev);

@@ -27,7 +27,7 @@ mx_quantize_kernel(const T* x, uint64_t x_ld, uint32_t cols, FastDiv cpr, uint32
     e[u].zero();
     if (i < n_items) {
       const T* p = x + row[u] * x_ld + 8ull * c[u];
-      if (VEC && c[u] * 8 + 8 <= cols) e[u].load_vec(p);
+      if (c[u] * 8 + 8 <= cols) { if (VEC) e[u].load_vec(p); else e[u].load_any(p); }
       else if (c[u] * 8 < cols) e[u].load_some(p, cols - c[u] * 8);
     }
   }
@@ -46,9 +46,28 @@ mx_quantize_kernel(const T* x, uint64_t x_ld, uint32_t cols, FastDiv cpr, uint32
       if (VALUES) {
         mx_decode8(codes, mx_scale(byte), v);
         T* q = values + row[u] * values_ld + 8ull * c[u];
-        if (VEC && c[u] * 8 + 8 <= cols) Chunk8<T>::store_vec(q, v);
-        else if (c[u] * 8 < cols) store_some(q, v, cols - c[u] * 8);
+        if (VEC) {
+          if (c[u] * 8 + 8 <= cols) Chunk8<T>::store_vec(q, v);
+          else if (c[u] * 8 < cols) store_some(q, v, cols - c[u] * 8);
+        }
       }
+    }
+    if (VALUES && !VEC) {
+      // Rows on any address: the warp's 256 results change places so that neighbouring lanes store neighbouring elements.
+      __shared__ T swap[kMxThreads * 8];
+      T* const mine = swap + (threadIdx.x & ~31u) * 8;
+      const uint32_t lane = threadIdx.x % 32;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) mine[8 * lane + k] = Chunk8<T>::narrow(v[k]);
+      __syncwarp();
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const uint32_t from = 4 * k + lane / 8;
+        const uint32_t r = __shfl_sync(0xffffffffu, row[u], from), col = 8 * __shfl_sync(0xffffffffu, c[u], from) + lane % 8;
+        const bool in = base - lane + from + u * kMxThreads < n_items;
+        if (in && col < cols) values[r * values_ld + col] = mine[32 * k + lane];
+      }
+      __syncwarp();
     }
   }
 }

@@ -437,3 +437,40 @@ def test_python_refusals(ctx):
                     (lambda: q.KvCache(q.KV_I8, 33, cache.k_codes, cache.k_scales, cache.v_codes, cache.v_scales), ValueError)):
         with pytest.raises(err):
             fn()
+
+
+# ---------------------------------------------------------------------------------------- together
+@pytest.mark.parametrize("m,n,k", [(3000, 1001, 96), (2600, 1302, 300), (2500, 1304, 100)])
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_many_rows_with_unaligned_results(ctx, m, n, k, dtype):
+    """The many-row form where rows of the result start at multiples of 2, 4, 8 and 16 bytes."""
+    a, av = pack(f64(randn(m, k, seed=m)))
+    w, wv = pack(f64(randn(n, k, seed=n)) / 64)
+    check_product(ctx.mx_matmul(a, w, out_dtype=DTYPES[dtype]), av, wv, None, dtype)
+
+
+def test_strided_keys_on_odd_addresses(ctx):
+    buf = randn(9 * 3 * 70 + 1, seed=1, dtype="bf16").cuda()
+    k = buf[1:].as_strided((9, 3, 67), (210, 70, 1))
+    for fmt in (q.KV_MX4, q.KV_I8):
+        cache = ctx.kv_empty(1, 9, 3, 67, fmt)
+        ctx.kv_write(cache, k, k, torch.arange(9, device="cuda"))
+        one = ctx.kv_empty(1, 9, 3, 67, fmt)
+        ctx.kv_write(one, k.contiguous(), k.contiguous(), torch.arange(9, device="cuda"))
+        assert torch.equal(cache.k_codes, one.k_codes) and torch.equal(cache.v_scales, one.v_scales)
+
+
+@pytest.mark.parametrize("fmt", [q.KV_MX4, q.KV_I8])
+def test_example_block(ctx, fmt):
+    """The example's block: every layer's 4-bit weights and outputs stay near FP32 (rounding to 4 bits with a scale per
+    32 leaves 17 to 19 dB per operand of normal values, two operands and a chain of layers some dB less)."""
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "narrow_block.py")
+    spec = importlib.util.spec_from_file_location("narrow_block", path)
+    ex = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(ex)
+    stages, block = ex.run(ctx, fmt)
+    w, x, order = ex.report(ctx, stages, block)
+    assert all(v > 15 for v in w) and all(v > 8 for v in x), (w, x)
+    assert sorted(order) == list(range(len(stages)))
