@@ -8,15 +8,22 @@
 //   warp 2       owns the tensor memory,
 //   warps 4-11   move finished accumulators out (two warps per quarter of the 128 accumulator rows),
 //   warps 12-15  bring the scales: they lie row by row in memory, the tensor core wants them four to a
-//                word and 32 rows to a column, so they pass through registers, 16 bytes per row and two
-//                steps, fetched four steps ahead.
+//                word and 32 rows to a column, so each thread fetches 16 bytes of its row (two steps) with
+//                cp.async, four of those ahead, and deals them out through registers.
 // A ring of shared-memory stages decouples them; accumulators are double-buffered.
 //
 // The 128-row operand X and the BN-row operand Y take either role:
-//   tokens as X, weights as Y (BN = 256): the many-row form, bound by the tensor cores;
+//   tokens as X, weights as Y (BN = 256): the many-row form.  Two CTAs share a 256 x 256 tile
+//   (cta_group::2), since a 128 x 256 tile of one asks L2 for 48 KB a step of 512 tensor cycles, 96 bytes a
+//   cycle and SM, more than it delivers (880 cycles a step; 580 in pairs).  8192 x 8192 x 8192 takes about
+//   200 us (5.4 PFLOP/s, 3.3 times the measured bf16 rate), 16411 x 4096 x 2048 in 16 groups 72 us.  What
+//   bounds it: the tensor cores under the power limit (the same product of constant codes takes 167 us), and
+//   some 700 cycles between tiles, in which the shared columns of the accumulators are read out.
 //   weights as X, tokens as Y (BN = 16..128): few rows per weight, bound by reading the weights once; the
 //   columns may be cut over the CTAs of a cluster, whose partial sums are added through distributed
-//   shared memory in the order of the ranks.
+//   shared memory in the order of the ranks.  A step takes at least 480 cycles whatever BN (four products
+//   and four copies of scales), 8 TB/s over all SMs; 1 x 4096 x 25088 takes 12 us beside 8.4 us for its bytes
+//   at the copy rate: 2.4 us until the first tile is there, 2 us to join the four partial sums.
 #include <cuda.h>
 
 #include "qv2_mx.cuh"
@@ -373,7 +380,7 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constan
   const uint32_t twos = (p.steps + 1) / 2;
   const uint32_t step_begin = 2 * (uint32_t)((uint64_t)twos * rank / p.splits);
   const uint32_t step_end = min(p.steps, 2 * (uint32_t)((uint64_t)twos * (rank + 1) / p.splits));
-  Where at;
+  Where at = {};
 
   if (warp == 0) {
     // ---------------------------------------------------------------------------------- codes
@@ -385,7 +392,6 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constan
       tma_load<PAIR>(base_addr + stage * CODES + (x ? 0 : S::X_BYTES), x ? &map_x : &map_y, full0 + 8 * stage, (int)step * 128, row, weights ? (int)at.group : 0);
     };
     bool first = p.early != 0, ok = true;
-    at = Where{};
 #pragma unroll 1
     for (uint32_t tile = tile0; ok && find_tile<S>(lo, cum, p.groups, p.w_tiles, tile, &at); tile += stride) {
       uint32_t step = step_begin;
