@@ -569,6 +569,11 @@ int qv2_mx_dequantize(qv2_ctx* ctx, const qv2_mx_matrix* m, void* y, uint32_t y_
 int qv2_mx_matmul(qv2_ctx* ctx, const qv2_mx_matrix* a, const qv2_mx_matrix* w, const float* bias,
                   const int64_t* offsets, void* y, uint32_t y_type, uint64_t y_ld);
 
+/* Host-only view of the form that a product takes, for tests (no GPU needed): how many of a's rows a tile holds, 16, 32, 64, 128 or
+ * 256, for `rows` rows against `groups` weights of n rows on a device of sm_count SMs, or a negative status.
+ * tiles, nullable: the most tiles that it may walk. */
+int qv2_debug_mx_form(uint64_t rows, uint64_t n, uint64_t groups, uint32_t sm_count, uint64_t* tiles);
+
 /* qv2_mx_quantize of x[rows][w->cols] into context scratch followed by qv2_mx_matmul: a layer of
  * 4-bit weights applied to activations as they come.  The scratch grows on demand (the first call
  * of a new largest size allocates, later ones do not). */

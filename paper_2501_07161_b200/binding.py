@@ -34,7 +34,7 @@ EXPORTS = ["qv2_create", "qv2_destroy", "qv2_status_string", "qv2_last_cuda_erro
            "qv2_sweep_graph_destroy", "qv2_check_nonfinite", "qv2_calibrate_ex", "qv2_group_hist_count",
            "qv2_sync_count", "qv2_set_schedule", "qv2_stage_count", "qv2_set_fold_mode",
            "qv2_set_phase_timing", "qv2_calibrate_phase_ms", "qv2_set_dependent_launch",
-           "qv2_mx_quantize", "qv2_mx_dequantize", "qv2_mx_matmul", "qv2_mx_linear", "qv2_kv_write", "qv2_kv_read"]
+           "qv2_mx_quantize", "qv2_mx_dequantize", "qv2_mx_matmul", "qv2_mx_linear", "qv2_kv_write", "qv2_kv_read", "qv2_debug_mx_form"]
 MX_BLOCK, MX_MAX_GROUPS = 32, 512
 KV_MX4, KV_I8 = 0, 1
 KL_BINS = 128
@@ -144,6 +144,7 @@ def lib() -> C.CDLL:
     L.qv2_mx_dequantize.argtypes = [vp, mp, vp, u32, u64]; L.qv2_mx_dequantize.restype = i32
     L.qv2_mx_matmul.argtypes = [vp, mp, mp, vp, vp, vp, u32, u64]; L.qv2_mx_matmul.restype = i32
     L.qv2_mx_linear.argtypes = [vp, vp, u32, u64, u64, mp, vp, vp, vp, u32, u64]; L.qv2_mx_linear.restype = i32
+    L.qv2_debug_mx_form.argtypes = [u64, u64, u64, u32, vp]; L.qv2_debug_mx_form.restype = i32
     L.qv2_kv_write.argtypes = [vp, kp, vp, u64, u64, vp, u64, u64, u32, u64, vp]; L.qv2_kv_write.restype = i32
     L.qv2_kv_read.argtypes = [vp, kp, vp, u64, u32, vp, u64, vp, vp, u32]; L.qv2_kv_read.restype = i32
     _lib = L
@@ -724,3 +725,12 @@ def plan_tiles(descs):
     buf = np.zeros((max(cnt, 1), 4), np.uint64)
     lib().qv2_debug_plan_tiles(descs, n, buf.ctypes.data, cnt)
     return [tuple(int(v) for v in row) for row in buf[:cnt]]
+
+
+def mx_form(rows: int, n: int, groups: int, sm_count: int):
+    """Host-only: (rows of a tile of the form that a product takes, the most tiles that it may walk)."""
+    tiles = C.c_uint64()
+    form = int(lib().qv2_debug_mx_form(rows, n, groups, sm_count, C.byref(tiles)))
+    if form < 0:
+        raise Qv2Error(form, "qv2_debug_mx_form")
+    return form, tiles.value

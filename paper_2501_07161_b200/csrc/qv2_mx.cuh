@@ -243,6 +243,7 @@ struct MxProduct {
   uint32_t* fault;       // host-mapped word, set when a kernel gave up waiting
 };
 cudaError_t launch_mx_matmul(const Launch& l, const MxProduct& p, uint64_t* launches);
+uint32_t mx_product_form(uint32_t m, uint32_t n, uint32_t groups, uint32_t sm_count, uint64_t* tiles);
 
 struct KvView {
   uint8_t* codes[2]; uint8_t* scales[2];       // keys, values

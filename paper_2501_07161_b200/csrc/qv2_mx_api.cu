@@ -164,6 +164,12 @@ extern "C" int qv2_mx_matmul(qv2_ctx* c, const qv2_mx_matrix* a, const qv2_mx_ma
   return logged(c, "qv2_mx_matmul", before, run());
 }
 
+extern "C" int qv2_debug_mx_form(uint64_t rows, uint64_t n, uint64_t groups, uint32_t sm_count, uint64_t* tiles) {
+  if (groups == 0 || sm_count == 0) return QV2_ERR_ARG;
+  if (rows > kMaxRows || n > kMaxRows || groups > QV2_MX_MAX_GROUPS) return QV2_ERR_SIZE;
+  return (int)mx_product_form((uint32_t)rows, (uint32_t)n, (uint32_t)groups, sm_count, tiles);
+}
+
 extern "C" int qv2_mx_linear(qv2_ctx* c, const void* x, uint32_t x_type, uint64_t x_ld, uint64_t rows, const qv2_mx_matrix* w,
                              const float* bias, const int64_t* offsets, void* y, uint32_t y_type, uint64_t y_ld) {
   if (!c) return QV2_ERR_NULL;

@@ -841,10 +841,10 @@ bool vec16(const MxView& v) { return ((uintptr_t)v.scales | v.scales_ld | v.scal
 
 // No more tiles than this, whatever the offsets say: every group has at most one row tile that is not full.
 template <class S>
-uint64_t most_tiles(const MxProduct& q) {
-  uint64_t row_tiles = (q.m + S::ROW_TILE - 1) / S::ROW_TILE;
-  if (q.groups > 1) row_tiles += q.groups < q.m ? q.groups : q.m;
-  return row_tiles * ((q.n + S::W_TILE - 1) / S::W_TILE);
+uint64_t most_tiles(uint64_t m, uint64_t n, uint64_t groups) {
+  uint64_t row_tiles = (m + S::ROW_TILE - 1) / S::ROW_TILE;
+  if (groups > 1) row_tiles += groups < m ? groups : m;
+  return row_tiles * ((n + S::W_TILE - 1) / S::W_TILE);
 }
 
 constexpr int kDevices = 64;                 // answers are kept for this many devices
@@ -891,7 +891,7 @@ cudaError_t launch_shape(const Launch& l, const MxProduct& q, ProductArgs p, uin
   p.out_align = where % 16 == 0 && row_bytes < (1ull << 40) ? 16 : where % 4 == 0 ? 4 : 2;
   if (S::TOKENS_X && p.out_align == 16 && !make_out_map(&mo, q)) return cudaErrorNotSupported;
   p.w_tiles = (q.n + S::W_TILE - 1) / S::W_TILE;
-  const uint64_t tiles = most_tiles<S>(q);
+  const uint64_t tiles = most_tiles<S>(q.m, q.n, q.groups);
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e == cudaSuccess) e = allow_shared<S>(dev);
@@ -929,6 +929,26 @@ using Few128 = Shape<128, false, 5>;
 
 }  // namespace
 
+// Rows of a tile of the form that a product takes (256: the many-row form), and the most tiles that it may walk.
+uint32_t mx_product_form(uint32_t m, uint32_t n, uint32_t groups, uint32_t sm_count, uint64_t* tiles) {
+  // Rows that meet one weight, on average.  Up to 64 of them are one tile beside the weights (the next wider tile
+  // costs up to a fifth more: 16 rows x 4096 x 4096 6.7 us at 16, 7.1 at 64 and 7.9 at 128).  More rows take the
+  // narrowest tile whose count does not exceed the SMs: at 4096 x 4096, 128 rows 8.9 us at 64 and 13.1 at 16 wide,
+  // 256 rows 10.0 at 64, 13.4 at 32 and 12.5 in the many-row form.  Where 128 wide is too many tiles the many-row form
+  // is faster: 768 rows 13.9 us against 16.3, 2048 rows 20.6 against 27.1.
+  const uint32_t per_weight = (m + groups - 1) / groups;
+  const uint64_t t16 = most_tiles<Few16>(m, n, groups), t32 = most_tiles<Few32>(m, n, groups), t64 = most_tiles<Few64>(m, n, groups),
+                 t128 = most_tiles<Few128>(m, n, groups);
+  uint32_t form = 256;
+  uint64_t t = most_tiles<ManyRows>(m, n, groups);
+  if (per_weight <= 16) { form = 16; t = t16; }
+  else if (per_weight <= 32 || (per_weight > 64 && t32 <= sm_count)) { form = 32; t = t32; }
+  else if (per_weight <= 64 || t64 <= sm_count) { form = 64; t = t64; }
+  else if (t128 <= sm_count) { form = 128; t = t128; }
+  if (tiles) *tiles = t;
+  return form;
+}
+
 cudaError_t launch_mx_matmul(const Launch& l, const MxProduct& q, uint64_t* launches) {
   ProductArgs p = {};
   p.bias = q.bias; p.offsets = q.offsets; p.out = q.y; p.out_ld = q.y_ld; p.dtype = q.dtype;
@@ -940,20 +960,13 @@ cudaError_t launch_mx_matmul(const Launch& l, const MxProduct& q, uint64_t* laun
     if (e == cudaSuccess) ++*launches;
     return e;
   }
-  // Rows that meet one weight, on average.  Up to 64 of them are one tile beside the weights (the next wider tile
-  // costs up to a fifth more: 16 rows x 4096 x 4096 6.7 us at 16, 7.1 at 64 and 7.9 at 128).  More rows take the
-  // narrowest tile whose count does not exceed the SMs: at 4096 x 4096, 128 rows 8.9 us at 64 and 13.1 at 16 wide,
-  // 256 rows 10.0 at 64, 13.4 at 32 and 12.5 in the many-row form.  Where 128 wide is too many tiles the many-row form
-  // is faster: 768 rows 13.9 us against 16.3, 2048 rows 20.6 against 27.1.
-  const uint32_t per_weight = (q.m + q.groups - 1) / q.groups;
-  const uint64_t sms = (uint64_t)l.sm_count;
-  if (per_weight <= 16) return launch_shape<Few16>(l, q, p, launches);
-  if (per_weight <= 32) return launch_shape<Few32>(l, q, p, launches);
-  if (per_weight <= 64) return launch_shape<Few64>(l, q, p, launches);
-  if (most_tiles<Few32>(q) <= sms) return launch_shape<Few32>(l, q, p, launches);
-  if (most_tiles<Few64>(q) <= sms) return launch_shape<Few64>(l, q, p, launches);
-  if (most_tiles<Few128>(q) <= sms) return launch_shape<Few128>(l, q, p, launches);
-  return launch_shape<ManyRows>(l, q, p, launches);
+  switch (mx_product_form(q.m, q.n, q.groups, (uint32_t)l.sm_count, nullptr)) {
+    case 16: return launch_shape<Few16>(l, q, p, launches);
+    case 32: return launch_shape<Few32>(l, q, p, launches);
+    case 64: return launch_shape<Few64>(l, q, p, launches);
+    case 128: return launch_shape<Few128>(l, q, p, launches);
+    default: return launch_shape<ManyRows>(l, q, p, launches);
+  }
 }
 
 }  // namespace qv2
