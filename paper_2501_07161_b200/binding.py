@@ -515,16 +515,20 @@ class Context:
         with torch.cuda.stream(self.stream):
             return like.new_empty(shape)
 
-    @staticmethod
-    def _rows(x: torch.Tensor, cols: int) -> torch.Tensor:
-        """x [..., cols] as [rows, cols] with consecutive elements."""
+    def _rows(self, x: torch.Tensor, cols: int) -> torch.Tensor:
+        """x [..., cols] as [rows, cols] with consecutive elements.  An x that is not a view of such rows is
+        copied, on the context's stream: nobody else could wait for that copy."""
         if x.dtype not in _DTYPE_FLAG:
             raise TypeError("activations must be float32, float16 or bfloat16")
         shape = x.shape
         if not shape or shape[-1] != cols:
             raise ValueError(f"the last dimension must be {cols}")
         if len(shape) != 2:
-            x = x.reshape(math.prod(shape[:-1]), cols)
+            if self._on_stream(x):
+                x = x.reshape(math.prod(shape[:-1]), cols)
+            else:
+                with torch.cuda.stream(self.stream):
+                    x = x.reshape(math.prod(shape[:-1]), cols)
         row, one = x.stride()
         if one != 1 and cols > 1:
             raise ValueError("the elements of a row must be consecutive")
