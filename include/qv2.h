@@ -576,7 +576,11 @@ int qv2_debug_mx_form(uint64_t rows, uint64_t n, uint64_t groups, uint32_t sm_co
 
 /* qv2_mx_quantize of x[rows][w->cols] into context scratch followed by qv2_mx_matmul: a layer of
  * 4-bit weights applied to activations as they come.  The scratch grows on demand (the first call
- * of a new largest size allocates, later ones do not). */
+ * of a new largest size allocates, later ones do not).
+ * A call may be captured in a CUDA graph of the caller's.  It cannot grow the scratch then: QV2_ERR_UNSUPPORTED unless an
+ * earlier call was as large.  The graph holds the scratch's address; a block that a later call outgrows is kept until
+ * the context is destroyed, which has to be after the last replay.  Replays and calls of the context share the scratch:
+ * they must follow one another, on one stream or by events. */
 int qv2_mx_linear(qv2_ctx* ctx, const void* x, uint32_t x_type, uint64_t x_ld, uint64_t rows,
                   const qv2_mx_matrix* w, const float* bias, const int64_t* offsets, void* y, uint32_t y_type,
                   uint64_t y_ld);

@@ -278,6 +278,7 @@ extern "C" int qv2_destroy(qv2_ctx* c) {
   cudaFree(c->d_partials_xe); cudaFree(c->d_kl_hist); cudaFree(c->d_tensor_absmax); cudaFree(c->d_keys);
   cudaFree(c->d_nf_acc); cudaFree(c->d_hist_acc); cudaFree(c->d_tickets); cudaFree(c->d_codes);
   cudaFree(c->d_rank); cudaFree(c->d_mx_codes); cudaFree(c->d_mx_scales);
+  for (void* p : c->kept) cudaFree(p);
   if (c->h_pinned) cudaFreeHost(c->h_pinned);
   cudaFreeHost(c->h_fault);
   for (int i = 0; i < kCodeRing; ++i) {

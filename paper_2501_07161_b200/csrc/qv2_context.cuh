@@ -63,8 +63,9 @@ struct qv2_ctx {
   uint8_t** d_codes = nullptr;    size_t cap_codes = 0;        // per-tensor code buffers of the current call
   double* d_rank = nullptr;                                    // 2 * kMaxRankLayers doubles
   // qv2_mx_linear: the activations of the current call in packed form
-  uint8_t* d_mx_codes = nullptr;  size_t cap_mx_codes = 0;
-  uint8_t* d_mx_scales = nullptr; size_t cap_mx_scales = 0;
+  uint8_t* d_mx_codes = nullptr;  size_t cap_mx_codes = 0;  bool mx_codes_captured = false;
+  uint8_t* d_mx_scales = nullptr; size_t cap_mx_scales = 0; bool mx_scales_captured = false;
+  std::vector<void*> kept;        // outgrown blocks whose addresses a graph of the caller's may hold; freed with the context
   uint32_t* h_fault = nullptr;    // host-mapped word and its device address: a kernel that gave up waiting sets it
   uint32_t* d_fault = nullptr;
   // pinned host staging for the plan upload
@@ -131,6 +132,22 @@ int grow(qv2_ctx* c, T** p, size_t* cap, size_t need, bool graph_held = true) {
   if (*p) { QV2_CUDA(c, cudaFree(*p)); *p = nullptr; *cap = 0; }
   QV2_CUDA(c, cudaMalloc((void**)p, want * sizeof(T)));
   *cap = want;
+  return QV2_OK;
+}
+
+// The same for a buffer whose address calls may leave in a graph that the caller captures (*captured: one has).  Such a
+// block is kept until the context ends, since nothing tells when the graph is gone; while the stream is capturing the buffer
+// cannot grow at all.
+inline int grow_capturable(qv2_ctx* c, uint8_t** p, size_t* cap, size_t need, bool capturing, bool* captured) {
+  if (need > *cap) {
+    if (capturing) return QV2_ERR_UNSUPPORTED;
+    if (*captured) {
+      try { c->kept.push_back(*p); } catch (const std::bad_alloc&) { return QV2_ERR_NOMEM; }
+      *p = nullptr; *cap = 0; *captured = false;
+    }
+    if (int st = grow(c, p, cap, need, false)) return st;
+  }
+  if (capturing) *captured = true;
   return QV2_OK;
 }
 

@@ -186,8 +186,11 @@ extern "C" int qv2_mx_linear(qv2_ctx* c, const void* x, uint32_t x_type, uint64_
     const uint64_t blocks = (w->cols + QV2_MX_BLOCK - 1) / QV2_MX_BLOCK;
     MxView a;
     a.codes_ld = 16 * blocks; a.scales_ld = (blocks + 15) / 16 * 16; a.codes_gs = a.scales_gs = 0;
-    if ((st = grow(c, &c->d_mx_codes, &c->cap_mx_codes, rows * a.codes_ld, false)) != QV2_OK) return st;
-    if ((st = grow(c, &c->d_mx_scales, &c->cap_mx_scales, rows * a.scales_ld, false)) != QV2_OK) return st;
+    cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+    QV2_CUDA(c, cudaStreamIsCapturing(c->stream, &capture));
+    const bool capturing = capture != cudaStreamCaptureStatusNone;
+    if ((st = grow_capturable(c, &c->d_mx_codes, &c->cap_mx_codes, rows * a.codes_ld, capturing, &c->mx_codes_captured)) != QV2_OK) return st;
+    if ((st = grow_capturable(c, &c->d_mx_scales, &c->cap_mx_scales, rows * a.scales_ld, capturing, &c->mx_scales_captured)) != QV2_OK) return st;
     a.codes = c->d_mx_codes; a.scales = c->d_mx_scales;
     if (w->cols) QV2_CUDA(c, launch_mx_quantize(launch_of(c), x, (uint32_t)xt, x_ld, rows, (uint32_t)w->cols, a, nullptr, 0, &c->launches));
     // The kernel that rounds x waits for all work before it and only then lets the product begin, so

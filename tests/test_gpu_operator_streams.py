@@ -49,3 +49,77 @@ def test_input_that_the_call_has_to_copy(ctx, own, call):
     else:
         assert got.shape == (40, 5, want.shape[-1]) and torch.equal(got, want)
     torch.cuda.synchronize()
+
+
+# ---------------------------------------------------------------------------------------- captured calls
+def captured(c, fn):
+    """fn(), captured on the context's stream."""
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(c.stream):
+        with torch.cuda.graph(g, stream=c.stream):
+            fn()
+    return g
+
+
+def replay(c, g):
+    with torch.cuda.stream(c.stream):
+        g.replay()
+    c.stream.synchronize()
+
+
+def test_replays_after_the_scratch_has_grown(ctx, own):
+    """Decoding steps are captured, prompts follow as ordinary calls and need a larger scratch, steps are replayed."""
+    w, w2 = ctx.mx_quantize(normal(300, 256, seed=2)), ctx.mx_quantize(normal(40, 2048, seed=3))
+    x, y = normal(9, 256, seed=1), torch.empty(9, 300, dtype=torch.bfloat16, device="cuda")
+    x2, y2 = normal(70, 2048, seed=4), torch.empty(70, 40, dtype=torch.bfloat16, device="cuda")
+    torch.cuda.synchronize()
+    own.mx_linear(x, w, out=y)
+    own.stream.synchronize()
+    graphs = [(captured(own, lambda: own.mx_linear(x, w, out=y)), x, y, w)]
+    for i, rows in enumerate((500, 3000, 20000)):          # each outgrows the last one's block
+        big = normal(rows, 2048, seed=rows)
+        torch.cuda.synchronize()
+        got = own.mx_linear(big, w2)
+        own.stream.synchronize()
+        assert torch.equal(got, ctx.mx_linear(big, w2))
+        if i == 0:                                          # a second graph holds the block that the first prompt needed
+            graphs.append((captured(own, lambda: own.mx_linear(x2, w2, out=y2)), x2, y2, w2))
+        junk = [torch.full((1 << k,), 255, dtype=torch.uint8, device="cuda") for k in range(10, 28)]
+        for g, xs, ys, ws in graphs:
+            xs.copy_(normal(*xs.shape, seed=50 + i))
+            ys.fill_(0)
+            torch.cuda.synchronize()
+            replay(own, g)
+            assert torch.equal(ys, ctx.mx_linear(xs, ws))
+        assert all(bool((t == 255).all()) for t in junk)
+        del junk
+    torch.cuda.synchronize()
+    del graphs, g
+
+
+def test_scratch_cannot_grow_under_capture(ctx, own):
+    """A call that would have to allocate says so, and the capture goes on without it."""
+    w = ctx.mx_quantize(normal(300, 256, seed=2))
+    x, big = normal(9, 256, seed=1), normal(4000, 256, seed=2)
+    y, ybig = torch.zeros(9, 300, dtype=torch.bfloat16, device="cuda"), torch.zeros(4000, 300, dtype=torch.bfloat16, device="cuda")
+    torch.cuda.synchronize()
+    own.mx_linear(x, w, out=y)
+    own.stream.synchronize()
+    said = []
+
+    def calls():
+        with pytest.raises(q.binding.Qv2Error) as e:
+            own.mx_linear(big, w, out=ybig)
+        said.append(e.value.status)
+        own.mx_linear(x, w, out=y)
+    g = captured(own, calls)
+    assert said == [-8]
+    y.zero_()
+    torch.cuda.synchronize()
+    replay(own, g)
+    assert torch.equal(y, ctx.mx_linear(x, w)) and not bool(ybig.any())
+    own.mx_linear(big, w, out=ybig)                         # outside of a capture it grows
+    replay(own, g)
+    assert torch.equal(ybig, ctx.mx_linear(big, w))
+    torch.cuda.synchronize()
+    del g
