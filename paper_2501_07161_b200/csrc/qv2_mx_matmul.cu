@@ -610,7 +610,7 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constan
         // The columns shared with the next tile are the last 64 of the first buffer and the first 64 of the second:
         // they go first, and a warp that has none of them lets the next tile in at once.
         const bool shares = side != b;
-        if (!shares && lane == 0) bar_arrive_at<PAIR>(free0 + 8 * b);
+        if (!shares && lane == 0) bar_arrive_at<PAIR>(free0 + 8 * b);        // (also: done with the tile before)
         // lane = token, columns = weight rows, 32 at a time.  They pass through 2 KB of shared memory (rows
         // of 64 bytes: 32 results of 16 bits, or in two rounds 16 of 32 bits) and leave as a tile by TMA.  Where the result's
         // rows are not aligned for TMA, or a group ends inside the tile, the warp stores the rows side by side itself.  (Every
@@ -703,6 +703,8 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constan
             __syncwarp();
           }
         }
+        // What was read from this buffer above is ordered before the warp's next arrival (which lets the products into it).
+        tc_fence_before();
         __syncwarp();
       } else {
         more = find_tile<S>(lo, cum, p.groups, p.w_tiles, tile + stride, &then);
