@@ -64,9 +64,12 @@ __device__ __forceinline__ void load_shifted(uint32_t (&out)[NW], const void* p)
 template <class T> struct Chunk8;
 template <> struct Chunk8<float> {
   float4 a, b;
-  __device__ __forceinline__ void load_vec(const float* p) {
-    a = ld_stream4(reinterpret_cast<const float4*>(p)); b = ld_stream4(reinterpret_cast<const float4*>(p) + 1);
+  static __device__ __forceinline__ float4 load4(const float* p) {     // volatile: stays behind dependency_wait()
+    float4 v;
+    asm volatile("ld.global.nc.L1::no_allocate.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "l"(p));
+    return v;
   }
+  __device__ __forceinline__ void load_vec(const float* p) { a = load4(p); b = load4(p + 4); }
   __device__ __forceinline__ void load_any(const float* p) {
     uint32_t w[8];
     load_shifted<8>(w, p);
@@ -100,8 +103,9 @@ template <> struct Chunk8<float> {
 struct Chunk8Half {              // the two 16-bit types: four words of two elements
   uint32_t w[4];
   __device__ __forceinline__ void load_words(const void* p) {
-    asm("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
-        : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "l"(p));
+    // volatile: stays behind dependency_wait()
+    asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "l"(p));
   }
   __device__ __forceinline__ void load_any(const void* p) { load_shifted<4>(w, p); }
   __device__ __forceinline__ void zero() { w[0] = w[1] = w[2] = w[3] = 0; }
