@@ -562,12 +562,21 @@ int qv2_mx_dequantize(qv2_ctx* ctx, const qv2_mx_matrix* m, void* y, uint32_t y_
  * bias, nullable: binary32 [groups][w->rows].  Inner sizes must agree, a->groups is 1,
  * w->groups <= QV2_MX_MAX_GROUPS, cols <= 2^26, rows of a and of a group of w <= 2^30, and
  * (ceil(a->rows / 16) + groups) * ceil(w->rows / 128) < 2^31.
- * Errors: _NULL, _ARG, _ALIGN, _SIZE, _CUDA, _NOMEM; QV2_ERR_TIMEOUT when an earlier product gave up
- * waiting for its own copies (it had no valid result; this call has done nothing).
+ * Errors: _NULL, _ARG, _ALIGN, _SIZE, _CUDA, _NOMEM.
  * The order of the sums depends on the sizes only: the same inputs give the same bits.
  * y must not overlap a, w, bias or offsets. */
 int qv2_mx_matmul(qv2_ctx* ctx, const qv2_mx_matrix* a, const qv2_mx_matrix* w, const float* bias,
                   const int64_t* offsets, void* y, uint32_t y_type, uint64_t y_ld);
+
+/* A product's kernel does not wait for its own copies for ever: after 2 seconds it gives up, its result is not valid, and the
+ * next call that rounds, multiplies or uses the cache below returns QV2_ERR_TIMEOUT and does nothing.  qv2_check_waits asks
+ * without such a call: it waits for the context's stream and returns QV2_ERR_TIMEOUT if a product, or a replay of a
+ * captured one, has given up since the last call that said so.  Replays on other streams are the caller's to wait
+ * for.  QV2_ERR_UNSUPPORTED while the stream is capturing. */
+int qv2_check_waits(qv2_ctx* ctx);
+
+/* For tests: what a kernel does that gives up waiting, done by the host. */
+int qv2_debug_fail_wait(qv2_ctx* ctx);
 
 /* Host-only view of the form that a product takes, for tests (no GPU needed): how many of a's rows a tile holds, 16, 32, 64, 128 or
  * 256, for `rows` rows against `groups` weights of n rows on a device of sm_count SMs, or a negative status.

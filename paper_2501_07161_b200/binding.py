@@ -34,7 +34,8 @@ EXPORTS = ["qv2_create", "qv2_destroy", "qv2_status_string", "qv2_last_cuda_erro
            "qv2_sweep_graph_destroy", "qv2_check_nonfinite", "qv2_calibrate_ex", "qv2_group_hist_count",
            "qv2_sync_count", "qv2_set_schedule", "qv2_stage_count", "qv2_set_fold_mode",
            "qv2_set_phase_timing", "qv2_calibrate_phase_ms", "qv2_set_dependent_launch",
-           "qv2_mx_quantize", "qv2_mx_dequantize", "qv2_mx_matmul", "qv2_mx_linear", "qv2_kv_write", "qv2_kv_read", "qv2_debug_mx_form"]
+           "qv2_mx_quantize", "qv2_mx_dequantize", "qv2_mx_matmul", "qv2_mx_linear", "qv2_kv_write", "qv2_kv_read", "qv2_debug_mx_form",
+           "qv2_check_waits", "qv2_debug_fail_wait"]
 MX_BLOCK, MX_MAX_GROUPS = 32, 512
 KV_MX4, KV_I8 = 0, 1
 KL_BINS = 128
@@ -144,6 +145,8 @@ def lib() -> C.CDLL:
     L.qv2_mx_dequantize.argtypes = [vp, mp, vp, u32, u64]; L.qv2_mx_dequantize.restype = i32
     L.qv2_mx_matmul.argtypes = [vp, mp, mp, vp, vp, vp, u32, u64]; L.qv2_mx_matmul.restype = i32
     L.qv2_mx_linear.argtypes = [vp, vp, u32, u64, u64, mp, vp, vp, vp, u32, u64]; L.qv2_mx_linear.restype = i32
+    for f in ("qv2_check_waits", "qv2_debug_fail_wait"):
+        getattr(L, f).argtypes = [vp]; getattr(L, f).restype = i32
     L.qv2_debug_mx_form.argtypes = [u64, u64, u64, u32, vp]; L.qv2_debug_mx_form.restype = i32
     L.qv2_kv_write.argtypes = [vp, kp, vp, u64, u64, vp, u64, u64, u32, u64, vp]; L.qv2_kv_write.restype = i32
     L.qv2_kv_read.argtypes = [vp, kp, vp, u64, u32, vp, u64, vp, vp, u32]; L.qv2_kv_read.restype = i32
@@ -627,6 +630,11 @@ class Context:
         _check(lib().qv2_mx_matmul(self._h, a._c, w._c, _ptr(bias), _ptr(offsets), y.data_ptr(), _DTYPE_FLAG[out_dtype], y.stride(0)),
                "qv2_mx_matmul")
         return y
+
+    def check_waits(self):
+        """Waits for the context's stream; raises (QV2_ERR_TIMEOUT) if a product, or a replay of a captured one, gave up
+        waiting for its own copies since the last call that reported it."""
+        _check(lib().qv2_check_waits(self._h), "qv2_check_waits")
 
     # -- quantized key / value cache ---------------------------------------------------------
     def kv_empty(self, pages: int, page_size: int, heads: int, head_dim: int, format: int = KV_I8) -> KvCache:

@@ -63,7 +63,8 @@ int check_product(const qv2_mx_matrix* w, uint64_t rows, const float* bias, cons
   return check_dense(y, dtype, y_ld, rows, w->rows);
 }
 
-// Whether a kernel of an earlier call gave up waiting; asking clears it.
+// Whether a kernel of an earlier call gave up waiting; asking clears it.  Every call asks once its arguments are in order, so
+// that what a failed product left behind is not taken further unnoticed.
 int take_fault(qv2_ctx* c) {
   if (!*(volatile uint32_t*)c->h_fault) return QV2_OK;
   *(volatile uint32_t*)c->h_fault = 0;
@@ -120,6 +121,7 @@ extern "C" int qv2_mx_quantize(qv2_ctx* c, const void* x, uint32_t x_type, uint6
     if (st != QV2_OK) return st;
     if ((st = check_dense(x, dtype, x_ld, out->rows, out->cols)) != QV2_OK) return st;
     if (values && (st = check_dense(values, dtype, values_ld, out->rows, out->cols)) != QV2_OK) return st;
+    if ((st = take_fault(c)) != QV2_OK) return st;
     if (out->rows == 0 || out->cols == 0) return QV2_OK;
     DeviceGuard guard(c->device);
     QV2_CUDA(c, launch_mx_quantize(launch_of(c), x, (uint32_t)dtype, x_ld, out->rows, (uint32_t)out->cols, view_of(out), values, values_ld, &c->launches));
@@ -137,6 +139,7 @@ extern "C" int qv2_mx_dequantize(qv2_ctx* c, const qv2_mx_matrix* m, void* y, ui
     int st = check_matrix(m, 1ull << 20, kMaxRows);
     if (st != QV2_OK) return st;
     if ((st = check_dense(y, dtype, y_ld, m->groups * m->rows, m->cols)) != QV2_OK) return st;
+    if ((st = take_fault(c)) != QV2_OK) return st;
     if (m->rows == 0 || m->cols == 0) return QV2_OK;
     DeviceGuard guard(c->device);
     QV2_CUDA(c, launch_mx_dequantize(launch_of(c), view_of(m), m->groups, m->rows, (uint32_t)m->cols, y, (uint32_t)dtype, y_ld, &c->launches));
@@ -162,6 +165,23 @@ extern "C" int qv2_mx_matmul(qv2_ctx* c, const qv2_mx_matrix* a, const qv2_mx_ma
     return run_product(c, view_of(a), a->rows, w, bias, offsets, y, dtype, y_ld, false);
   };
   return logged(c, "qv2_mx_matmul", before, run());
+}
+
+extern "C" int qv2_check_waits(qv2_ctx* c) {
+  if (!c) return QV2_ERR_NULL;
+  DeviceGuard guard(c->device);
+  cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+  QV2_CUDA(c, cudaStreamIsCapturing(c->stream, &capture));
+  if (capture != cudaStreamCaptureStatusNone) return QV2_ERR_UNSUPPORTED;
+  ++c->syncs;
+  QV2_CUDA(c, cudaStreamSynchronize(c->stream));
+  return take_fault(c);
+}
+
+extern "C" int qv2_debug_fail_wait(qv2_ctx* c) {
+  if (!c) return QV2_ERR_NULL;
+  *(volatile uint32_t*)c->h_fault = 1;
+  return QV2_OK;
 }
 
 extern "C" int qv2_debug_mx_form(uint64_t rows, uint64_t n, uint64_t groups, uint32_t sm_count, uint64_t* tiles) {
@@ -211,9 +231,10 @@ extern "C" int qv2_kv_write(qv2_ctx* c, const qv2_kv_cache* cache, const void* k
     if (st != QV2_OK) return st;
     if (dtype < 0) return QV2_ERR_ARG;
     if (tokens > (1ull << 40)) return QV2_ERR_SIZE;
+    if (tokens && (!k || !v || !slots)) return QV2_ERR_NULL;
+    if (tokens && (((uintptr_t)k | (uintptr_t)v) % dtype_size((uint32_t)dtype) || (uintptr_t)slots % 8)) return QV2_ERR_ALIGN;
+    if ((st = take_fault(c)) != QV2_OK) return st;
     if (tokens == 0) return QV2_OK;
-    if (!k || !v || !slots) return QV2_ERR_NULL;
-    if (((uintptr_t)k | (uintptr_t)v) % dtype_size((uint32_t)dtype) || (uintptr_t)slots % 8) return QV2_ERR_ALIGN;
     if (cache->pages == 0) return QV2_OK;                      // no slot exists: every token is skipped
     DeviceGuard guard(c->device);
     KvNew n;
@@ -236,9 +257,10 @@ extern "C" int qv2_kv_read(qv2_ctx* c, const qv2_kv_cache* cache, const int32_t*
     if (st != QV2_OK) return st;
     if (dtype < 0) return QV2_ERR_ARG;
     if (total > (1ull << 30) || seqs > (1u << 30) || table_ld > (1ull << 40)) return QV2_ERR_SIZE;
+    if (total && ((!k && !v) || !starts || (seqs && table_ld && !table))) return QV2_ERR_NULL;
+    if (total && (((uintptr_t)k | (uintptr_t)v) % dtype_size((uint32_t)dtype) || (uintptr_t)starts % 8 || (uintptr_t)table % 4)) return QV2_ERR_ALIGN;
+    if ((st = take_fault(c)) != QV2_OK) return st;
     if (total == 0) return QV2_OK;
-    if ((!k && !v) || !starts || (seqs && table_ld && !table)) return QV2_ERR_NULL;
-    if (((uintptr_t)k | (uintptr_t)v) % dtype_size((uint32_t)dtype) || (uintptr_t)starts % 8 || (uintptr_t)table % 4) return QV2_ERR_ALIGN;
     DeviceGuard guard(c->device);
     KvRead r;
     r.table = table; r.table_ld = table_ld; r.starts = starts; r.seqs = seqs; r.total = total; r.y[0] = k; r.y[1] = v; r.dtype = (uint32_t)dtype;

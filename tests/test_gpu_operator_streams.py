@@ -123,3 +123,62 @@ def test_scratch_cannot_grow_under_capture(ctx, own):
     assert torch.equal(ybig, ctx.mx_linear(big, w))
     torch.cuda.synchronize()
     del g
+
+
+# ---------------------------------------------------------------------------------------- a kernel that gave up
+def test_a_failed_product_is_reported_once(own):
+    """The word that a kernel sets when it gives up is set from the host: whatever comes next says so and does nothing, the call
+    after that works; asking needs no further call."""
+    import ctypes as C
+    c, L = own, q.lib()
+    with torch.cuda.stream(c.stream):
+        x = normal(4, 64)
+        w = c.mx_quantize(x)
+        y, marked = torch.full((4, 4), 7.0, dtype=torch.bfloat16, device="cuda"), torch.full((4, 4), 7.0, dtype=torch.bfloat16, device="cuda")
+        cache = c.kv_empty(1, 4, 1, 64, q.KV_I8)
+        cache.k_codes.fill_(3)
+        kept = cache.k_codes.clone()
+        kv, slots = x.view(4, 1, 64), torch.arange(4, device="cuda")
+        table, starts = torch.zeros(1, 1, dtype=torch.int32, device="cuda"), torch.tensor([0, 4], device="cuda")
+        calls = [lambda: c.mx_quantize(x), lambda: c.mx_dequantize(w), lambda: c.mx_matmul(w, w, out=y, out_dtype=torch.bfloat16), lambda: c.mx_linear(x, w, out=y),
+                 lambda: c.kv_write(cache, kv, kv, slots), lambda: c.kv_write(cache, kv[:0], kv[:0], slots[:0]), lambda: c.kv_read(cache, table, starts, 4),
+                 lambda: c.kv_read(cache, table, starts, 0), c.check_waits]
+        for call in calls:
+            assert L.qv2_debug_fail_wait(c._h) == 0
+            before = c.launches
+            with pytest.raises(q.binding.Qv2Error) as e:
+                call()
+            assert e.value.status == -9 and c.launches == before
+        c.stream.synchronize()
+        assert torch.equal(y, marked) and torch.equal(cache.k_codes, kept)
+        for call in calls:                                  # told once
+            call()
+        c.stream.synchronize()
+        assert not torch.equal(y, marked) and not torch.equal(cache.k_codes, kept)
+        # arguments that are refused leave the report to the next call
+        assert L.qv2_debug_fail_wait(c._h) == 0
+        assert L.qv2_mx_dequantize(c._h, None, None, q.IN_F32, 0) == -2
+        syncs = c.syncs
+        assert L.qv2_check_waits(c._h) == -9 and L.qv2_check_waits(c._h) == 0 and c.syncs == syncs + 2
+    assert L.qv2_check_waits(None) == -2 and L.qv2_debug_fail_wait(None) == -2
+
+
+def test_asking_under_capture(own):
+    w = own.mx_quantize(normal(300, 256, seed=2))
+    x, y = normal(9, 256, seed=1), torch.zeros(9, 300, dtype=torch.bfloat16, device="cuda")
+    torch.cuda.synchronize()
+    own.mx_linear(x, w, out=y)
+    own.stream.synchronize()
+    want, said = y.clone(), []
+
+    def calls():
+        said.append(q.lib().qv2_check_waits(own._h))
+        own.mx_linear(x, w, out=y)
+    g = captured(own, calls)
+    assert said == [-8]
+    y.zero_()
+    torch.cuda.synchronize()
+    replay(own, g)
+    own.check_waits()
+    assert torch.equal(y, want)
+    del g
