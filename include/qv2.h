@@ -541,6 +541,9 @@ typedef struct {
   uint64_t codes_ld, scales_ld;      /* bytes between rows */
   uint64_t codes_gs, scales_gs;      /* bytes between groups; not read when groups <= 1 */
 } qv2_mx_matrix;
+/* Codes behind the last column of a row's last block: rounding writes zeros there.  A matrix that comes from elsewhere may
+ * hold anything there as long as the other operand of its products has zeros, which activations rounded by this library
+ * do; two such matrices may not meet in qv2_mx_matmul, whose sums run over whole blocks. */
 
 /* Rounds x[rows][cols] (row r at x + r*x_ld elements) to 4 bits: rows and cols are those of `out`,
  * whose groups must be 1.  values, nullable: the dequantized copy, element type x_type, rows

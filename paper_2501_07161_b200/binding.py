@@ -230,7 +230,8 @@ class MxMatrix:
     """A matrix (or, with a leading dimension, one per expert) in the microscaled 4-bit format:
     codes uint8 [(groups,) rows, 16 * ceil(cols / 32)], scales uint8 [(groups,) rows, ceil(cols / 32)].
     Rows may be strided; bytes of a row are consecutive.  Rows of scales that are multiples of 16
-    bytes apart load fastest (mx_empty allocates them so)."""
+    bytes apart load fastest (mx_empty allocates them so).  Codes behind the last column have to be zero
+    in at least one of the two operands of mx_matmul (mx_quantize leaves them so)."""
     codes: torch.Tensor
     scales: torch.Tensor
     cols: int

@@ -284,3 +284,22 @@ def test_cache_read_in_long_runs(ctx, dim, heads, page, dtype, fmt):
             v = codes.flatten(0, 1)[at].float() * scales.flatten(0, 1)[at].unsqueeze(-1)
         v[none] = 0
         assert torch.equal(y, v.to(DTYPES[dtype]))
+
+
+@pytest.mark.parametrize("m", [3, 100, 700])
+@pytest.mark.parametrize("k", [33, 1000, 2101])
+def test_weights_may_hold_anything_behind_their_last_column(ctx, m, k):
+    """The activations' codes are zero there, so a weight from elsewhere need not be; dequantizing does not look there."""
+    w = packed(200, k, 1)
+    g = torch.Generator(device="cuda").manual_seed(2)
+    dirty = torch.randint(0, 256, w.codes.shape, dtype=torch.uint8, device="cuda", generator=g)
+    full, half = k // 2, k % 2
+    dirty[:, :full] = w.codes[:, :full]
+    if half:
+        dirty[:, full] = (w.codes[:, full] & 15) | (dirty[:, full] & 240)
+    other = q.MxMatrix(dirty, w.scales, k)
+    assert not torch.equal(dirty, w.codes)
+    x = activations(m, k, 3, "bf16")
+    assert torch.equal(ctx.mx_linear(x, other), ctx.mx_linear(x, w))
+    assert torch.equal(ctx.mx_matmul(ctx.mx_quantize(x), other), ctx.mx_matmul(ctx.mx_quantize(x), w))
+    assert torch.equal(ctx.mx_dequantize(other), ctx.mx_dequantize(w))
