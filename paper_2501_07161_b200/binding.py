@@ -580,7 +580,7 @@ class Context:
             raise ValueError("a dense product takes codes [rows, bytes], a grouped one [groups, rows, bytes]")
         if bias is not None and (bias.dtype != torch.float32 or not bias.is_contiguous() or bias.shape != shape[:-1]):
             raise ValueError("bias must be dense float32 [(groups,) rows of the weight]")
-        if grouped and (offsets.dtype != torch.int64 or offsets.shape != (w.groups + 1,) or not offsets.is_contiguous()):
+        if grouped and (offsets is None or offsets.dtype != torch.int64 or offsets.shape != (w.groups + 1,) or not offsets.is_contiguous()):
             raise ValueError("offsets must be dense int64 [groups + 1]")
 
     def _out(self, out, same, shape, dtype):

@@ -303,3 +303,8 @@ def test_weights_may_hold_anything_behind_their_last_column(ctx, m, k):
     assert torch.equal(ctx.mx_linear(x, other), ctx.mx_linear(x, w))
     assert torch.equal(ctx.mx_matmul(ctx.mx_quantize(x), other), ctx.mx_matmul(ctx.mx_quantize(x), w))
     assert torch.equal(ctx.mx_dequantize(other), ctx.mx_dequantize(w))
+
+
+def test_grouped_product_without_offsets_is_refused(ctx):
+    with pytest.raises(ValueError):
+        ctx.mx_linear_grouped(activations(4, 64, 1, "bf16"), None, packed(8, 64, 2, groups=2))
