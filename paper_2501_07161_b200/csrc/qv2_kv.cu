@@ -1,8 +1,8 @@
 // The quantized key / value cache: rows of one head rounded on their way into their slots, and
 // whole sequences gathered back through a page table.  Both directions are bound by the bytes of
 // the unquantized side (256 of 256 + 68 bytes per row of 128 bfloat16 elements at 4 bits).  204 K tokens
-// of 8 heads x 128 read back from 4 bits (1.06 GB) take 177 us = 5.9 TB/s, 28 K tokens written in 8 bits
-// (173 MB) 37 us = 4.7 TB/s, and read back 29 us.  A CTA begins with a chain of look-ups (sequence, page,
+// of 8 heads x 128 read back from 4 bits (1.06 GB) take 177 us = 5.9 TB/s, 23 K tokens written in 8 bits
+// (145 MB) 39 us = 3.7 TB/s, and read back 30 us = 4.8 TB/s.  A CTA begins with a chain of look-ups (sequence, page,
 // codes: some 2.5 us), so it takes up to 128 tokens (the same read: 232 us at 16 tokens, 190 at 64).
 #include "qv2_mx.cuh"
 

@@ -15,15 +15,16 @@
 // The 128-row operand X and the BN-row operand Y take either role:
 //   tokens as X, weights as Y (BN = 256): the many-row form.  Two CTAs share a 256 x 256 tile
 //   (cta_group::2), since a 128 x 256 tile of one asks L2 for 48 KB a step of 512 tensor cycles, 96 bytes a
-//   cycle and SM, more than it delivers (880 cycles a step; 580 in pairs).  8192 x 8192 x 8192 takes about
-//   200 us (5.4 PFLOP/s, 3.3 times the measured bf16 rate), 16411 x 4096 x 2048 in 16 groups 72 us.  What
-//   bounds it: the tensor cores under the power limit (the same product of constant codes takes 167 us), and
-//   some 700 cycles between tiles, in which the shared columns of the accumulators are read out.
+//   cycle and SM, more than it delivers (880 cycles a step; 580 in pairs).  8192 x 8192 x 8192 takes 239 us
+//   back to back (4.6 PFLOP/s, 2.8 times the measured bf16 rate; the clock settles at 1380 MHz) and 203 in a
+//   burst after a pause, 16411 x 4096 x 2048 in 16 groups 92 and 78 us.  What bounds it: the tensor cores under
+//   the power limit (constant codes take 167 instead of 203 us in a burst), and some 700 cycles between tiles,
+//   in which the shared columns of the accumulators are read out.
 //   weights as X, tokens as Y (BN = 16..128): few rows per weight, bound by reading the weights once; the
 //   columns may be cut over the CTAs of a cluster, whose partial sums are added through distributed
 //   shared memory in the order of the ranks.  A step takes at least 480 cycles whatever BN (four products
-//   and four copies of scales), 8 TB/s over all SMs; 1 x 4096 x 25088 takes 12 us beside 8.4 us for its bytes
-//   at the copy rate: 2.4 us until the first tile is there, 2 us to join the four partial sums.
+//   and four copies of scales), 8 TB/s over all SMs; 1 x 4096 x 25088 takes 14.3 us beside 8.4 us for its bytes
+//   at the copy rate: 128 of 148 SMs, 2.4 us until the first tile is there, 2 us to join the four partial sums.
 #include <cuda.h>
 
 #include "qv2_mx.cuh"
@@ -937,7 +938,8 @@ uint32_t mx_product_form(uint32_t m, uint32_t n, uint32_t groups, uint32_t sm_co
   // costs up to a fifth more: 16 rows x 4096 x 4096 6.7 us at 16, 7.1 at 64 and 7.9 at 128).  More rows take the
   // narrowest tile whose count does not exceed the SMs: at 4096 x 4096, 128 rows 8.9 us at 64 and 13.1 at 16 wide,
   // 256 rows 10.0 at 64, 13.4 at 32 and 12.5 in the many-row form.  Where 128 wide is too many tiles the many-row form
-  // is faster: 768 rows 13.9 us against 16.3, 2048 rows 20.6 against 27.1.
+  // is faster: 768 rows 13.9 us against 16.3, 2048 rows 20.6 against 27.1.  (All of them bursts with the weights in L2.
+  // Other shapes were not measured against the rule, and of groups it knows only the average.)
   const uint32_t per_weight = (m + groups - 1) / groups;
   const uint64_t t16 = most_tiles<Few16>(m, n, groups), t32 = most_tiles<Few32>(m, n, groups), t64 = most_tiles<Few64>(m, n, groups),
                  t128 = most_tiles<Few128>(m, n, groups);

@@ -2,7 +2,9 @@
 // lanes share a block of 32 elements, eight consecutive elements each, so that a warp reads and
 // writes runs of consecutive bytes, and the block's largest magnitude takes two shuffles.  Bound by
 // memory: 16384 x 8192 bfloat16 elements with their values (608 MB) take 93 us = 6.5 TB/s, the copy rate;
-// 1001 x 25088 binary32 ones (214 MB) 34 us; 8192 x 8191 (rows on any address) 46 us beside 31 us aligned.
+// 1001 x 25088 binary32 ones (214 MB) 34 us (back to back, at the clocks that hold then, 102 and 35).  Rows on any
+// address are loaded twice over (load_shifted): 8192 x 8191 codes 46 us beside 33 us aligned, with values 93 beside
+// 52; dequantized to them, element by element, 187 us beside 26 us for the bytes.
 #include "qv2_mx.cuh"
 
 namespace qv2 {
