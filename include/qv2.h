@@ -632,6 +632,92 @@ int qv2_kv_write(qv2_ctx* ctx, const qv2_kv_cache* cache, const void* k, uint64_
 int qv2_kv_read(qv2_ctx* ctx, const qv2_kv_cache* cache, const int32_t* table, uint64_t table_ld, uint32_t seqs,
                 const int64_t* starts, uint64_t total, void* k, void* v, uint32_t type);
 
+/*
+ * ---- Around the cache: pages, rotated keys and queries, attention ----------------------------------
+ *
+ * A step of a served model: qv2_kv_plan gives the new tokens of every request their positions and slots, qv2_norm_rotate
+ * prepares queries and keys, qv2_kv_write rounds keys and values into the slots, qv2_kv_attend reads the cache.  None of
+ * them needs a length on the host, so a step can be captured once and replayed.
+ */
+
+/* Pages and slots for the new tokens of `seqs` requests.  Sequence s held max(lens[s], 0) tokens in the pages
+ * table[s*table_ld + 0 ..] (`width` entries of a row may be used) and gets max(fresh[s], 0) more.  The pages that it lacks are
+ * taken from the end of free_pages[0 .. *free_count), in the order of the sequences, and written into its row of the table;
+ * where the list has run out the entry becomes -1.  (A request that ends gives its pages back by writing them behind the count.)
+ *   lens_out[seqs]      tokens after the step; may be lens itself
+ *   q_starts[seqs+1]    running sum of the new tokens: new token t belongs to the sequence with q_starts[s] <= t < q_starts[s+1]
+ *   starts[seqs+1]      running sum of lens_out, as qv2_kv_read takes it
+ *   slots, positions    [total]: of each new token its slot in the cache, -1 where it has no page, and its position in its
+ *                       sequence; behind the last new token -1 and 0.  New tokens past `total` are left out.
+ *   count_out           pages left in the list; may be free_count itself
+ *   missing             pages that the list did not have; nullable
+ * All on the device; free_pages has free_size entries, and *free_count is held to 0 .. free_size.  Lengths are held to 2^40,
+ * seqs <= QV2_PLAN_MAX_SEQS, page_size * (width + 1) < 2^31.  No output overlaps an input other than as said.
+ * Errors: _NULL, _ARG, _ALIGN, _SIZE, _CUDA. */
+#define QV2_PLAN_MAX_SEQS 65536u
+typedef struct {
+  const int64_t *lens, *fresh;
+  int32_t* table;
+  uint64_t table_ld, width;
+  const int32_t* free_pages;
+  uint64_t free_size;
+  const int64_t* free_count;
+  int64_t *lens_out, *q_starts, *starts, *slots, *positions, *count_out, *missing;
+  uint64_t total;
+  uint32_t seqs, page_size;
+} qv2_page_plan;
+int qv2_kv_plan(qv2_ctx* ctx, const qv2_page_plan* plan);
+
+/* RMS norm of every head of a token and the rotation by its position, in one pass over up to two tensors of heads (queries and
+ * keys).  For a row x[head_dim], in binary32:
+ *   n_d = x_d * weight_d / sqrt(mean(x^2) + eps)         (weight NULL: n = x)
+ *   the pairs (n_i, n_{i+rot/2}), or with QV2_ROTATE_PAIRS (n_{2i}, n_{2i+1}), i < rot/2, become
+ *   (a cos t - b sin t, b cos t + a sin t),  t = positions[token] * freqs[i] in binary64; elements from rot on stay n_d
+ * rounded once to the element type.  Element (t, h, d) of a tensor lies at x + t*token_ld + h*head_ld + d (strides in
+ * elements, any values); y likewise; y may be x with the same strides and may not overlap it otherwise.
+ * positions: device, one per token.  freqs: device, binary32 [rot/2], NULL if rot is 0.  weight: device, binary32 [head_dim].
+ * rot is even and <= head_dim, head_dim <= QV2_SERVE_MAX_DIM, heads <= 65536, tokens <= 2^30.
+ * Errors: _NULL, _ARG, _ALIGN, _SIZE, _CUDA. */
+#define QV2_SERVE_MAX_DIM 256u
+enum { QV2_ROTATE_HALVES = 0, QV2_ROTATE_PAIRS = 1 };
+typedef struct {
+  const void* x;
+  void* y;
+  uint64_t x_token_ld, x_head_ld, y_token_ld, y_head_ld;
+  const float* weight;
+  uint32_t heads;              /* 0: no such tensor */
+} qv2_head_rows;
+int qv2_norm_rotate(qv2_ctx* ctx, const qv2_head_rows* queries, const qv2_head_rows* keys, uint32_t type, uint32_t head_dim,
+                    uint32_t rot, uint32_t order, float eps, uint64_t tokens, const int64_t* positions, const float* freqs);
+
+/* Attention of new tokens over the cache, which already holds their own keys and values.  Sequence s has lens[s] tokens in
+ * the pages of its row of the table; rows q_starts[s] .. q_starts[s+1]-1 of q are the queries of its last n tokens, query i at
+ * position p = lens[s] - n + i.  It sees the tokens j with max(0, p - window + 1) <= j <= p (window 0: from 0) whose page
+ * number is valid, and of those
+ *   x_j = scale * sum_d q_d k_jd;  with cap > 0, x_j = cap * tanh(x_j / cap);  with slopes, x_j += slopes[head] * (j - p)
+ *   out_d = sum_j softmax(x)_j v_jd,   lse = log sum_j exp(x_j)
+ * Query heads h of a token share the key/value head h / (q_heads / cache->heads).  A query that sees no token has out = 0 and
+ * lse = -inf; one that sees a token whose key or value holds a NaN (a poisoned row or block) has NaN throughout, and so has one that itself
+ * holds a NaN or an infinity.  What a query does not see does not change its result.
+ * q: element (t, h, d) at q + t*q_token_ld + h*q_head_ld + d.  out: dense [total][q_heads][head_dim], element type as q's;
+ * lse: binary32 [total][q_heads], nullable.  Rows outside every sequence are left as they were.  q_starts: non-decreasing,
+ * held to 0 .. total.  max_new: no sequence has more queries than this (rows past it are not written); 0: unknown.
+ * Codes and scales enter exactly; queries of 16 bits are exact, of 32 bits held to 2^-22 of their largest element; weights
+ * p_j times the value's scale are rounded to 11 bits (22 for 32-bit queries); sums are binary32.
+ * The order of the sums depends on the lengths and sizes only: the same inputs give the same bits.
+ * q_heads is a multiple of cache->heads and <= 65536, head_dim <= QV2_SERVE_MAX_DIM, table_ld * page_size < 2^31,
+ * seqs <= 65536, total * q_heads < 2^31.  The scratch grows and is captured as that of qv2_mx_linear.
+ * Errors: _NULL, _ARG, _ALIGN, _SIZE, _CUDA, _NOMEM, _UNSUPPORTED. */
+typedef struct {
+  float scale, cap;
+  uint64_t window;
+  const float* slopes;         /* device, binary32 [q_heads], nullable */
+  uint64_t max_new;
+} qv2_attend_cfg;
+int qv2_kv_attend(qv2_ctx* ctx, const qv2_kv_cache* cache, const void* q, uint64_t q_token_ld, uint64_t q_head_ld, uint32_t q_heads,
+                  uint32_t type, uint64_t total, const int64_t* q_starts, const int64_t* lens, uint32_t seqs, const int32_t* table,
+                  uint64_t table_ld, const qv2_attend_cfg* cfg, void* out, float* lse);
+
 #ifdef __cplusplus
 }
 #endif

@@ -35,9 +35,11 @@ EXPORTS = ["qv2_create", "qv2_destroy", "qv2_status_string", "qv2_last_cuda_erro
            "qv2_sync_count", "qv2_set_schedule", "qv2_stage_count", "qv2_set_fold_mode",
            "qv2_set_phase_timing", "qv2_calibrate_phase_ms", "qv2_set_dependent_launch",
            "qv2_mx_quantize", "qv2_mx_dequantize", "qv2_mx_matmul", "qv2_mx_linear", "qv2_kv_write", "qv2_kv_read", "qv2_debug_mx_form",
-           "qv2_check_waits", "qv2_debug_fail_wait"]
+           "qv2_check_waits", "qv2_debug_fail_wait", "qv2_kv_plan", "qv2_norm_rotate", "qv2_kv_attend"]
 MX_BLOCK, MX_MAX_GROUPS = 32, 512
 KV_MX4, KV_I8 = 0, 1
+ROTATE_HALVES, ROTATE_PAIRS = 0, 1
+SERVE_MAX_DIM, PLAN_MAX_SEQS = 256, 65536
 KL_BINS = 128
 NO_GROUP = 0xFFFFFFFF
 NOALLOC_MAX_ELEMS = 1 << 27
@@ -81,6 +83,22 @@ class MxMatrixC(C.Structure):
 class KvCacheC(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("k_codes", "k_scales", "v_codes", "v_scales")] + \
                [("pages", C.c_uint64)] + [(n, C.c_uint32) for n in ("page_size", "heads", "head_dim", "format")]
+
+
+class PagePlanC(C.Structure):
+    _fields_ = [("lens", C.c_void_p), ("fresh", C.c_void_p), ("table", C.c_void_p), ("table_ld", C.c_uint64), ("width", C.c_uint64),
+                ("free_pages", C.c_void_p), ("free_size", C.c_uint64), ("free_count", C.c_void_p)] + \
+               [(n, C.c_void_p) for n in ("lens_out", "q_starts", "starts", "slots", "positions", "count_out", "missing")] + \
+               [("total", C.c_uint64), ("seqs", C.c_uint32), ("page_size", C.c_uint32)]
+
+
+class HeadRowsC(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("y", C.c_void_p)] + [(n, C.c_uint64) for n in ("x_token_ld", "x_head_ld", "y_token_ld", "y_head_ld")] + \
+               [("weight", C.c_void_p), ("heads", C.c_uint32)]
+
+
+class AttendCfgC(C.Structure):
+    _fields_ = [("scale", C.c_float), ("cap", C.c_float), ("window", C.c_uint64), ("slopes", C.c_void_p), ("max_new", C.c_uint64)]
 
 
 _lib = None
@@ -150,6 +168,11 @@ def lib() -> C.CDLL:
     L.qv2_debug_mx_form.argtypes = [u64, u64, u64, u32, vp]; L.qv2_debug_mx_form.restype = i32
     L.qv2_kv_write.argtypes = [vp, kp, vp, u64, u64, vp, u64, u64, u32, u64, vp]; L.qv2_kv_write.restype = i32
     L.qv2_kv_read.argtypes = [vp, kp, vp, u64, u32, vp, u64, vp, vp, u32]; L.qv2_kv_read.restype = i32
+    L.qv2_kv_plan.argtypes = [vp, C.POINTER(PagePlanC)]; L.qv2_kv_plan.restype = i32
+    hp = C.POINTER(HeadRowsC)
+    L.qv2_norm_rotate.argtypes = [vp, hp, hp, u32, u32, u32, u32, C.c_float, u64, vp, vp]; L.qv2_norm_rotate.restype = i32
+    L.qv2_kv_attend.argtypes = [vp, kp, vp, u64, u64, u32, u32, u64, vp, vp, u32, vp, u64, C.POINTER(AttendCfgC), vp, vp]
+    L.qv2_kv_attend.restype = i32
     _lib = L
     return L
 
@@ -302,6 +325,19 @@ class KvCache:
         object.__setattr__(self, "_c", KvCacheC(
             self.k_codes.data_ptr(), self.k_scales.data_ptr(), self.v_codes.data_ptr(), self.v_scales.data_ptr(),
             shape[0], shape[1], shape[2], self.head_dim, self.format))
+
+
+@dataclass
+class PagePlan:
+    """What kv_plan says about a step: int64 on the device.  kv_write takes slots, norm_rotate positions, kv_attend q_starts and
+    lens, kv_read starts."""
+    lens: torch.Tensor            # [seqs] tokens after the step
+    q_starts: torch.Tensor        # [seqs + 1] running sum of the new tokens
+    starts: torch.Tensor          # [seqs + 1] running sum of lens
+    slots: torch.Tensor           # [total] slot of each new token, -1: none
+    positions: torch.Tensor       # [total] its position in its sequence
+    free_count: torch.Tensor      # [1] pages left in the list
+    missing: torch.Tensor         # [1] pages that the list did not have
 
 
 class Context:
@@ -688,6 +724,115 @@ class Context:
         _check(lib().qv2_kv_read(self._h, c, table.data_ptr(), width, seqs, starts.data_ptr(), total, k.data_ptr(), v.data_ptr(), type_),
                "qv2_kv_read")
         return k, v
+
+    # -- around the cache: pages, rotated keys and queries, attention --------------------------
+    def kv_plan(self, lens: torch.Tensor, fresh: torch.Tensor, page_size: int, table: torch.Tensor, free_pages: torch.Tensor,
+                free_count: torch.Tensor, total: int, out: Optional[PagePlan] = None) -> PagePlan:
+        """Positions and slots of the next tokens of every request, and the pages that they lack: lens, fresh int64 [seqs] tokens
+        held and new, table int32 [seqs, width] (gets the new pages), free_pages int32 [n] of which the first free_count
+        (int64 [1]) are free and the last of those are taken.  total: room for that many new tokens; what they do not
+        fill gets slot -1 and position 0.  Pass `out` to reuse its tensors; its lens and free_count may be the
+        arguments themselves, which a captured step wants.  Pages of a request that has ended go back by writing
+        them behind the count."""
+        if lens.dtype != torch.int64 or lens.dim() != 1 or not lens.is_contiguous() or fresh.dtype != torch.int64 or fresh.shape != lens.shape or \
+                not fresh.is_contiguous():
+            raise ValueError("lens and fresh must be dense int64 [seqs]")
+        if table.dtype != torch.int32 or table.dim() != 2 or table.shape[0] != lens.shape[0] or (table.stride(1) != 1 and table.shape[1] > 1):
+            raise ValueError("table must be int32 [seqs, pages], its rows consecutive")
+        if free_pages.dtype != torch.int32 or free_pages.dim() != 1 or not free_pages.is_contiguous():
+            raise ValueError("free_pages must be dense int32")
+        if free_count.dtype != torch.int64 or free_count.numel() != 1:
+            raise ValueError("free_count must be one int64")
+        seqs, (_, width) = lens.shape[0], table.shape
+        same = self._on_stream(lens, fresh, table, free_pages, free_count)
+        sizes = {"lens": seqs, "q_starts": seqs + 1, "starts": seqs + 1, "slots": total, "positions": total, "free_count": 1, "missing": 1}
+        if out is None:
+            out = PagePlan(*(self._new(same, (n,), torch.int64) for n in sizes.values()))
+        else:
+            for name, n in sizes.items():
+                t = getattr(out, name)
+                if t.dtype != torch.int64 or t.shape != (n,) or not t.is_contiguous():
+                    raise ValueError(f"out.{name} must be dense int64 [{n}]")
+            self._on_stream(*(getattr(out, name) for name in sizes))
+        p = PagePlanC(lens.data_ptr(), fresh.data_ptr(), table.data_ptr(), max(table.stride(0), width), width, free_pages.data_ptr(), free_pages.numel(),
+                      free_count.data_ptr(), out.lens.data_ptr(), out.q_starts.data_ptr(), out.starts.data_ptr(), out.slots.data_ptr(),
+                      out.positions.data_ptr(), out.free_count.data_ptr(), out.missing.data_ptr(), total, seqs, page_size)
+        _check(lib().qv2_kv_plan(self._h, p), "qv2_kv_plan")
+        return out
+
+    def _head_rows(self, x, weight, out, same, dim):
+        if x is None:
+            return None, None
+        if weight is not None and (weight.dtype != torch.float32 or weight.shape != (dim,) or not weight.is_contiguous()):
+            raise ValueError("weights must be dense float32 [dim]")
+        if out is None:
+            out = self._new(same, x.shape, x.dtype)
+        elif out.shape != x.shape or out.dtype != x.dtype:
+            raise ValueError("an output must have its input's shape and type")
+        if dim > 1 and (x.stride(2) != 1 or out.stride(2) != 1):
+            raise ValueError("the elements of a head must be consecutive")
+        return out, HeadRowsC(x.data_ptr(), out.data_ptr(), x.stride(0), x.stride(1), out.stride(0), out.stride(1), _ptr(weight), x.shape[1])
+
+    def norm_rotate(self, q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Tensor, freqs: Optional[torch.Tensor],
+                    q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6, pairs: bool = False,
+                    out: Optional[Sequence[Optional[torch.Tensor]]] = None):
+        """Queries and keys [tokens, heads, dim] (any strides of tokens and heads; k may be None): RMS norm of every head where its
+        weight (float32 [dim]) is given, then the first 2 * len(freqs) elements of each head turned by positions (int64 [tokens])
+        times freqs (float32), in pairs (i, i + len(freqs)) or, with `pairs`, (2i, 2i + 1).  -> (q, k), new
+        tensors unless `out` = (q, k) gives them; they may be the inputs themselves."""
+        if q.dim() != 3 or (k is not None and (k.dim() != 3 or k.shape[0] != q.shape[0] or k.shape[2] != q.shape[2] or k.dtype != q.dtype)):
+            raise ValueError("queries and keys must be [tokens, heads, dim] of the same tokens, size and type")
+        type_ = _DTYPE_FLAG.get(q.dtype)
+        if type_ is None:
+            raise TypeError("queries and keys must be float32, float16 or bfloat16")
+        tokens, _, dim = q.shape
+        if positions.dtype != torch.int64 or positions.shape != (tokens,) or not positions.is_contiguous():
+            raise ValueError("positions must be dense int64 [tokens]")
+        if freqs is not None and (freqs.dtype != torch.float32 or freqs.dim() != 1 or not freqs.is_contiguous()):
+            raise ValueError("freqs must be dense float32")
+        yq, yk = out if out is not None else (None, None)
+        same = self._on_stream(q, k, positions, freqs, q_weight, k_weight, yq, yk)
+        yq, qc = self._head_rows(q, q_weight, yq, same, dim)
+        yk, kc = self._head_rows(k, k_weight, yk, same, dim)
+        _check(lib().qv2_norm_rotate(self._h, qc, kc, type_, dim, 0 if freqs is None else 2 * freqs.numel(), ROTATE_PAIRS if pairs else ROTATE_HALVES, eps,
+                                     tokens, positions.data_ptr(), _ptr(freqs)), "qv2_norm_rotate")
+        return yq, yk
+
+    def kv_attend(self, cache: KvCache, q: torch.Tensor, q_starts: torch.Tensor, lens: torch.Tensor, table: torch.Tensor,
+                  scale: Optional[float] = None, window: int = 0, cap: float = 0.0, slopes: Optional[torch.Tensor] = None,
+                  max_new: Optional[int] = None, want_lse: bool = False, out: Optional[torch.Tensor] = None):
+        """Attention of the new tokens q [tokens, q_heads, dim] (any strides of tokens and heads) over the cache, which holds their
+        keys and values already: rows q_starts[s] .. q_starts[s+1]-1 (int64 [seqs + 1]) are the last of the lens[s] (int64 [seqs])
+        tokens of sequence s, whose pages are row s of table (int32 [seqs, pages]).  Each sees itself and what went before, at
+        most `window` tokens if that is given; scores times `scale` (1 / sqrt(dim)) may be capped (cap * tanh(x / cap)) and biased by slopes
+        (float32 [q_heads]) times the distance.  max_new: no sequence has more new tokens (the host often knows; rows past it are not written).
+        -> [tokens, q_heads, dim] of q's type, with want_lse also float32 [tokens, q_heads], the logarithm of the
+        sum of exponentials.  Rows of no sequence are left as they were in `out` (undefined in a new result)."""
+        type_, c = _DTYPE_FLAG.get(q.dtype), cache._c
+        if type_ is None:
+            raise TypeError("queries must be float32, float16 or bfloat16")
+        if q.dim() != 3 or q.shape[2] != c.head_dim or (c.head_dim > 1 and q.stride(2) != 1):
+            raise ValueError("queries must be [tokens, q_heads, dim] of the cache, the elements of a head consecutive")
+        if table.dtype != torch.int32 or table.dim() != 2 or not table.is_contiguous():
+            raise ValueError("table must be dense int32 [seqs, pages]")
+        seqs, width = table.shape
+        if q_starts.dtype != torch.int64 or q_starts.shape != (seqs + 1,) or not q_starts.is_contiguous() or \
+                lens.dtype != torch.int64 or lens.shape != (seqs,) or not lens.is_contiguous():
+            raise ValueError("q_starts must be dense int64 [seqs + 1], lens [seqs]")
+        tokens, q_heads, dim = q.shape
+        if slopes is not None and (slopes.dtype != torch.float32 or slopes.shape != (q_heads,) or not slopes.is_contiguous()):
+            raise ValueError("slopes must be dense float32 [q_heads]")
+        if max_new is not None and max_new < 1 or window < 0:
+            raise ValueError("max_new must be positive, window not negative")
+        same = self._on_stream(q, q_starts, lens, table, slopes, cache.k_codes, out)
+        if not same:
+            self._on_stream(cache.k_scales, cache.v_codes, cache.v_scales)
+        y = self._out(out, same, q.shape, q.dtype)
+        lse = self._new(same, (tokens, q_heads), torch.float32) if want_lse else None
+        cfg = AttendCfgC(dim ** -0.5 if scale is None else scale, cap, window, _ptr(slopes), max_new or 0)
+        _check(lib().qv2_kv_attend(self._h, c, q.data_ptr(), q.stride(0), q.stride(1), q_heads, type_, tokens, q_starts.data_ptr(), lens.data_ptr(), seqs,
+                                   table.data_ptr(), width, cfg, y.data_ptr(), _ptr(lse)), "qv2_kv_attend")
+        return (y, lse) if want_lse else y
 
 
 def quant_metrics_noalloc(desc: TensorDesc, step: torch.Tensor, inv: torch.Tensor, offset: torch.Tensor,

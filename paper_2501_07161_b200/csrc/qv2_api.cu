@@ -247,8 +247,12 @@ extern "C" int qv2_create(qv2_ctx** out, int device, void* stream) {
   if (e == cudaSuccess) e = cudaMalloc((void**)&c->d_rank, kRankScratchDoubles * sizeof(double));
   if (e == cudaSuccess) e = cudaHostAlloc((void**)&c->h_fault, sizeof(uint32_t), cudaHostAllocMapped);
   if (e == cudaSuccess) { *c->h_fault = 0; e = cudaHostGetDevicePointer((void**)&c->d_fault, c->h_fault, 0); }
+  if (e == cudaSuccess) e = cudaMalloc((void**)&c->d_plan_ticket, sizeof(uint32_t));
+  if (e == cudaSuccess) e = cudaMemset(c->d_plan_ticket, 0, sizeof(uint32_t));
+  if (e == cudaSuccess) e = cudaStreamSynchronize(cudaStreamLegacy);     // the context's stream may not wait for that one
   if (e != cudaSuccess) {
     cudaFree(c->d_rank);
+    cudaFree(c->d_plan_ticket);
     if (c->h_fault) cudaFreeHost(c->h_fault);
     delete c;
     return e == cudaErrorMemoryAllocation ? QV2_ERR_NOMEM : QV2_ERR_CUDA;
@@ -278,6 +282,7 @@ extern "C" int qv2_destroy(qv2_ctx* c) {
   cudaFree(c->d_partials_xe); cudaFree(c->d_kl_hist); cudaFree(c->d_tensor_absmax); cudaFree(c->d_keys);
   cudaFree(c->d_nf_acc); cudaFree(c->d_hist_acc); cudaFree(c->d_tickets); cudaFree(c->d_codes);
   cudaFree(c->d_rank); cudaFree(c->d_mx_codes); cudaFree(c->d_mx_scales);
+  cudaFree(c->d_attend); cudaFree(c->d_plan_ticket);
   for (void* p : c->kept) cudaFree(p);
   if (c->h_pinned) cudaFreeHost(c->h_pinned);
   cudaFreeHost(c->h_fault);

@@ -65,6 +65,9 @@ struct qv2_ctx {
   // qv2_mx_linear: the activations of the current call in packed form
   uint8_t* d_mx_codes = nullptr;  size_t cap_mx_codes = 0;  bool mx_codes_captured = false;
   uint8_t* d_mx_scales = nullptr; size_t cap_mx_scales = 0; bool mx_scales_captured = false;
+  // qv2_kv_attend: partial results of the current call; qv2_kv_plan: a counter that every call leaves at zero
+  uint8_t* d_attend = nullptr; size_t cap_attend = 0; bool attend_captured = false;
+  uint32_t* d_plan_ticket = nullptr;
   std::vector<void*> kept;        // outgrown blocks whose addresses a graph of the caller's may hold; freed with the context
   uint32_t* h_fault = nullptr;    // host-mapped word and its device address: a kernel that gave up waiting sets it
   uint32_t* d_fault = nullptr;
