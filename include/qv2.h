@@ -701,7 +701,7 @@ int qv2_norm_rotate(qv2_ctx* ctx, const qv2_head_rows* queries, const qv2_head_r
  * holds a NaN or an infinity.  What a query does not see does not change its result.
  * q: element (t, h, d) at q + t*q_token_ld + h*q_head_ld + d.  out: dense [total][q_heads][head_dim], element type as q's;
  * lse: binary32 [total][q_heads], nullable.  Rows outside every sequence are left as they were.  q_starts: non-decreasing,
- * held to 0 .. total.  max_new: no sequence has more queries than this (rows past it are not written); 0: unknown.
+ * held to 0 .. total; lens: held to 0 .. 2^31 - 1.  max_new: no sequence has more queries than this (rows past it are not written); 0: unknown.
  * Codes and scales enter exactly; queries of 16 bits are exact, of 32 bits held to 2^-22 of their largest element; weights
  * p_j times the value's scale are rounded to 11 bits (22 for 32-bit queries); sums are binary32.
  * The order of the sums depends on the lengths and sizes only: the same inputs give the same bits.

@@ -1,95 +1,740 @@
-// Attention of new tokens over the quantized paged cache.
-#include "qv2_serve.cuh"
+// Attention of new tokens over the quantized paged cache, few query rows to a key head: decoding steps and drafts.
+//
+// Bound by reading the cache (a key or value of 128 elements is 68 bytes at 4 bits, 132 at 8), next by turning codes into
+// operands.  A warp has one key head and a run of tokens and needs no other warp until the end: codes of TOK tokens
+// come by cp.async into its own ring in shared memory, go through registers as operands of mma.sync (16 tokens x 8 query rows
+// for the scores, transposed probabilities for the values), and the softmax runs along (running maximum and sum).
+//
+// Codes enter as they are: 4-bit codes and 8-bit integers are exact in binary16.  Scales of keys multiply the scores of their block
+// (32 columns: two products), or of the row; scales of values are split into the row's (multiplied into its weight) and
+// a power of two per block (multiplied into the codes, exactly).  Queries are brought to the top of binary16's range by
+// a power of two per row, so 16-bit ones are exact; of 32-bit ones (TERMS = 2) the rest of the rounding enters as a second
+// operand, and so for the weights.  Weights p_j * scale_j are held against the largest value scale met so far and
+// rounded to binary16, 2^14 at most, so what binary16 loses is below 2^-38 of the largest.
+#include "qv2_attend.cuh"
 
 namespace qv2 {
 
 namespace {
 
-constexpr uint32_t kAttendThreads = 256;
+constexpr uint32_t kWarps = 8, kThreads = 32 * kWarps;
+constexpr uint32_t kDepth = 2;                             // stages of a warp's ring
+constexpr int kWeightBits = 13;                            // weights stand 2^13 above p * scale / (largest scale)
+constexpr int kFactorBits = 12;                            // 4 bits: block factors stand 2^12 above scale / (largest of the row)
 
-template <class T> __device__ __forceinline__ float widen1(T v);
-template <> __device__ __forceinline__ float widen1(float v) { return v; }
-template <> __device__ __forceinline__ float widen1(__half v) { return __half2float(v); }
-template <> __device__ __forceinline__ float widen1(__nv_bfloat16 v) { return __bfloat162float(v); }
-
-// Element d of a cached row.
-template <int FORMAT>
-__device__ __forceinline__ float cached(const KvView& c, int which, uint64_t at, uint32_t d, uint32_t blocks) {
-  if (FORMAT == QV2_KV_I8) return (float)(int8_t)__ldg(c.codes[which] + at * c.dim + d) * __ldg(reinterpret_cast<const float*>(c.scales[which]) + at);
-  const uint32_t code = __ldg(c.codes[which] + at * 16 * blocks + d / 2) >> (4 * (d & 1));
-  float v[8];
-  mx_decode8(code & 15u, mx_scale(__ldg(c.scales[which] + at * blocks + d / 32)), v);
-  return v[0];
+__device__ __forceinline__ uint32_t shared_at(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }     // -126..127
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copy4(uint32_t dst, const void* src, bool there) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(there ? 4 : 0) : "memory");
+}
+__device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  return r;
+}
+__device__ __forceinline__ uint32_t pack_half(float lo, float hi) { const __half2 h = __floats2half2_rn(lo, hi); return *reinterpret_cast<const uint32_t*>(&h); }
+__device__ __forceinline__ uint32_t half_mul(uint32_t a, uint32_t b) {
+  const __half2 h = __hmul2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+// The four pairs of numbers of a word of 4-bit codes, as they lie.
+__device__ __forceinline__ void four_bits(uint32_t w, uint32_t (&h)[4]) {
+  asm("{\n\t.reg .b8 c0, c1, c2, c3;\n\t"
+      "mov.b32 {c0, c1, c2, c3}, %4;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %0, c0;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %1, c1;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %2, c2;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %3, c3;\n\t}"
+      : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(w));
+}
+// Bytes S and T of w, which are 8-bit integers plus 128, as a pair: 0x6400 + byte is the number 1024 + byte in binary16.
+template <uint32_t SELECT>
+__device__ __forceinline__ uint32_t eight_bits(uint32_t w) {
+  const uint32_t biased = __byte_perm(w, 0x64646464u, SELECT);
+  const __half2 h = __hsub2(*reinterpret_cast<const __half2*>(&biased), __half2half2(__ushort_as_half((unsigned short)0x6480)));
+  return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-// A CTA has one query head of one sequence, a warp one query at a time; lane l holds elements l, l + 32, ...
-template <class T, int FORMAT>
-__global__ void __launch_bounds__(kAttendThreads) attend_simple_kernel(AttendArgs a, FastDiv page) {
+template <uint32_t N>
+__device__ __forceinline__ void load_words(uint32_t (&w)[N], const uint8_t* p) {
+  if constexpr (N == 1) w[0] = *reinterpret_cast<const uint32_t*>(p);
+  else if constexpr (N == 2) { const uint2 v = *reinterpret_cast<const uint2*>(p); w[0] = v.x; w[1] = v.y; }
+  else
+#pragma unroll
+    for (uint32_t i = 0; i < N; i += 4) { const uint4 v = *reinterpret_cast<const uint4*>(p + 4 * i); w[i] = v.x; w[i + 1] = v.y; w[i + 2] = v.z; w[i + 3] = v.w; }
+}
+
+// cap * tanh(x / cap).  For results of 16 bits tanh(y) = 1 - 2 / (1 + e^2y), which is off by some 2^-23 of cap.
+template <int TERMS>
+__device__ __forceinline__ float capped(float x, float cap) {
+  if (TERMS == 2) return cap * tanhf(x / cap);
+  return cap - __fdividef(2.f * cap, 1.f + exp2_fast(2.f * kLog2e * __fdividef(x, cap)));
+}
+
+template <int FORMAT_, int DP_, int NT_, int TERMS_>
+struct Form {
+  static constexpr int FORMAT = FORMAT_, DP = DP_, NT = NT_, TERMS = TERMS_;
+  static constexpr bool MX = FORMAT == QV2_KV_MX4;
+  static constexpr uint32_t ROWS = 8 * NT;                 // query rows of an item
+  static constexpr uint32_t NB = DP / 32;                  // blocks of a row
+  static constexpr uint32_t RB = MX ? DP / 2 : DP;         // bytes of a row's codes
+  static constexpr uint32_t TOK = RB <= 64 ? 32 : 16;      // tokens of a stage: some 4 KB of codes
+  static constexpr uint32_t TILES = TOK / 16;
+  // Rows in shared memory lie so far apart that the loads of a warp (keys: 8 rows, 4 lanes each; values: 4 pairs of rows, 8
+  // lanes each) meet every bank once.
+  static constexpr uint32_t KS = RB + (MX ? 16 : 32), VS = RB + 16;
+  static constexpr uint32_t RAW = MX ? 4 * ((NB + 6) / 4) : 4;      // bytes of a row's scales as they lie in memory: whole words
+  static constexpr uint32_t STAGE = TOK * (KS + VS + 2 * RAW + 4);  // ... and a word that says where they begin, or that there is no such token
+  static constexpr uint32_t READY = MX ? TOK * (4 * NB + 4) + TOK * 2 * NB : TOK * 8;   // scales as the products want them
+  static constexpr uint32_t WARP = (kDepth * STAGE + READY + 15) / 16 * 16;
+  static constexpr uint32_t EXCHANGE = kWarps * ROWS * (DP + 2) * 4;
+  static constexpr uint32_t SMEM = kWarps * WARP > EXCHANGE ? kWarps * WARP : EXCHANGE;
+  static constexpr uint32_t PIECE = ROWS * (DP + 2);       // floats of a head of a partial result
+  // CTAs per SM.  Where the accumulators and operands of a thread leave no room in 128 registers, one.
+  static constexpr int RESIDENT = (DP / 16) * 4 * NT + 4 * NB * NT * TERMS > 64 || SMEM > 113000 ? 1 : 2;
+};
+
+struct RowsArgs {
+  AttendArgs a;
+  FastDiv page, group;
+  uint32_t hw, hw_log;                                     // key heads of a CTA (a power of two), warps / hw warps share the tokens
+  uint32_t row_limit;                                      // sequences of more rows are not this kernel's
+  uint32_t vec_codes, vec_out;                             // codes by 16 bytes, results by four elements
+  float* parts;
+  AttendPiece* pieces;
+};
+
+// Units of every item of a sequence, and its items.
+template <class F>
+__device__ __forceinline__ void units_of(const RowsArgs& p, const AttendSeq& s, uint32_t* units, uint32_t* tiles) {
+  const uint64_t rows = (uint64_t)s.n * p.a.group;
+  *tiles = rows > p.row_limit ? 0 : (uint32_t)((rows + F::ROWS - 1) / F::ROWS);
+  const uint32_t sees = (uint32_t)p.a.window + (F::ROWS + p.a.group - 1) / p.a.group;       // tokens that a tile of rows sees at most
+  const uint32_t wide = min(min((uint32_t)s.len, p.a.room), sees), unit = F::TOK * (kWarps >> p.hw_log);
+  *units = max(1u, (wide + unit - 1) / unit);
+}
+
+template <class F>
+__global__ void __launch_bounds__(kThreads, F::RESIDENT) attend_rows_kernel(const RowsArgs p) {
+  constexpr bool MX = F::MX;
+  constexpr int NT = F::NT, DP = F::DP, TERMS = F::TERMS;
+  constexpr uint32_t NB = F::NB, TOK = F::TOK, TILES = F::TILES, ROWS = F::ROWS;
+  extern __shared__ __align__(16) uint8_t smem[];
+  __shared__ uint64_t scan[kWarps];
+  __shared__ AttendUnits found;
+  __shared__ float2 top_sum[kWarps][ROWS];
+  const AttendArgs& a = p.a;
+  const uint32_t tid = threadIdx.x, warp = tid / 32, lane = tid % 32, g = lane / 4, t = lane % 4;
   dependency_wait();
   allow_dependents();
-  const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32, head = blockIdx.x, kv = head / a.group, blocks = (a.c.dim + 31) / 32;
-  const AttendSeq s = attend_seq(a, blockIdx.y);
-  const int64_t room = (int64_t)a.table_ld * page.d;
-  const float slope = a.slopes ? __ldg(a.slopes + head) : 0.f;
-  for (uint32_t i = warp; i < s.n; i += kAttendThreads / 32) {
-    const uint64_t row = s.row0 + i;
-    const int64_t pos = s.len - s.n + i, j0 = max(pos - a.window + 1, (int64_t)0), j1 = min(pos + 1, room);
-    float q[8], o[8], top = -INFINITY, sum = 0.f;
+
+  // ---- this CTA's units
+  const uint32_t groups = a.c.heads >> p.hw_log;                               // groups of key heads
+  auto units_in = [&](uint32_t s) -> uint64_t {
+    if (s >= a.seqs) return 0;
+    uint32_t units, tiles;
+    units_of<F>(p, attend_seq(a, s), &units, &tiles);
+    return (uint64_t)units * tiles * groups;
+  };
+  uint64_t all = 0;
+  for (uint32_t base = 0; base < a.seqs; base += kThreads) all += units_in(base + tid);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const uint32_t d = lane + 32 * k;
-      q[k] = d < a.c.dim ? widen1<T>(((const T*)a.q)[row * a.q_token_ld + head * a.q_head_ld + d]) : 0.f;
-      o[k] = 0.f;
-    }
-    for (int64_t j = j0; j < j1; ++j) {
-      const uint32_t pg = page.div((uint32_t)j);
-      const int32_t id = __ldg(a.table + blockIdx.y * a.table_ld + pg);
-      if (id < 0 || (uint32_t)id >= a.c.pages) continue;
-      const uint64_t at = ((uint64_t)id * page.d + ((uint32_t)j - pg * page.d)) * a.c.heads + kv;
-      float x = 0.f;
+  for (int o = 16; o > 0; o >>= 1) all += __shfl_xor_sync(0xffffffffu, all, o);
+  if (lane == 0) scan[warp] = all;
+  __syncthreads();
+  all = 0;
 #pragma unroll
-      for (int k = 0; k < 8; ++k)
-        if (lane + 32 * k < a.c.dim) x = fmaf(q[k], cached<FORMAT>(a.c, 0, at, lane + 32 * k, blocks), x);
+  for (uint32_t w = 0; w < kWarps; ++w) all += scan[w];
+  const uint32_t ctas = (uint32_t)min((uint64_t)gridDim.x, all);                // every one of these has a unit at least
+  if (tid == 0) p.pieces[blockIdx.x].followers = 0;
+  if (blockIdx.x >= ctas) return;
+  const uint64_t u_begin = all * blockIdx.x / ctas, u_end = all * (blockIdx.x + 1) / ctas;
+  for (uint64_t base = 0, before = 0; base < a.seqs; base += kThreads) {        // which sequence u_begin falls into
+    __syncthreads();
+    const uint64_t mine = units_in((uint32_t)base + tid);
+    uint64_t sum = mine;
 #pragma unroll
-      for (int b = 16; b > 0; b >>= 1) x += __shfl_xor_sync(0xffffffffu, x, b);
-      x *= a.scale;
-      if (a.cap > 0.f) x = a.cap * tanhf(x / a.cap);
-      x += slope * (float)(j - pos);
-      float v[8];
-      bool bad = false;
+    for (int o = 1; o < 32; o <<= 1) { const uint64_t v = __shfl_up_sync(0xffffffffu, sum, o); if (lane >= o) sum += v; }
+    if (lane == 31) scan[warp] = sum;
+    __syncthreads();
+    uint64_t whole = 0;
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        v[k] = lane + 32 * k < a.c.dim ? cached<FORMAT>(a.c, 1, at, lane + 32 * k, blocks) : 0.f;
-        bad |= isnan(v[k]);
+    for (uint32_t w = 0; w < kWarps; ++w) { if (w < warp) sum += scan[w]; whole += scan[w]; }
+    const uint64_t first = before + sum - mine;
+    if (mine && u_begin >= first && u_begin < first + mine) { found.before = first; found.seq = (uint32_t)base + tid; }
+    before += whole;
+    if (u_begin < before) break;
+  }
+  __syncthreads();
+  uint32_t seq = found.seq;
+  uint64_t at_unit = u_begin, seq_begin = found.before;
+
+  const uint32_t head_in = warp & (p.hw - 1), part = warp >> p.hw_log, parts = kWarps >> p.hw_log;
+  uint8_t* const mine = smem + warp * F::WARP;
+  const uint32_t ring = shared_at(mine);
+  uint8_t* const ready = mine + kDepth * F::STAGE;
+  float* const k_scale = reinterpret_cast<float*>(ready);                       // 4 bits: [token][block], 8 bits: [token]
+  float* const v_scale = k_scale + TOK * (MX ? NB : 1);                         // [token], against the largest
+  __half* const v_factor = reinterpret_cast<__half*>(v_scale + TOK);            // 4 bits: [block][token]
+  const uint32_t blocks = (a.c.dim + 31) / 32, row_bytes = MX ? 16 * blocks : a.c.dim;
+
+  while (at_unit < u_end) {
+    // ---- the next item, or the part of it that is this CTA's
+    AttendSeq s = attend_seq(a, seq);
+    uint32_t units, tiles;
+    units_of<F>(p, s, &units, &tiles);
+    const uint64_t in_seq = (uint64_t)units * tiles * groups;
+    if (at_unit - seq_begin >= in_seq) { seq_begin += in_seq; ++seq; continue; }
+    const uint32_t item = (uint32_t)((at_unit - seq_begin) / units), unit0 = (uint32_t)((at_unit - seq_begin) % units);
+    const uint32_t unit1 = (uint32_t)min((uint64_t)units, unit0 + (u_end - at_unit));
+    const uint32_t tile = item / groups, hg = item % groups, kv = (hg << p.hw_log) + head_in;
+    const uint32_t rows = s.n * a.group, row0 = tile * ROWS, row1 = min(rows, row0 + ROWS);
+    const int32_t pos0 = s.len - (int32_t)s.n;                                  // position of the sequence's first query
+    const int32_t p_first = pos0 + (int32_t)p.group.div(row0), p_last = pos0 + (int32_t)p.group.div(row1 - 1);
+    const uint32_t j0 = min(p_first >= a.window ? (uint32_t)(p_first - a.window + 1) : 0u, a.room);   // tokens that any of the rows sees: j0 .. j1 - 1
+    const uint32_t j1 = max(min((uint32_t)(max(p_last, -1) + 1), a.room), j0);
+    const int32_t* const pages = a.table + seq * a.table_ld;
+
+    // ---- queries: as operands, with what brings their scores back (to powers of two unless they are capped)
+    uint32_t qf[TERMS][NT][4 * NB];
+    float back[NT][2];
+    int32_t pos[NT][2];
+    float slope[NT][2];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const uint32_t r = row0 + 8 * n + g, i = p.group.div(r);
+      const bool there = r < row1;
+      float v[NB][8];
+      uint32_t top = 0;
+      const uint64_t q_at = (uint64_t)(s.row0 + i) * a.q_token_ld + (uint64_t)(kv * a.group + (r - i * a.group)) * a.q_head_ld;
+#pragma unroll
+      for (uint32_t b = 0; b < NB; ++b) {
+        const uint32_t d = 32 * b + 8 * t;
+        auto bring = [&](auto chunk, const auto* from) {
+          chunk.zero();
+          if (there && d + 8 <= a.c.dim) chunk.load_any(from + q_at + d);
+          else if (there && d < a.c.dim) chunk.load_some(from + q_at + d, a.c.dim - d);
+          chunk.widen(v[b]);
+          top = max(top, chunk.top_bits());
+        };
+        if (a.dtype == kBF16) bring(Chunk8<__nv_bfloat16>(), (const __nv_bfloat16*)a.q);
+        else if (a.dtype == kF16) bring(Chunk8<__half>(), (const __half*)a.q);
+        else bring(Chunk8<float>(), (const float*)a.q);
       }
-      const float poison = __any_sync(0xffffffffu, bad) ? NAN : 0.f;
-      const float now = isnan(x) ? x : fmaxf(top, x), was = top == -INFINITY ? 0.f : expf(top - now), p = expf(x - now);
-      top = now;
-      sum = sum * was + p;
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      const int e = top ? max((int)(top >> 23) - 127, -100) : 0;                // the largest element is 2^e to 2^(e+1)
+      const float up = power_of_two(14 - min(e, 127));
 #pragma unroll
-      for (int k = 0; k < 8; ++k) o[k] = fmaf(p, v[k] + poison, o[k] * was);
+      for (uint32_t b = 0; b < NB; ++b)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const float x = v[b][2 * k] * up, y = v[b][2 * k + 1] * up;
+          qf[0][n][4 * b + k] = pack_half(x, y);
+          if (TERMS == 2) {
+            const float2 h = __half22float2(*reinterpret_cast<const __half2*>(&qf[0][n][4 * b + k]));
+            qf[TERMS - 1][n][4 * b + k] = pack_half(x - h.x, y - h.y);
+          }
+        }
+      const float down = top >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : power_of_two(min(e, 127) - 14) * a.scale * (a.cap > 0.f ? 1.f : kLog2e);
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        back[n][k] = __shfl_sync(0xffffffffu, down, 4 * (2 * t + k));
+        const uint32_t rr = row0 + 8 * n + 2 * t + k, ii = p.group.div(rr);
+        pos[n][k] = rr < row1 ? pos0 + (int32_t)ii : p_last;                    // (rows that are not there hold nothing up)
+        slope[n][k] = a.slopes && rr < row1 ? kLog2e * __ldg(a.slopes + kv * a.group + (rr - ii * a.group)) : 0.f;
+      }
     }
+    float o[NT][DP / 16][4], top_x[NT][2], sum[NT][2];
+    int v_top = -126;                                                          // exponent of the largest value scale so far
 #pragma unroll
-    for (int k = 0; k < 8; ++k)
-      if (lane + 32 * k < a.c.dim) ((T*)a.out)[(row * a.q_heads + head) * a.c.dim + lane + 32 * k] = Chunk8<T>::narrow(sum == 0.f ? 0.f : o[k] / sum);
-    if (a.lse && lane == 0) a.lse[row * a.q_heads + head] = sum == 0.f ? -INFINITY : top + logf(sum);
+    for (int n = 0; n < NT; ++n) {
+      top_x[n][0] = top_x[n][1] = -INFINITY; sum[n][0] = sum[n][1] = 0.f;
+#pragma unroll
+      for (int m = 0; m < DP / 16; ++m)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) o[n][m][k] = 0.f;
+    }
+
+    // ---- tokens: stage k of this warp begins at j0 + (first + k * parts) * TOK
+    const uint32_t n_stages = unit1 - unit0;
+    auto stage_token = [&](uint32_t k) { return (uint64_t)j0 + (uint64_t)((unit0 + k) * parts + part) * TOK; };
+    auto page_of = [&](uint32_t k) -> int32_t {                                  // of token `lane` of a stage; negative: no such token
+      const uint64_t j = stage_token(k) + lane;
+      if (k >= n_stages || lane >= TOK || j >= j1) return -1;
+      const int32_t id = __ldg(pages + p.page.div((uint32_t)j));
+      return id >= 0 && (uint32_t)id < a.c.pages ? id : -1;
+    };
+    auto fetch = [&](uint32_t k, int32_t id) {                                   // codes and scales of a stage into its place of the ring
+      const uint32_t place = (k % kDepth) * F::STAGE;
+      if (k < n_stages) {
+        const uint32_t j = (uint32_t)stage_token(k) + lane, off = j - p.page.div(j) * p.page.d;
+        const uint64_t at = id < 0 ? 0 : ((uint64_t)(uint32_t)id * p.page.d + off) * a.c.heads + kv;
+        constexpr uint32_t CH = F::RB / 16, PER = 32 / CH;                       // 16-byte pieces of a row, rows of one instruction
+#pragma unroll
+        for (uint32_t i = 0; i < TOK / PER; ++i) {
+          const uint32_t tok = i * PER + lane / CH, c16 = 16 * (lane % CH);
+          const uint64_t row = __shfl_sync(0xffffffffu, at, tok);
+          const bool there = __shfl_sync(0xffffffffu, id, tok) >= 0 && c16 < row_bytes;
+#pragma unroll
+          for (int w = 0; w < 2; ++w) {
+            const uint32_t dst = place + (w ? TOK * F::KS + tok * F::VS : tok * F::KS) + c16;
+            const uint8_t* src = a.c.codes[w] + (there ? row * row_bytes + c16 : 0);
+            if (MX || p.vec_codes) copy16(ring + dst, src, there);
+            else
+              for (uint32_t b = 0; b < 16; ++b) mine[dst + b] = there && c16 + b < row_bytes ? __ldg(src + b) : (uint8_t)0;
+          }
+        }
+        const uint32_t raw = place + TOK * (F::KS + F::VS);
+        if (lane < TOK) {
+          if (MX) {
+            const uint64_t first = at * blocks;
+            uint32_t skip = 0;
+#pragma unroll
+            for (int w = 0; w < 2; ++w) {                                        // whole words, each of which holds a wanted byte
+              const uintptr_t from = (uintptr_t)a.c.scales[w] + first;
+              const uint32_t lead = (uint32_t)(from & 3u);
+              skip |= lead << (8 * w);
+#pragma unroll
+              for (uint32_t i = 0; i < F::RAW / 4; ++i)
+                if (4 * i < lead + blocks) copy4(ring + raw + w * TOK * F::RAW + lane * F::RAW + 4 * i, (const void*)((from & ~(uintptr_t)3u) + 4 * i), id >= 0);
+            }
+            *reinterpret_cast<uint32_t*>(mine + raw + 2 * TOK * F::RAW + 4 * lane) = id >= 0 ? skip : ~0u;
+          } else {
+#pragma unroll
+            for (int w = 0; w < 2; ++w) copy4(ring + raw + w * TOK * F::RAW + 4 * lane, reinterpret_cast<const float*>(a.c.scales[w]) + at, id >= 0);
+            *reinterpret_cast<uint32_t*>(mine + raw + 2 * TOK * F::RAW + 4 * lane) = id >= 0 ? 0u : ~0u;
+          }
+        }
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    int32_t next_id = page_of(0);
+#pragma unroll 1
+    for (uint32_t k = 0; k < kDepth; ++k) {
+      const int32_t id = next_id;
+      next_id = page_of(k + 1);
+      fetch(k, id);
+    }
+#pragma unroll 1
+    for (uint32_t k = 0; k < n_stages; ++k) {
+      asm volatile("cp.async.wait_group %0;" ::"n"(kDepth - 1) : "memory");
+      __syncwarp();
+      const int32_t id = next_id;                                                // of stage k + kDepth
+      next_id = page_of(k + kDepth + 1);
+      const uint32_t place = (k % kDepth) * F::STAGE, raw = place + TOK * (F::KS + F::VS);
+      const uint32_t j_stage = (uint32_t)stage_token(k);
+
+      // ---- scales of the stage's tokens, one to a lane
+      uint32_t meta = ~0u;
+      if (lane < TOK) meta = *reinterpret_cast<const uint32_t*>(mine + raw + 2 * TOK * F::RAW + 4 * lane);
+      const uint32_t real = __ballot_sync(0xffffffffu, meta != ~0u);             // tokens that there are
+      float v_row = 0.f;                                                         // scale of this lane's value
+      uint32_t v_bytes[MX ? NB : 1];
+      int v_most = 0;
+      if (MX) {
+        const uint8_t* kb = mine + raw + lane * F::RAW + (meta & 3u);
+        const uint8_t* vb = mine + raw + TOK * F::RAW + lane * F::RAW + (meta >> 8 & 3u);
+#pragma unroll
+        for (uint32_t b = 0; b < NB; ++b) {
+          v_bytes[MX ? b : 0] = 0;
+          float ks = 0.f;
+          if (meta != ~0u && b < blocks) {
+            ks = mx_scale(kb[b]);
+            v_bytes[MX ? b : 0] = vb[b];
+            v_most = max(v_most, (int)vb[b]);
+          }
+          if (lane < TOK) k_scale[lane * NB + b] = ks;
+        }
+        v_row = meta == ~0u ? 0.f : mx_scale((uint32_t)v_most);                   // NaN if any block is poisoned
+#pragma unroll
+        for (uint32_t b = 0; b < NB; ++b) {
+          // 2^(own - row's largest + kFactorBits) in binary16, down to its smallest number 2^-24
+          const int f = (int)v_bytes[MX ? b : 0] - v_most + kFactorBits;
+          const uint32_t h = v_most == 255 || f < -24 ? 0u : f >= -14 ? (uint32_t)(f + 15) << 10 : 1u << (f + 24);
+          if (lane < TOK) v_factor[b * TOK + lane] = __ushort_as_half((unsigned short)h);
+        }
+      } else if (lane < TOK) {
+        k_scale[lane] = *reinterpret_cast<const float*>(mine + raw + 4 * lane);
+        v_row = *reinterpret_cast<const float*>(mine + raw + TOK * F::RAW + 4 * lane);
+      }
+      const uint32_t field = __float_as_uint(v_row) >> 23 & 255u;                // finite scales are positive
+      const int highest = __reduce_max_sync(0xffffffffu, field == 255u ? -126 : min(max((int)field - 127, -126), 126));
+      if (highest > v_top) {
+        const float f = v_top == -126 ? 0.f : power_of_two(max(v_top - highest, -126));   // (nothing has been added at -126 that could be seen)
+        v_top = highest;
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int m = 0; m < DP / 16; ++m)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[n][m][i] *= f;
+      }
+      if (lane < TOK) v_scale[lane] = v_row * power_of_two(-v_top) * (float)(1 << kWeightBits);
+      __syncwarp();
+
+      // ---- scores: rows are tokens, columns queries
+      float x[TILES][NT][4];
+#pragma unroll
+      for (uint32_t l = 0; l < TILES; ++l) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[l][n][i] = 0.f;
+        const uint8_t* k0 = mine + place + (16 * l + g) * F::KS;
+        const uint8_t* k1 = k0 + 8 * F::KS;
+#pragma unroll
+        for (uint32_t b = 0; b < NB; ++b) {
+          uint32_t c0[4], c1[4];
+          if (MX) {
+            four_bits(*reinterpret_cast<const uint32_t*>(k0 + 16 * b + 4 * t), c0);
+            four_bits(*reinterpret_cast<const uint32_t*>(k1 + 16 * b + 4 * t), c1);
+          } else {
+            const uint2 w0 = *reinterpret_cast<const uint2*>(k0 + 32 * b + 8 * t), w1 = *reinterpret_cast<const uint2*>(k1 + 32 * b + 8 * t);
+            c0[0] = eight_bits<0x4140>(w0.x ^ 0x80808080u); c0[1] = eight_bits<0x4342>(w0.x ^ 0x80808080u);
+            c0[2] = eight_bits<0x4140>(w0.y ^ 0x80808080u); c0[3] = eight_bits<0x4342>(w0.y ^ 0x80808080u);
+            c1[0] = eight_bits<0x4140>(w1.x ^ 0x80808080u); c1[1] = eight_bits<0x4342>(w1.x ^ 0x80808080u);
+            c1[2] = eight_bits<0x4140>(w1.y ^ 0x80808080u); c1[3] = eight_bits<0x4342>(w1.y ^ 0x80808080u);
+          }
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            float acc[4] = {0.f, 0.f, 0.f, 0.f};
+            float (&into)[4] = MX ? acc : x[l][n];
+#pragma unroll
+            for (int term = TERMS - 1; term >= 0; --term) {
+              mma16816(into, c0[0], c1[0], c0[1], c1[1], qf[term][n][4 * b], qf[term][n][4 * b + 1]);
+              mma16816(into, c0[2], c1[2], c0[3], c1[3], qf[term][n][4 * b + 2], qf[term][n][4 * b + 3]);
+            }
+            if (MX) {
+              const float s0 = k_scale[(16 * l + g) * NB + b], s1 = k_scale[(16 * l + g + 8) * NB + b];
+              x[l][n][0] = fmaf(acc[0], s0, x[l][n][0]); x[l][n][1] = fmaf(acc[1], s0, x[l][n][1]);
+              x[l][n][2] = fmaf(acc[2], s1, x[l][n][2]); x[l][n][3] = fmaf(acc[3], s1, x[l][n][3]);
+            }
+          }
+        }
+        if (!MX) {
+          const float s0 = k_scale[16 * l + g], s1 = k_scale[16 * l + g + 8];
+#pragma unroll
+          for (int n = 0; n < NT; ++n) { x[l][n][0] *= s0; x[l][n][1] *= s0; x[l][n][2] *= s1; x[l][n][3] *= s1; }
+        }
+      }
+
+      // ---- what is seen, and the softmax so far
+      const bool plain = !(a.cap > 0.f) && !a.slopes;
+      const bool every = real == 0xffffffffu >> (32 - TOK) && (int32_t)(j_stage + TOK - 1) <= p_first && p_last - (int32_t)j_stage < a.window;
+      uint32_t seen = 0xffffffffu;                                               // bit of x[l][n][i]: 4 * (l * NT + n) + i
+      static_assert(4 * TILES * NT <= 32, "bits");
+#pragma unroll
+      for (uint32_t l = 0; l < TILES; ++l)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float v = x[l][n][i] * back[n][i & 1];
+            const uint32_t tok = 16 * l + g + 8 * (i >> 1);
+            const int32_t at = (int32_t)(j_stage + tok), mine_pos = pos[n][i & 1];
+            if (!plain) {
+              if (a.cap > 0.f) v = kLog2e * capped<TERMS>(v, a.cap);
+              v = fmaf(slope[n][i & 1], (float)(int32_t)((uint32_t)at - (uint32_t)mine_pos), v);
+            }
+            if (!every) {
+              const bool ok = (real >> tok & 1u) && at <= mine_pos && (uint32_t)mine_pos - (uint32_t)at < (uint32_t)a.window;
+              if (!ok) { v = -INFINITY; seen &= ~(1u << (4 * (l * NT + n) + i)); }
+            }
+            x[l][n][i] = v;
+          }
+      bool moved = false;
+      float shrink[NT][2];
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          float m = fmaxf(x[0][n][k], x[0][n][k + 2]);
+#pragma unroll
+          for (uint32_t l = 1; l < TILES; ++l) m = fmaxf(m, fmaxf(x[l][n][k], x[l][n][k + 2]));
+#pragma unroll
+          for (int b = 4; b < 32; b <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, b));
+          m = fmaxf(m, top_x[n][k]);
+          const float from = m == -INFINITY ? 0.f : m;
+          shrink[n][k] = exp2_fast(top_x[n][k] - from);
+          moved |= top_x[n][k] != m;
+          top_x[n][k] = m;
+          float add = 0.f;
+#pragma unroll
+          for (uint32_t l = 0; l < TILES; ++l) {
+            x[l][n][k] = exp2_fast(x[l][n][k] - from); x[l][n][k + 2] = exp2_fast(x[l][n][k + 2] - from);
+            add += x[l][n][k] + x[l][n][k + 2];
+          }
+          sum[n][k] = fmaf(sum[n][k], shrink[n][k], add);
+        }
+      if (__any_sync(0xffffffffu, moved)) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int m = 0; m < DP / 16; ++m) {
+            o[n][m][0] *= shrink[n][0]; o[n][m][1] *= shrink[n][1]; o[n][m][2] *= shrink[n][0]; o[n][m][3] *= shrink[n][1];
+          }
+      }
+      uint32_t wf[TERMS][TILES][NT][2];                                          // weights as operands: rows tokens, columns queries
+#pragma unroll
+      for (uint32_t l = 0; l < TILES; ++l)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            const float vs = v_scale[16 * l + g + 8 * r];
+            const uint32_t bit = 4 * (l * NT + n) + 2 * r;
+            const float w0 = seen >> bit & 1u ? x[l][n][2 * r] * vs : 0.f, w1 = seen >> (bit + 1) & 1u ? x[l][n][2 * r + 1] * vs : 0.f;
+            const uint32_t h = pack_half(w0, w1);
+            wf[0][l][n][r] = transpose8x8(h);
+            if (TERMS == 2) {
+              const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
+              wf[TERMS - 1][l][n][r] = transpose8x8(pack_half(w0 - f.x, w1 - f.y));
+            }
+          }
+
+      // ---- values: rows are elements (this lane's DP / 8 neighbouring ones, two by two), columns queries
+      const uint8_t* v0 = mine + place + TOK * F::KS + 2 * t * F::VS + g * (F::RB / 8);
+      auto product = [&](uint32_t l, int m, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, float (&into)[NT][4]) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int term = TERMS - 1; term >= 0; --term)
+            mma16816(TERMS == 2 ? into[n] : o[n][m], a0, a1, a2, a3, wf[term][l][n][0], wf[term][l][n][1]);
+      };
+      constexpr uint32_t WORDS = F::RB / 32;                                     // words of a row that are this lane's
+      constexpr int PER_WORD = MX ? 4 : 2;                                       // products of a word
+      uint32_t code[TILES][4][WORDS];                                            // of tokens 2t, 2t + 1, 2t + 8, 2t + 9
+#pragma unroll
+      for (uint32_t l = 0; l < TILES; ++l)
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) load_words<WORDS>(code[l][i], v0 + (16 * l + (i & 1) + 8 * (i >> 1)) * F::VS);
+#pragma unroll
+      for (uint32_t w = 0; w < WORDS; ++w) {
+        float fresh[PER_WORD][NT][4];                                            // TERMS = 2: sums of this stage alone, added in binary32 below
+        if (TERMS == 2)
+#pragma unroll
+          for (int m = 0; m < PER_WORD; ++m)
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) fresh[m][n][i] = 0.f;
+#pragma unroll
+        for (uint32_t l = 0; l < TILES; ++l) {
+          const uint32_t wa = code[l][0][w], wb = code[l][1][w], wc = code[l][2][w], wd = code[l][3][w];
+          if (MX) {
+            const uint32_t block = g * NB / 8;
+            const uint32_t f0 = *reinterpret_cast<const uint32_t*>(v_factor + block * TOK + 16 * l + 2 * t);
+            const uint32_t f1 = *reinterpret_cast<const uint32_t*>(v_factor + block * TOK + 16 * l + 2 * t + 8);
+            constexpr uint32_t LOW = 0x0f0f0f0fu;
+            uint32_t e0[4], d0[4], e1[4], d1[4];                                 // even and odd elements, two tokens to a pair
+            four_bits((wa & LOW) | ((wb & LOW) << 4), e0);
+            four_bits(((wa >> 4) & LOW) | (wb & ~LOW), d0);
+            four_bits((wc & LOW) | ((wd & LOW) << 4), e1);
+            four_bits(((wc >> 4) & LOW) | (wd & ~LOW), d1);
+#pragma unroll
+            for (int m = 0; m < 4; ++m) product(l, 4 * w + m, half_mul(e0[m], f0), half_mul(d0[m], f0), half_mul(e1[m], f1), half_mul(d1[m], f1), fresh[m % PER_WORD]);
+          } else {
+            const uint32_t xa = wa ^ 0x80808080u, xb = wb ^ 0x80808080u, xc = wc ^ 0x80808080u, xd = wd ^ 0x80808080u;
+            const uint32_t ab0 = __byte_perm(xa, xb, 0x5140), ab1 = __byte_perm(xa, xb, 0x7362), cd0 = __byte_perm(xc, xd, 0x5140), cd1 = __byte_perm(xc, xd, 0x7362);
+            product(l, 2 * w, eight_bits<0x4140>(ab0), eight_bits<0x4342>(ab0), eight_bits<0x4140>(cd0), eight_bits<0x4342>(cd0), fresh[0]);
+            product(l, 2 * w + 1, eight_bits<0x4140>(ab1), eight_bits<0x4342>(ab1), eight_bits<0x4140>(cd1), eight_bits<0x4342>(cd1), fresh[1]);
+          }
+        }
+        if (TERMS == 2)
+#pragma unroll
+          for (int m = 0; m < PER_WORD; ++m)
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) o[n][PER_WORD * w + m][i] += fresh[m][n][i];
+      }
+      __syncwarp();
+      fetch(k + kDepth, id);
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+
+    // ---- the warps' results meet in shared memory
+    __syncthreads();
+    float* const o_all = reinterpret_cast<float*>(smem);                          // [warp][row][DP]
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        float total = sum[n][k];
+#pragma unroll
+        for (int b = 4; b < 32; b <<= 1) total += __shfl_xor_sync(0xffffffffu, total, b);
+        const uint32_t r = 8 * n + 2 * t + k;
+        if (g == 0) top_sum[warp][r] = make_float2(top_x[n][k], total);
+        float* to = o_all + (warp * ROWS + r) * DP + g * (DP / 8);
+        const float f0 = power_of_two(-kWeightBits - (MX ? kFactorBits : 0)), f1 = power_of_two(v_top);
+#pragma unroll
+        for (int m = 0; m < DP / 16; ++m) *reinterpret_cast<float2*>(to + 2 * m) = make_float2(o[n][m][k] * f0 * f1, o[n][m][k + 2] * f0 * f1);
+      }
+    __syncthreads();
+    const bool whole = unit0 == 0 && unit1 == units;
+    const uint32_t place = unit0 == 0 ? 1 : 0;
+    float* const to_part = p.parts + ((uint64_t)blockIdx.x * 2 + place) * p.hw * F::PIECE;
+    if (!whole && place == 1 && tid == 0) {
+      // the item's last unit is among those of CTA c where c * all / ctas <= last < (c + 1) * all / ctas
+      const uint64_t last = at_unit + units - 1;
+      uint32_t c = (uint32_t)(last * ctas / all);
+      while (all * c / ctas > last) --c;
+      while (all * (c + 1) / ctas <= last) ++c;
+      AttendPiece h;
+      h.followers = c - blockIdx.x; h.row0 = s.row0; h.rows = rows; h.tile = tile; h.heads = hg;
+      p.pieces[blockIdx.x] = h;
+    }
+    const uint32_t n_rows = row1 - row0, quads = DP / 4;
+    for (uint32_t i = tid; i < p.hw * n_rows * quads; i += kThreads) {
+      const uint32_t d = 4 * (i % quads), r = i / quads % n_rows, h = i / quads / n_rows;
+      float top = -INFINITY, total = 0.f;
+      for (uint32_t w = h; w < kWarps; w += p.hw) top = fmaxf(top, top_sum[w][r].x);
+      const float from = top == -INFINITY ? 0.f : top;
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (uint32_t w = h; w < kWarps; w += p.hw) {
+        const float2 ts = top_sum[w][r];
+        const float f = exp2_fast(ts.x - from);
+        const float4 ov = *reinterpret_cast<const float4*>(o_all + (w * ROWS + r) * DP + d);
+        total = fmaf(ts.y, f, total);
+        v.x = fmaf(ov.x, f, v.x); v.y = fmaf(ov.y, f, v.y); v.z = fmaf(ov.z, f, v.z); v.w = fmaf(ov.w, f, v.w);
+      }
+      if (whole) attend_store(a, s.row0, row0 + r, p.group, (hg << p.hw_log) + h, d, v, top, total, p.vec_out);
+      else {
+        *reinterpret_cast<float4*>(to_part + (h * ROWS + r) * DP + d) = v;
+        if (d == 0) *reinterpret_cast<float2*>(to_part + p.hw * ROWS * DP + 2 * (h * ROWS + r)) = make_float2(top, total);
+      }
+    }
+    __syncthreads();
+    at_unit += unit1 - unit0;
   }
 }
 
-template <class T>
-cudaError_t attend_typed(const Launch& l, const AttendArgs& a, uint64_t* launches) {
-  auto* kernel = a.c.format == QV2_KV_MX4 ? attend_simple_kernel<T, QV2_KV_MX4> : attend_simple_kernel<T, QV2_KV_I8>;
-  cudaError_t e = launch_grid(l, kernel, dim3(a.q_heads, a.seqs), kAttendThreads, 0, a, FastDiv(a.c.page_size));
+// Adds up the items that were cut.  CTA (c, y) has every kJoinRows-th row of the item that main CTA c began; its warps share the pieces.
+constexpr uint32_t kJoinThreads = 256, kJoinRows = 8;
+__global__ void __launch_bounds__(kJoinThreads)
+attend_join_kernel(const AttendArgs a, FastDiv group, const float* parts, const AttendPiece* pieces, uint32_t hw, uint32_t hw_log, uint32_t tile_rows, uint32_t dp, uint32_t vec_out) {
+  __shared__ float4 sums[kJoinThreads / 32][64];
+  __shared__ float2 top_sum[kJoinThreads / 32];
+  dependency_wait();
+  allow_dependents();
+  const AttendPiece h = pieces[blockIdx.x];
+  if (h.followers == 0) return;
+  const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32, quads = dp / 4, n_rows = min(tile_rows, h.rows - h.tile * tile_rows);
+  const uint64_t piece = (uint64_t)hw * tile_rows * (dp + 2);
+  for (uint32_t i = blockIdx.y; i < n_rows << hw_log; i += kJoinRows) {
+    const uint32_t r = i >> hw_log, head = i & (hw - 1);
+    float top = -INFINITY, total = 0.f;
+    float4 v[2] = {};
+#pragma unroll 4
+    for (uint32_t f = warp; f <= h.followers; f += kJoinThreads / 32) {
+      const float* from = parts + ((uint64_t)(blockIdx.x + f) * 2 + (f == 0 ? 1 : 0)) * piece;
+      const float2 ts = *reinterpret_cast<const float2*>(from + hw * tile_rows * dp + 2 * (head * tile_rows + r));
+      const float m = fmaxf(top, ts.x), base = m == -INFINITY ? 0.f : m, was = exp2_fast(top - base), is = exp2_fast(ts.x - base);
+      top = m;
+      total = total * was + ts.y * is;
+#pragma unroll
+      for (uint32_t k = 0; k < 2; ++k)
+        if (lane + 32 * k < quads) {
+          const float4 x = *reinterpret_cast<const float4*>(from + (head * tile_rows + r) * dp + 4 * (lane + 32 * k));
+          v[k].x = v[k].x * was + x.x * is; v[k].y = v[k].y * was + x.y * is; v[k].z = v[k].z * was + x.z * is; v[k].w = v[k].w * was + x.w * is;
+        }
+    }
+#pragma unroll
+    for (uint32_t k = 0; k < 2; ++k) sums[warp][lane + 32 * k] = v[k];
+    if (lane == 0) top_sum[warp] = make_float2(top, total);
+    __syncthreads();
+    if (threadIdx.x < quads) {
+      top = -INFINITY; total = 0.f;
+      for (uint32_t w = 0; w < kJoinThreads / 32; ++w) top = fmaxf(top, top_sum[w].x);
+      const float base = top == -INFINITY ? 0.f : top;
+      float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (uint32_t w = 0; w < kJoinThreads / 32; ++w) {
+        const float f = exp2_fast(top_sum[w].x - base);
+        const float4 x = sums[w][threadIdx.x];
+        total = fmaf(top_sum[w].y, f, total);
+        y.x = fmaf(x.x, f, y.x); y.y = fmaf(x.y, f, y.y); y.z = fmaf(x.z, f, y.z); y.w = fmaf(x.w, f, y.w);
+      }
+      attend_store(a, h.row0, h.tile * tile_rows + r, group, (h.heads << hw_log) + head, 4 * threadIdx.x, y, top, total, vec_out);
+    }
+    __syncthreads();
+  }
+}
+
+constexpr int kDevices = 64;
+
+template <class F>
+cudaError_t launch_rows(const Launch& l, RowsArgs p, const AttendRun& run, uint64_t* launches) {
+  static bool allowed[kDevices] = {};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev >= kDevices || !allowed[dev]) {
+    e = cudaFuncSetAttribute(attend_rows_kernel<F>, cudaFuncAttributeMaxDynamicSharedMemorySize, F::SMEM);
+    if (e != cudaSuccess) return e;
+    if (dev < kDevices) allowed[dev] = true;
+  }
+  p.parts = reinterpret_cast<float*>(run.scratch);
+  p.pieces = reinterpret_cast<AttendPiece*>(run.scratch + run.parts_bytes);
+  e = launch_grid(l, attend_rows_kernel<F>, dim3(run.ctas), kThreads, F::SMEM, p);
+  if (e != cudaSuccess) return e;
+  ++*launches;
+  e = launch_grid(l, attend_join_kernel, dim3(run.ctas, kJoinRows), kJoinThreads, 0, p.a, p.group, p.parts, p.pieces, p.hw, p.hw_log, F::ROWS, (uint32_t)F::DP, p.vec_out);
   if (e == cudaSuccess) ++*launches;
   return e;
 }
 
+template <int FORMAT, int DP>
+cudaError_t launch_format(const Launch& l, const RowsArgs& p, const AttendRun& run, uint64_t* launches) {
+  if (run.terms == 2) {
+    if constexpr (DP <= 128) if (run.rows == 16) return launch_rows<Form<FORMAT, DP, 2, 2>>(l, p, run, launches);
+    return launch_rows<Form<FORMAT, DP, 1, 2>>(l, p, run, launches);
+  }
+  if constexpr (DP <= 128) if (run.rows == 16) return launch_rows<Form<FORMAT, DP, 2, 1>>(l, p, run, launches);
+  return launch_rows<Form<FORMAT, DP, 1, 1>>(l, p, run, launches);
+}
+
+template <int FORMAT>
+cudaError_t launch_dim(const Launch& l, const RowsArgs& p, const AttendRun& run, uint64_t* launches) {
+  if (run.dp == 64) return launch_format<FORMAT, 64>(l, p, run, launches);
+  if (run.dp == 128) return launch_format<FORMAT, 128>(l, p, run, launches);
+  return launch_format<FORMAT, 256>(l, p, run, launches);
+}
+
 }  // namespace
 
-cudaError_t launch_kv_attend(const Launch& l, const AttendArgs& a, uint64_t* launches) {
-  if (a.dtype == kF16) return attend_typed<__half>(l, a, launches);
-  if (a.dtype == kBF16) return attend_typed<__nv_bfloat16>(l, a, launches);
-  return attend_typed<float>(l, a, launches);
+// Which kernel form a call takes, and the scratch that it needs.
+AttendRun plan_kv_attend(const AttendArgs& a, int sm_count) {
+  AttendRun r = {};
+  r.dp = a.c.dim <= 64 ? 64 : a.c.dim <= 128 ? 128 : 256;
+  r.terms = a.dtype == kF32 ? 2 : 1;
+  const uint64_t most = (uint64_t)a.max_new * a.group;             // query rows of a sequence and key head
+  r.rows = r.dp <= 128 && most > 8 ? 16 : 8;
+  r.hw_log = 0;
+  while (r.hw_log < 3 && a.c.heads % (2u << r.hw_log) == 0) ++r.hw_log;
+  // Two CTAs per SM, fewer where there cannot be a unit of 16 tokens for each
+  const uint64_t tiles = (uint64_t)a.total * a.group / r.rows + a.seqs, units = tiles * (a.c.heads >> r.hw_log) * (a.room / 16 + 1);
+  const uint64_t ctas = 2 * (uint64_t)sm_count;
+  r.ctas = (uint32_t)(units < ctas ? units : ctas);
+  r.parts_bytes = (uint64_t)r.ctas * 2 * (1u << r.hw_log) * r.rows * (r.dp + 2) * sizeof(float);
+  r.scratch_bytes = r.parts_bytes + r.ctas * sizeof(AttendPiece);
+  return r;
+}
+
+cudaError_t launch_kv_attend(const Launch& l, const AttendArgs& a, const AttendRun& run, uint64_t* launches) {
+  RowsArgs p;
+  p.a = a; p.page = FastDiv(a.c.page_size); p.group = FastDiv(a.group);
+  p.hw = 1u << run.hw_log; p.hw_log = run.hw_log; p.row_limit = 0xffffffffu;
+  p.vec_codes = a.c.dim % 16 == 0 && ((uintptr_t)a.c.codes[0] | (uintptr_t)a.c.codes[1]) % 16 == 0;
+  p.vec_out = a.c.dim % 4 == 0 && (uintptr_t)a.out % (4 * dtype_size(a.dtype)) == 0;
+  return a.c.format == QV2_KV_MX4 ? launch_dim<QV2_KV_MX4>(l, p, run, launches) : launch_dim<QV2_KV_I8>(l, p, run, launches);
 }
 
 }  // namespace qv2

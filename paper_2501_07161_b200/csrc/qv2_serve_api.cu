@@ -1,6 +1,7 @@
 // C-ABI layer of page planning, norm with rotation, and attention over the cache.
 #include <cmath>
 
+#include "qv2_attend.cuh"
 #include "qv2_call.cuh"
 #include "qv2_serve.cuh"
 
@@ -100,10 +101,16 @@ extern "C" int qv2_kv_attend(qv2_ctx* c, const qv2_kv_cache* cache, const void* 
     a.c = view_of(cache);
     a.q = q; a.q_token_ld = q_token_ld; a.q_head_ld = q_head_ld; a.q_heads = q_heads; a.group = q_heads / cache->heads;
     a.total = (uint32_t)total; a.seqs = seqs; a.starts = q_starts; a.lens = lens; a.table = table; a.table_ld = table_ld;
-    a.scale = cfg->scale; a.cap = cfg->cap; a.window = cfg->window && cfg->window < (1ull << 62) ? (int64_t)cfg->window : (int64_t)1 << 62;
+    a.scale = cfg->scale; a.cap = cfg->cap; a.window = cfg->window && cfg->window < 0x7fffffffull ? (int32_t)cfg->window : 0x7fffffff;
     a.slopes = cfg->slopes; a.out = out; a.lse = lse; a.dtype = (uint32_t)dtype;
     a.max_new = cfg->max_new && cfg->max_new < total ? (uint32_t)cfg->max_new : (uint32_t)total;
-    QV2_CUDA(c, launch_kv_attend(launch_of(c), a, &c->launches));
+    a.room = cache->pages ? (uint32_t)(table_ld * cache->page_size) : 0;
+    AttendRun r = plan_kv_attend(a, c->sm_count);
+    cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+    QV2_CUDA(c, cudaStreamIsCapturing(c->stream, &capture));
+    if ((st = grow_capturable(c, &c->d_attend, &c->cap_attend, r.scratch_bytes, capture != cudaStreamCaptureStatusNone, &c->attend_captured)) != QV2_OK) return st;
+    r.scratch = c->d_attend;
+    QV2_CUDA(c, launch_kv_attend(launch_of(c), a, r, &c->launches));
     return QV2_OK;
   };
   return logged(c, "qv2_kv_attend", before, run());
