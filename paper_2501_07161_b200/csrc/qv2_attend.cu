@@ -23,7 +23,6 @@ constexpr int kWeightBits = 13;                            // weights stand 2^13
 constexpr int kFactorBits = 12;                            // 4 bits: block factors stand 2^12 above scale / (largest of the row)
 
 __device__ __forceinline__ uint32_t shared_at(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-__device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }     // -126..127
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
 }
@@ -39,29 +38,6 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
   return r;
 }
-__device__ __forceinline__ uint32_t pack_half(float lo, float hi) { const __half2 h = __floats2half2_rn(lo, hi); return *reinterpret_cast<const uint32_t*>(&h); }
-__device__ __forceinline__ uint32_t half_mul(uint32_t a, uint32_t b) {
-  const __half2 h = __hmul2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
-  return *reinterpret_cast<const uint32_t*>(&h);
-}
-// The four pairs of numbers of a word of 4-bit codes, as they lie.
-__device__ __forceinline__ void four_bits(uint32_t w, uint32_t (&h)[4]) {
-  asm("{\n\t.reg .b8 c0, c1, c2, c3;\n\t"
-      "mov.b32 {c0, c1, c2, c3}, %4;\n\t"
-      "cvt.rn.f16x2.e2m1x2 %0, c0;\n\t"
-      "cvt.rn.f16x2.e2m1x2 %1, c1;\n\t"
-      "cvt.rn.f16x2.e2m1x2 %2, c2;\n\t"
-      "cvt.rn.f16x2.e2m1x2 %3, c3;\n\t}"
-      : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(w));
-}
-// Bytes S and T of w, which are 8-bit integers plus 128, as a pair: 0x6400 + byte is the number 1024 + byte in binary16.
-template <uint32_t SELECT>
-__device__ __forceinline__ uint32_t eight_bits(uint32_t w) {
-  const uint32_t biased = __byte_perm(w, 0x64646464u, SELECT);
-  const __half2 h = __hsub2(*reinterpret_cast<const __half2*>(&biased), __half2half2(__ushort_as_half((unsigned short)0x6480)));
-  return *reinterpret_cast<const uint32_t*>(&h);
-}
-
 template <uint32_t N>
 __device__ __forceinline__ void load_words(uint32_t (&w)[N], const uint8_t* p) {
   if constexpr (N == 1) w[0] = *reinterpret_cast<const uint32_t*>(p);
@@ -69,13 +45,6 @@ __device__ __forceinline__ void load_words(uint32_t (&w)[N], const uint8_t* p) {
   else
 #pragma unroll
     for (uint32_t i = 0; i < N; i += 4) { const uint4 v = *reinterpret_cast<const uint4*>(p + 4 * i); w[i] = v.x; w[i + 1] = v.y; w[i + 2] = v.z; w[i + 3] = v.w; }
-}
-
-// cap * tanh(x / cap).  For results of 16 bits tanh(y) = 1 - 2 / (1 + e^2y), which is off by some 2^-23 of cap.
-template <int TERMS>
-__device__ __forceinline__ float capped(float x, float cap) {
-  if (TERMS == 2) return cap * tanhf(x / cap);
-  return cap - __fdividef(2.f * cap, 1.f + exp2_fast(2.f * kLog2e * __fdividef(x, cap)));
 }
 
 template <int FORMAT_, int DP_, int NT_, int TERMS_>
@@ -441,7 +410,7 @@ __global__ void __launch_bounds__(kThreads, F::RESIDENT) attend_rows_kernel(cons
             const uint32_t tok = 16 * l + g + 8 * (i >> 1);
             const int32_t at = (int32_t)(j_stage + tok), mine_pos = pos[n][i & 1];
             if (!plain) {
-              if (a.cap > 0.f) v = kLog2e * capped<TERMS>(v, a.cap);
+              if (a.cap > 0.f) v = kLog2e * (TERMS == 2 ? a.cap * tanhf(v / a.cap) : capped_fast(v, a.cap));
               v = fmaf(slope[n][i & 1], (float)(int32_t)((uint32_t)at - (uint32_t)mine_pos), v);
             }
             if (!every) {
@@ -668,6 +637,38 @@ attend_join_kernel(const AttendArgs a, FastDiv group, const float* parts, const 
   }
 }
 
+// The same where an item has many rows and few pieces: a warp adds up a row.
+__global__ void __launch_bounds__(kJoinThreads)
+attend_join_rows_kernel(const AttendArgs a, FastDiv group, const float* parts, const AttendPiece* pieces, uint32_t tile_rows, uint32_t dp, uint32_t vec_out) {
+  dependency_wait();
+  allow_dependents();
+  const AttendPiece h = pieces[blockIdx.x];
+  if (h.followers == 0) return;
+  const uint32_t lane = threadIdx.x % 32, quads = dp / 4, n_rows = min(tile_rows, h.rows - h.tile * tile_rows);
+  const uint64_t piece = (uint64_t)tile_rows * (dp + 2);
+  for (uint32_t r = blockIdx.y * (kJoinThreads / 32) + threadIdx.x / 32; r < n_rows; r += gridDim.y * (kJoinThreads / 32)) {
+    float top = -INFINITY, total = 0.f;
+    float4 v[2] = {};
+#pragma unroll 2
+    for (uint32_t f = 0; f <= h.followers; ++f) {
+      const float* from = parts + ((uint64_t)(blockIdx.x + f) * 2 + (f == 0 ? 1 : 0)) * piece;
+      const float2 ts = *reinterpret_cast<const float2*>(from + tile_rows * dp + 2 * r);
+      const float m = fmaxf(top, ts.x), base = m == -INFINITY ? 0.f : m, was = exp2_fast(top - base), is = exp2_fast(ts.x - base);
+      top = m;
+      total = total * was + ts.y * is;
+#pragma unroll
+      for (uint32_t k = 0; k < 2; ++k)
+        if (lane + 32 * k < quads) {
+          const float4 x = *reinterpret_cast<const float4*>(from + (uint64_t)r * dp + 4 * (lane + 32 * k));
+          v[k].x = v[k].x * was + x.x * is; v[k].y = v[k].y * was + x.y * is; v[k].z = v[k].z * was + x.z * is; v[k].w = v[k].w * was + x.w * is;
+        }
+    }
+#pragma unroll
+    for (uint32_t k = 0; k < 2; ++k)
+      if (lane + 32 * k < quads) attend_store(a, h.row0, h.tile * tile_rows + r, group, h.heads, 4 * (lane + 32 * k), v[k], top, total, vec_out);
+  }
+}
+
 constexpr int kDevices = 64;
 
 template <class F>
@@ -682,13 +683,11 @@ cudaError_t launch_rows(const Launch& l, RowsArgs p, const AttendRun& run, uint6
     if (dev < kDevices) allowed[dev] = true;
   }
   p.parts = reinterpret_cast<float*>(run.scratch);
-  p.pieces = reinterpret_cast<AttendPiece*>(run.scratch + run.parts_bytes);
+  p.pieces = reinterpret_cast<AttendPiece*>(run.scratch + attend_parts_bytes(run.ctas, p.hw, F::ROWS, F::DP));
   e = launch_grid(l, attend_rows_kernel<F>, dim3(run.ctas), kThreads, F::SMEM, p);
   if (e != cudaSuccess) return e;
   ++*launches;
-  e = launch_grid(l, attend_join_kernel, dim3(run.ctas, kJoinRows), kJoinThreads, 0, p.a, p.group, p.parts, p.pieces, p.hw, p.hw_log, F::ROWS, (uint32_t)F::DP, p.vec_out);
-  if (e == cudaSuccess) ++*launches;
-  return e;
+  return launch_attend_join(l, p.a, p.parts, p.pieces, run.ctas, p.hw_log, F::ROWS, F::DP, launches);
 }
 
 template <int FORMAT, int DP>
@@ -710,31 +709,52 @@ cudaError_t launch_dim(const Launch& l, const RowsArgs& p, const AttendRun& run,
 
 }  // namespace
 
-// Which kernel form a call takes, and the scratch that it needs.
+cudaError_t launch_attend_join(const Launch& l, const AttendArgs& a, const float* parts, const AttendPiece* pieces, uint32_t ctas, uint32_t hw_log, uint32_t tile_rows,
+                               uint32_t dp, uint64_t* launches) {
+  cudaError_t e = tile_rows >= 128 ? launch_grid(l, attend_join_rows_kernel, dim3(ctas, 8), kJoinThreads, 0, a, FastDiv(a.group), parts, pieces, tile_rows, dp, attend_vec_out(a))
+                                   : launch_grid(l, attend_join_kernel, dim3(ctas, kJoinRows), kJoinThreads, 0, a, FastDiv(a.group), parts, pieces, 1u << hw_log, hw_log,
+                                                 tile_rows, dp, attend_vec_out(a));
+  if (e == cudaSuccess) ++*launches;
+  return e;
+}
+
+// Which forms a call takes, and the scratch that it needs.
 AttendRun plan_kv_attend(const AttendArgs& a, int sm_count) {
   AttendRun r = {};
   r.dp = a.c.dim <= 64 ? 64 : a.c.dim <= 128 ? 128 : 256;
   r.terms = a.dtype == kF32 ? 2 : 1;
   const uint64_t most = (uint64_t)a.max_new * a.group;             // query rows of a sequence and key head
   r.rows = r.dp <= 128 && most > 8 ? 16 : 8;
+  // Sequences of more than 16 rows go to the tensor cores' tiles of 128 rows, which binary32 has no operands for.
+  r.few = r.terms == 2 || most <= 16 ? 0xffffffffu : a.seqs == 1 ? 0 : 16;
   r.hw_log = 0;
   while (r.hw_log < 3 && a.c.heads % (2u << r.hw_log) == 0) ++r.hw_log;
   // Two CTAs per SM, fewer where there cannot be a unit of 16 tokens for each
   const uint64_t tiles = (uint64_t)a.total * a.group / r.rows + a.seqs, units = tiles * (a.c.heads >> r.hw_log) * (a.room / 16 + 1);
   const uint64_t ctas = 2 * (uint64_t)sm_count;
   r.ctas = (uint32_t)(units < ctas ? units : ctas);
-  r.parts_bytes = (uint64_t)r.ctas * 2 * (1u << r.hw_log) * r.rows * (r.dp + 2) * sizeof(float);
-  r.scratch_bytes = r.parts_bytes + r.ctas * sizeof(AttendPiece);
+  uint64_t most_bytes = r.few == 0 ? 0 : attend_parts_bytes(r.ctas, 1u << r.hw_log, r.rows, r.dp) + r.ctas * sizeof(AttendPiece);
+  if (r.few != 0xffffffffu) {
+    const uint64_t many = ((uint64_t)a.total * a.group / chunk_rows(r.dp) + a.seqs) * a.c.heads * (a.room / 64 + 1);
+    r.chunk_ctas = (uint32_t)(many < (uint64_t)sm_count ? many : sm_count);
+    const uint64_t bytes = attend_parts_bytes(r.chunk_ctas, 1, chunk_rows(r.dp), r.dp) + r.chunk_ctas * sizeof(AttendPiece);
+    if (bytes > most_bytes) most_bytes = bytes;
+  }
+  r.scratch_bytes = most_bytes;
   return r;
 }
 
 cudaError_t launch_kv_attend(const Launch& l, const AttendArgs& a, const AttendRun& run, uint64_t* launches) {
-  RowsArgs p;
-  p.a = a; p.page = FastDiv(a.c.page_size); p.group = FastDiv(a.group);
-  p.hw = 1u << run.hw_log; p.hw_log = run.hw_log; p.row_limit = 0xffffffffu;
-  p.vec_codes = a.c.dim % 16 == 0 && ((uintptr_t)a.c.codes[0] | (uintptr_t)a.c.codes[1]) % 16 == 0;
-  p.vec_out = a.c.dim % 4 == 0 && (uintptr_t)a.out % (4 * dtype_size(a.dtype)) == 0;
-  return a.c.format == QV2_KV_MX4 ? launch_dim<QV2_KV_MX4>(l, p, run, launches) : launch_dim<QV2_KV_I8>(l, p, run, launches);
+  if (run.few != 0) {
+    RowsArgs p;
+    p.a = a; p.page = FastDiv(a.c.page_size); p.group = FastDiv(a.group);
+    p.hw = 1u << run.hw_log; p.hw_log = run.hw_log; p.row_limit = run.few;
+    p.vec_codes = a.c.dim % 16 == 0 && ((uintptr_t)a.c.codes[0] | (uintptr_t)a.c.codes[1]) % 16 == 0;
+    p.vec_out = attend_vec_out(a);
+    cudaError_t e = a.c.format == QV2_KV_MX4 ? launch_dim<QV2_KV_MX4>(l, p, run, launches) : launch_dim<QV2_KV_I8>(l, p, run, launches);
+    if (e != cudaSuccess || run.few == 0xffffffffu) return e;
+  }
+  return launch_attend_chunk(l, a, run, launches);
 }
 
 }  // namespace qv2

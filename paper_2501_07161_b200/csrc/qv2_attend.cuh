@@ -59,6 +59,35 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 __device__ __forceinline__ float exp2_fast(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 
+__device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }     // -126..127
+__device__ __forceinline__ uint32_t pack_half(float lo, float hi) { const __half2 h = __floats2half2_rn(lo, hi); return *reinterpret_cast<const uint32_t*>(&h); }
+__device__ __forceinline__ uint32_t half_mul(uint32_t a, uint32_t b) {
+  const __half2 h = __hmul2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+// The four pairs of numbers of a word of 4-bit codes, as they lie.
+__device__ __forceinline__ void four_bits(uint32_t w, uint32_t (&h)[4]) {
+  asm("{\n\t.reg .b8 c0, c1, c2, c3;\n\t"
+      "mov.b32 {c0, c1, c2, c3}, %4;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %0, c0;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %1, c1;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %2, c2;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %3, c3;\n\t}"
+      : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(w));
+}
+// Bytes S and T of w, which are 8-bit integers plus 128, as a pair: 0x6400 + byte is the number 1024 + byte in binary16.
+template <uint32_t SELECT>
+__device__ __forceinline__ uint32_t eight_bits(uint32_t w) {
+  const uint32_t biased = __byte_perm(w, 0x64646464u, SELECT);
+  const __half2 h = __hsub2(*reinterpret_cast<const __half2*>(&biased), __half2half2(__ushort_as_half((unsigned short)0x6480)));
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// cap * tanh(x / cap) for results of 16 bits: tanh(y) = 1 - 2 / (1 + e^2y), off by some 2^-23 of cap.
+__device__ __forceinline__ float capped_fast(float x, float cap) {
+  return cap - __fdividef(2.f * cap, 1.f + exp2_fast(2.f * kLog2e * __fdividef(x, cap)));
+}
+
 // Elements d .. d + 3 of the result of query row r (of a sequence and key head), from sums of which the largest score, to powers of two, is `top`.
 __device__ __forceinline__ void attend_store(const AttendArgs& a, uint32_t q_row0, uint32_t r, const FastDiv& group, uint32_t kv, uint32_t d, float4 v,
                                              float top, float total, bool vec) {
@@ -87,11 +116,21 @@ __device__ __forceinline__ void attend_store(const AttendArgs& a, uint32_t q_row
 
 // The form of a call, and its scratch: partial results, then an AttendPiece per CTA.
 struct AttendRun {
-  uint32_t dp, terms, rows, hw_log, ctas;
-  uint64_t parts_bytes, scratch_bytes;
+  uint32_t dp, terms, rows, hw_log, ctas;      // the form for few rows
+  uint32_t few;                                // sequences of more query rows (per key head) take the other form; 2^32 - 1: none does, 0: all do
+  uint32_t chunk_ctas;
+  uint64_t scratch_bytes;
   uint8_t* scratch;
+  uint32_t* fault;                             // host-mapped word, set when a kernel gave up waiting
 };
 AttendRun plan_kv_attend(const AttendArgs& a, int sm_count);
+constexpr uint32_t chunk_rows(uint32_t dp) { return dp == 256 ? 128 : 256; }      // query rows of an item of the form for many
+cudaError_t launch_attend_chunk(const Launch& l, const AttendArgs& a, const AttendRun& run, uint64_t* launches);
+// Adds up what was cut: parts as a form left them, hw key heads (a power of two) and tile_rows query rows to an item.
+cudaError_t launch_attend_join(const Launch& l, const AttendArgs& a, const float* parts, const AttendPiece* pieces, uint32_t ctas, uint32_t hw_log, uint32_t tile_rows,
+                               uint32_t dp, uint64_t* launches);
+inline uint32_t attend_vec_out(const AttendArgs& a) { return a.c.dim % 4 == 0 && (uintptr_t)a.out % (4 * dtype_size(a.dtype)) == 0; }
+inline uint64_t attend_parts_bytes(uint32_t ctas, uint32_t hw, uint32_t tile_rows, uint32_t dp) { return (uint64_t)ctas * 2 * hw * tile_rows * (dp + 2) * sizeof(float); }
 cudaError_t launch_kv_attend(const Launch& l, const AttendArgs& a, const AttendRun& run, uint64_t* launches);
 
 }  // namespace qv2

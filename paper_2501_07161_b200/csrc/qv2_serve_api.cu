@@ -109,7 +109,7 @@ extern "C" int qv2_kv_attend(qv2_ctx* c, const qv2_kv_cache* cache, const void* 
     cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
     QV2_CUDA(c, cudaStreamIsCapturing(c->stream, &capture));
     if ((st = grow_capturable(c, &c->d_attend, &c->cap_attend, r.scratch_bytes, capture != cudaStreamCaptureStatusNone, &c->attend_captured)) != QV2_OK) return st;
-    r.scratch = c->d_attend;
+    r.scratch = c->d_attend; r.fault = c->d_fault;
     QV2_CUDA(c, launch_kv_attend(launch_of(c), a, r, &c->launches));
     return QV2_OK;
   };
