@@ -8,10 +8,12 @@
 // While one tile's softmax runs the tensor cores are at the other tile's products.  Bound by the exponentials (16 a cycle and SM: 2048
 // cycles for 2 x 128 x 128 scores) next to the products (2 x 2 x 512 cycles for 128 elements).
 //
-// Codes are exact in binary16: 8-bit integers as they are, 4-bit codes times a power of two that says how far their block's scale is below
-// the row's largest.  What is left is one number per token: keys' multiply their column of scores, values' their weights, held
-// against the largest so far (its exponent is the CTA's; results are brought along when it grows).  The
-// reference of a row's softmax follows its maximum only when that has doubled its largest weight, so results are seldom rescaled.
+// Codes are exact in binary16.  At 4 bits they are multiplied by their block's scale over the largest of the tile (keys) or of the item so far
+// (values), a power of two: exact unless a scale is 2^36 below that.  8-bit integers enter as they are, and what is left is one number per
+// token: keys' multiply their column of scores, values' their weights, held against the largest so far.  When that grows,
+// results are brought along.  The reference of a row's softmax follows its maximum only when the largest weight has grown
+// 2^kSlack-fold, so results are seldom rescaled.  A poisoned key is a NaN among the operands; a poisoned value must not be (it would
+// reach the rows that do not see it, too): it is left out there and enters through the weights of those that do.
 #include "qv2_attend.cuh"
 #include "qv2_tensor.cuh"
 
@@ -20,9 +22,9 @@ namespace qv2 {
 namespace {
 
 constexpr uint32_t kChunkThreads = 13 * 32;
-constexpr int kChunkBits = 13;              // weights stand 2^13 above p * scale / (largest scale): at most 2^15, p being at most 2
-constexpr int kChunkFactor = 13;            // 4 bits: numbers stand 2^13 above code * scale / (largest of the row): 6 * 2^13 at most
-constexpr float kSlack = 1.f;               // the reference of a row's softmax follows its maximum when that is above it by more (a power of two)
+constexpr int kChunkFactor = 13;            // 4 bits: operands stand 2^13 above code * scale / (largest scale): 6 * 2^13 at most
+constexpr float kSlack = 4.f;               // a row's largest weight is 2^kSlack at most ...
+constexpr int kWeightBits = 10;             // ... and weights stand 2^10 above that: at most 2^15 (8 bits: times up to 2), and what binary16 loses below 2^-35
 
 __device__ __forceinline__ void bar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
 __device__ __forceinline__ void tensor_commit(uint32_t bar) {
@@ -60,6 +62,18 @@ __device__ __forceinline__ void tensor_write16(uint32_t at, const uint32_t (&v)[
                  "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(at) : "memory");
 }
 __device__ __forceinline__ void tensor_write_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// Two at a time.
+__device__ __forceinline__ void mul2(float& x, float& y, float a, float b) {
+  asm("{\n\t.reg .b64 p, q;\n\tmov.b64 p, {%0, %1};\n\tmov.b64 q, {%2, %3};\n\tmul.rn.f32x2 p, p, q;\n\tmov.b64 {%0, %1}, p;\n\t}" : "+f"(x), "+f"(y) : "f"(a), "f"(b));
+}
+__device__ __forceinline__ void add2(float& x, float& y, float a, float b) {
+  asm("{\n\t.reg .b64 p, q;\n\tmov.b64 p, {%0, %1};\n\tmov.b64 q, {%2, %3};\n\tadd.rn.f32x2 p, p, q;\n\tmov.b64 {%0, %1}, p;\n\t}" : "+f"(x), "+f"(y) : "f"(a), "f"(b));
+}
+__device__ __forceinline__ void fma2(float& x, float& y, float f, float c) {
+  asm("{\n\t.reg .b64 p, q, r;\n\tmov.b64 p, {%0, %1};\n\tmov.b64 q, {%2, %2};\n\tmov.b64 r, {%3, %3};\n\tfma.rn.f32x2 p, p, q, r;\n\tmov.b64 {%0, %1}, p;\n\t}"
+      : "+f"(x), "+f"(y) : "f"(f), "f"(c));
+}
+__device__ __forceinline__ float max3(float a, float b, float c) { float r; asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c)); return r; }
 // Whether all 128 threads of the four converting warps say yes.
 __device__ __forceinline__ bool all_converting(bool ok) {
   uint32_t r;
@@ -77,9 +91,10 @@ __device__ __forceinline__ uint64_t columns_desc(uint32_t addr, uint32_t panel) 
   return (uint64_t)((addr & 0x3ffffu) >> 4) | ((uint64_t)(panel >> 4) << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
 }
 
-template <int FORMAT_, int DP_>
+template <int FORMAT_, int DP_, bool PLAIN_>
 struct Chunk {
   static constexpr int FORMAT = FORMAT_, DP = DP_;
+  static constexpr bool PLAIN = PLAIN_;                               // no cap, no slopes
   static constexpr bool MX = FORMAT == QV2_KV_MX4;
   static constexpr uint32_t QT = DP == 256 ? 1 : 2;                   // query tiles
   static constexpr uint32_t ROWS = 128 * QT;
@@ -88,7 +103,7 @@ struct Chunk {
   static constexpr uint32_t Q_PANEL = 128 * 128, Q_TILE = Q_PANEL * (DP / 64);
   static constexpr uint32_t PANEL = KT * 128, KV_TILE = PANEL * (DP / 64);
   static constexpr uint32_t STAGES = 2;
-  static constexpr uint32_t META = 2 * 4 * KT + 16 + 16;              // scales of keys, of values, which tokens there are, the exponent of the values' scales
+  static constexpr uint32_t META = 2 * 4 * KT + 16 + 16 + 16;         // 8 bits: scales of keys, of values; which tokens there are; whose value is poisoned; largest exponents
   static constexpr uint32_t SMEM = 1024 + QT * Q_TILE + STAGES * (2 * KV_TILE + META) + 256;
   static constexpr uint32_t O_COL = QT * KT;                          // tensor memory: scores of the tiles, then their results
   static_assert(O_COL + QT * DP <= 512, "tensor memory");
@@ -105,7 +120,7 @@ struct ChunkArgs {
   AttendArgs a;
   FastDiv page, group;
   uint32_t few;                             // sequences of as many rows or fewer are the other kernel's
-  uint32_t vec_codes, vec_out;
+  uint32_t vec_q, vec_codes, vec_out;       // 16-byte loads of queries and of codes, stores of eight results
   float* parts;
   AttendPiece* pieces;
   uint32_t* fault;
@@ -172,7 +187,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
   __shared__ struct { uint64_t before; uint32_t seq; } found;
   __shared__ uint64_t bars[17];
   __shared__ uint32_t tmem_slot, failed_flag;
-  __shared__ int32_t highest[2][4];
+  __shared__ int32_t highest[2][2][4];
   const AttendArgs& a = p.a;
   const uint32_t tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
   uint8_t* const base = raw + ((1024u - (smem_addr(raw) & 1023u)) & 1023u);
@@ -266,168 +281,126 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
     at.enter(p);
   }
 
-  if (warp < 4 * QT) {
+  if (warp < 8) {
     // ---------------------------------------------------------------------------------- softmax
     const uint32_t t = warp / 4, lanes = ((warp % 4) * 32) << 16, r_in = 128 * t + (warp % 4) * 32 + lane;
     const uint32_t s_at = tmem + t * KT + lanes, o_at = tmem + F::O_COL + t * DP + lanes;
-    uint32_t turn = 0;                                       // tiles done: phases of s_full, o_done; stage of the metadata
-    const bool plain = !(a.cap > 0.f) && !a.slopes;
-    uint32_t tiles_before = 0;                               // tiles of all items so far, with or without this warp's query tile
-    do {
-      const uint32_t n_units = at.unit1 - at.unit;
-      const bool takes_part = t == 0 || at.t.row1 - at.t.row0 > 128;
-      if (takes_part) {
-        // the row: brought to the top of binary16's range by a power of two, signed like the scale
-        const uint32_t r = at.t.row0 + r_in, i = p.group.div(min(r, at.t.row1 - 1)), head = at.kv * p.group.d + (min(r, at.t.row1 - 1) - i * p.group.d);
-        const bool there = r < at.t.row1;
-        const int32_t pos = at.t.pos0 + (int32_t)i;
-        const int32_t pos_first = __shfl_sync(0xffffffffu, pos, 0), pos_last = __shfl_sync(0xffffffffu, pos, 31);
-        const uint64_t from = (uint64_t)(at.s.row0 + i) * a.q_token_ld + (uint64_t)head * a.q_head_ld;
+    uint32_t turn = 0;                                       // tiles that this query tile took part in: phases of s_full, o_done
+    uint32_t tiles_before = 0;                               // all tiles so far: stage of the metadata
+    // What a thread knows about its row of an item.
+    struct Row {
+      int32_t pos, pos_first, pos_last;                      // of the row, and of the first and last one of the warp
+      uint32_t out_row, head;                                // row of the results, query head
+      float back, slope;                                     // what the scores are multiplied by (to powers of two unless they are capped)
+      bool there, part;                                      // the row exists; the tile takes part in the item
+    } row = {}, ahead = {};
+    Walk<F> to = at;
+    bool more = true, ok = t < QT;
+    float ref = -INFINITY, sum = 0.f;
+    int v_top = -126;
+#pragma unroll 1
+    for (bool begin = true; ok; begin = false) {
+      if (!begin) { to = at; more = to.next(p); }
+      ahead.part = more && (t == 0 || to.t.row1 - to.t.row0 > 128);
+      if (ahead.part) {
+        // the next item's row, brought to the top of binary16's range by a power of two, signed like the scale.  (The products with the
+        // last item's rows are done: their scores have been read.)
+        const uint32_t r = to.t.row0 + r_in, rc = min(r, to.t.row1 - 1), i = p.group.div(rc), in_group = rc - i * p.group.d;
+        ahead.head = to.kv * p.group.d + in_group;
+        ahead.there = r < to.t.row1;
+        ahead.out_row = to.s.row0 + i;
+        ahead.pos = to.t.pos0 + (int32_t)i;
+        ahead.pos_first = __shfl_sync(0xffffffffu, ahead.pos, 0);
+        ahead.pos_last = __shfl_sync(0xffffffffu, ahead.pos, 31);
+        const uint64_t from = (uint64_t)ahead.out_row * a.q_token_ld + (uint64_t)ahead.head * a.q_head_ld;
         uint32_t top = 0;
-        auto each = [&](auto zero, const auto* q, auto&& use) {
-#pragma unroll 1
-          for (uint32_t d = 0; d < DP; d += 8) {
-            auto e = zero;
-            e.zero();
-            if (there && d + 8 <= a.c.dim) e.load_any(q + from + d);
-            else if (there && d < a.c.dim) e.load_some(q + from + d, a.c.dim - d);
-            use(e, d);
-          }
-        };
-        auto most = [&](auto& e, uint32_t) { top = max(top, e.top_bits()); };
-        if (a.dtype == kBF16) each(Chunk8<__nv_bfloat16>(), (const __nv_bfloat16*)a.q, most);
-        else each(Chunk8<__half>(), (const __half*)a.q, most);
-        const int e = top ? max((int)(top >> 23) - 127, -100) : 0;
-        const float up = copysignf(power_of_two(14 - min(e, 127)), a.scale);
-        auto put = [&](auto& c, uint32_t d) {
-          float v[8];
-          c.widen(v);
-          uint32_t h[4];
+        int e = 0;
+        // (rows that are not there take another's elements, times zero)
+        auto bring = [&](auto zero, const auto* q) {
+          constexpr uint32_t HELD = DP == 64 ? 8 : 16;                 // groups of 8 elements in flight
+          decltype(zero) c[HELD];
+          auto load = [&](uint32_t d0) {
+            if (p.vec_q) {
 #pragma unroll
-          for (int k = 0; k < 4; ++k) h[k] = pack_half(v[2 * k] * up, v[2 * k + 1] * up);
-          const uint32_t row = r_in % 128, to = q_at + t * F::Q_TILE + (d / 64) * F::Q_PANEL + row * 128 + (((d / 8) ^ row) & 7) * 16;
-          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(h[0]), "r"(h[1]), "r"(h[2]), "r"(h[3]) : "memory");
-        };
-        if (a.dtype == kBF16) each(Chunk8<__nv_bfloat16>(), (const __nv_bfloat16*)a.q, put);
-        else each(Chunk8<__half>(), (const __half*)a.q, put);
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        __syncwarp();
-        if (lane == 0) bar_arrive(q_full(t));
-        const float back = top >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : power_of_two(min(e, 127) - 14) * power_of_two(MX ? -kChunkFactor : 0) * fabsf(a.scale) * (a.cap > 0.f ? 1.f : kLog2e);
-        const float slope = a.slopes ? kLog2e * __ldg(a.slopes + head) : 0.f;
-
-        float ref = -INFINITY, sum = 0.f;
-        int v_top = -126;
-        bool ok = true;
-#pragma unroll 1
-        for (uint32_t u = 0; u < n_units; ++u, ++turn) {
-          const uint32_t stage = (tiles_before + u) % F::STAGES;
-          const uint8_t* const m = meta + stage * F::META;
-          const float4* const k_scale = reinterpret_cast<const float4*>(m);
-          const float4* const v_scale = reinterpret_cast<const float4*>(m + 4 * KT);
-          const uint32_t* const real = reinterpret_cast<const uint32_t*>(m + 8 * KT);
-          if (!bar_wait(s_full(t), turn & 1, failed)) { ok = false; break; }
-          tc_fence_after();
-          const int v_now = *reinterpret_cast<const int32_t*>(m + 8 * KT + 16);
-          const uint32_t j = at.t.j0 + (at.unit + u) * KT;
-          bool every = (int32_t)(j + KT - 1) <= pos_first && pos_last - (int32_t)j < a.window;
+              for (uint32_t k = 0; k < HELD; ++k) c[k].load_vec(q + from + min(d0 + 8 * k, a.c.dim - 8));
+            } else {
 #pragma unroll
-          for (uint32_t k = 0; k < KT / 32; ++k) every &= real[k] == 0xffffffffu;
-
-          // scores, to powers of two: the largest
-          auto scores = [&](uint32_t c, float (&x)[32]) {
-            tensor_read(s_at + 32 * c, x);
-#pragma unroll
-            for (uint32_t k = 0; k < 8; ++k) {
-              const float4 f = k_scale[8 * c + k];
-              x[4 * k] *= f.x; x[4 * k + 1] *= f.y; x[4 * k + 2] *= f.z; x[4 * k + 3] *= f.w;
-            }
-            if (!plain) {
-#pragma unroll
-              for (uint32_t k = 0; k < 32; ++k) {
-                float v = x[k] * back;
-                if (a.cap > 0.f) v = kLog2e * capped_fast(v, a.cap);
-                x[k] = fmaf(slope, (float)(int32_t)(j + 32 * c + k - (uint32_t)pos), v);
-              }
-            }
-            if (!every) {
-              const uint32_t there_bits = real[c];
-#pragma unroll
-              for (uint32_t k = 0; k < 32; ++k) {
-                const int32_t tok = (int32_t)(j + 32 * c + k);
-                if (!((there_bits >> k & 1u) && tok <= pos && (uint32_t)pos - (uint32_t)tok < (uint32_t)a.window)) x[k] = -INFINITY;
+              for (uint32_t k = 0; k < HELD; ++k) {
+                const uint32_t d = d0 + 8 * k;
+                c[k].zero();
+                if (d + 8 <= a.c.dim) c[k].load_any(q + from + d);
+                else if (d < a.c.dim) c[k].load_some(q + from + d, a.c.dim - d);
               }
             }
           };
-          const float mul = !plain ? 1.f : back < 1.2e-38f ? 1.2e-38f : back;      // not 0: it multiplies minus infinity, too
-          float x[32], high = -INFINITY;
 #pragma unroll 1
-          for (uint32_t c = 0; c < KT / 32; ++c) {
-            scores(c, x);
+          for (uint32_t d0 = 0; d0 < DP; d0 += 8 * HELD) {
+            load(d0);
 #pragma unroll
-            for (uint32_t k = 0; k < 32; ++k) high = fmaxf(high, x[k]);
+            for (uint32_t k = 0; k < HELD; ++k) top = max(top, c[k].top_bits());
           }
-          high = high == -INFINITY ? high : high * mul;      // (NaN from a poisoned query: its scores are NaN below)
-          float soft = 1.f, values = 1.f;
-          if (high > ref + kSlack) { soft = exp2_fast(ref - high); ref = high; }
-          if (v_now != v_top) { values = power_of_two(max(v_top - v_now, -126)); v_top = v_now; }
-          sum *= soft;
-          if (u > 0 && __any_sync(0xffffffffu, soft * values != 1.f)) {
-            if (!bar_wait(o_done(t), (turn - 1) & 1, failed)) { ok = false; break; }
-            tc_fence_after();
+          e = top ? max((int)(top >> 23) - 127, -100) : 0;
+          const float up = ahead.there ? copysignf(power_of_two(14 - min(e, 127)), a.scale) : 0.f;
 #pragma unroll 1
-            for (uint32_t c = 0; c < DP / 32; ++c) {
-              float o[32];
-              tensor_read(o_at + 32 * c, o);
+          for (uint32_t d0 = 0; d0 < DP; d0 += 8 * HELD) {
+            if (DP > 8 * HELD) load(d0);
 #pragma unroll
-              for (uint32_t k = 0; k < 32; ++k) o[k] *= soft * values;
-              tensor_write(o_at + 32 * c, o);
+            for (uint32_t k = 0; k < HELD; ++k) {
+              const uint32_t d = d0 + 8 * k, in = r_in % 128, where = q_at + t * F::Q_TILE + (d / 64) * F::Q_PANEL + in * 128 + (((d / 8) ^ in) & 7) * 16;
+              const float f = d < a.c.dim ? up : 0.f;
+              float v[8];
+              c[k].widen(v);
+              uint32_t h[4];
+#pragma unroll
+              for (int i2 = 0; i2 < 4; ++i2) h[i2] = pack_half(v[2 * i2] * f, v[2 * i2 + 1] * f);
+              asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(where), "r"(h[0]), "r"(h[1]), "r"(h[2]), "r"(h[3]) : "memory");
             }
           }
-          const float from_ref = ref == -INFINITY ? 0.f : ref;
-#pragma unroll 1
-          for (uint32_t c = 0; c < KT / 32; ++c) {
-            scores(c, x);
-            uint32_t h[16];
-#pragma unroll
-            for (uint32_t k = 0; k < 8; ++k) {
-              const float4 f = v_scale[8 * c + k];
-              float w[4] = {f.x, f.y, f.z, f.w};
-#pragma unroll
-              for (uint32_t i2 = 0; i2 < 4; ++i2) {
-                const float e2 = exp2_fast(fmaf(x[4 * k + i2], mul, -from_ref));
-                sum += e2;
-                w[i2] = every || x[4 * k + i2] != -INFINITY ? e2 * w[i2] : 0.f;
-              }
-              h[2 * k] = pack_half(w[0], w[1]);
-              h[2 * k + 1] = pack_half(w[2], w[3]);
-            }
-            tensor_write16(s_at + 16 * c, h);
-          }
-          tensor_write_wait();
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) bar_arrive(p_full(t));
-        }
-        if (!ok) break;
-        // ---- the rows' results
+        };
+        if (a.dtype == kBF16) bring(Chunk8<__nv_bfloat16>(), (const __nv_bfloat16*)a.q);
+        else bring(Chunk8<__half>(), (const __half*)a.q);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) bar_arrive(q_full(t));
+        ahead.back = top >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : power_of_two(min(e, 127) - 14) * power_of_two(MX ? -kChunkFactor : 0) * fabsf(a.scale) * (!F::PLAIN && a.cap > 0.f ? 1.f : kLog2e);
+        ahead.slope = !F::PLAIN && a.slopes ? kLog2e * __ldg(a.slopes + ahead.head) : 0.f;
+      }
+      if (!begin && row.part) {
+        // ---- results of the item that is done
         if (!bar_wait(o_done(t), (turn - 1) & 1, failed)) break;
         tc_fence_after();
         const bool whole = at.unit == 0 && at.unit1 == at.t.units;
         const uint32_t place = at.unit == 0 ? 1 : 0;
         float* const part = p.parts + ((uint64_t)blockIdx.x * 2 + place) * F::ROWS * (DP + 2);
-        const float f0 = power_of_two(-kChunkBits - (MX ? kChunkFactor : 0)), f1 = power_of_two(v_top);
-        if (!whole && there) *reinterpret_cast<float2*>(part + F::ROWS * DP + 2 * r_in) = make_float2(ref, sum);
+        sum *= power_of_two(-kWeightBits);
+        const float f0 = power_of_two(-kWeightBits - (MX ? kChunkFactor : 0)) * (!whole ? 1.f : sum == 0.f ? 0.f : 1.f / sum), f1 = power_of_two(v_top);
+        const uint64_t out_at = (uint64_t)row.out_row * a.q_heads + row.head;
+        if (!whole && row.there) *reinterpret_cast<float2*>(part + F::ROWS * DP + 2 * r_in) = make_float2(ref, sum);
+        if (whole && row.there && a.lse) a.lse[out_at] = sum == 0.f ? -INFINITY : (ref + log2f(sum)) * kLn2;
 #pragma unroll 1
         for (uint32_t c = 0; c < DP / 32; ++c) {
           float o[32];
           tensor_read(o_at + 32 * c, o);
-          if (!there) continue;
+          if (!row.there) continue;
 #pragma unroll
-          for (uint32_t k = 0; k < 8; ++k) {
-            const float4 v = make_float4(o[4 * k] * f0 * f1, o[4 * k + 1] * f0 * f1, o[4 * k + 2] * f0 * f1, o[4 * k + 3] * f0 * f1);
-            if (whole) attend_store(a, at.s.row0, r, p.group, at.kv, 32 * c + 4 * k, v, ref, sum, p.vec_out);
-            else *reinterpret_cast<float4*>(part + r_in * DP + 32 * c + 4 * k) = v;
+          for (uint32_t k = 0; k < 32; ++k) o[k] = o[k] * f0 * f1;
+          if (!whole) {
+#pragma unroll
+            for (uint32_t k = 0; k < 32; k += 4) *reinterpret_cast<float4*>(part + r_in * DP + 32 * c + k) = make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
+          } else {
+            auto store = [&](auto* out) {
+              using T = typename std::remove_pointer<decltype(out)>::type;
+#pragma unroll
+              for (uint32_t k = 0; k < 32; k += 8) {
+                const float v[8] = {o[k], o[k + 1], o[k + 2], o[k + 3], o[k + 4], o[k + 5], o[k + 6], o[k + 7]};
+                const uint32_t d = 32 * c + k;
+                T* const where = out + out_at * a.c.dim + d;
+                if (p.vec_out) { if (d < a.c.dim) Chunk8<T>::store_vec(where, v); }
+                else if (d < a.c.dim) store_some(where, v, a.c.dim - d);
+              }
+            };
+            if (a.dtype == kBF16) store((__nv_bfloat16*)a.out);
+            else store((__half*)a.out);
           }
         }
         if (!whole && place == 1 && tid == 0) {
@@ -442,9 +415,140 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
         tc_fence_before();
         __syncwarp();
       }
+      if (!more) break;
+      at = to;
+      row = ahead;
+      const uint32_t n_units = at.unit1 - at.unit;
+      if (row.part) {
+        ref = -INFINITY; sum = 0.f; v_top = -126;
+#pragma unroll 1
+        for (uint32_t u = 0; u < n_units; ++u, ++turn) {
+          const uint8_t* const m = meta + (tiles_before + u) % F::STAGES * F::META;
+          const float4* const k_scale = reinterpret_cast<const float4*>(m);
+          const float4* const v_scale = reinterpret_cast<const float4*>(m + 4 * KT);
+          const uint32_t* const real = reinterpret_cast<const uint32_t*>(m + 8 * KT);
+          const uint32_t* const bad = real + 4;
+          const uint32_t j = at.t.j0 + (at.unit + u) * KT;
+          if (!bar_wait(s_full(t), turn & 1, failed)) { ok = false; break; }
+          tc_fence_after();
+          const int2 tops = *reinterpret_cast<const int2*>(m + 8 * KT + 32);         // exponents of the tile's keys (4 bits), of the values so far
+          bool every = (int32_t)(j + KT - 1) <= row.pos_first && row.pos_last - (int32_t)j < a.window;
+#pragma unroll
+          for (uint32_t k = 0; k < KT / 32; ++k) every &= real[k] == 0xffffffffu;
+          bool poisoned = false;
+#pragma unroll
+          for (uint32_t k = 0; k < KT / 32; ++k) poisoned |= MX && bad[k] != 0;
+          // what turns a score of the product into one to powers of two; not 0, since it multiplies minus infinity, too
+          const float unit = MX ? row.back * power_of_two(tops.x) : row.back, mul = !F::PLAIN ? 1.f : unit < 1.2e-38f ? 1.2e-38f : unit;
+          // scores of 32 tokens, up to mul
+          auto scores = [&](uint32_t c, float (&x)[32]) {
+            tensor_read(s_at + 32 * c, x);
+            if (!MX) {
+#pragma unroll
+              for (uint32_t k = 0; k < 8; ++k) {
+                const float4 f = k_scale[8 * c + k];
+                mul2(x[4 * k], x[4 * k + 1], f.x, f.y);
+                mul2(x[4 * k + 2], x[4 * k + 3], f.z, f.w);
+              }
+            }
+            if (!F::PLAIN) {
+#pragma unroll
+              for (uint32_t k = 0; k < 32; ++k) {
+                float v = x[k] * unit;
+                if (a.cap > 0.f) v = kLog2e * capped_fast(v, a.cap);
+                x[k] = fmaf(row.slope, (float)(int32_t)(j + 32 * c + k - (uint32_t)row.pos), v);
+              }
+            }
+            if (!every) {
+              const uint32_t bits = real[c];
+#pragma unroll
+              for (uint32_t k = 0; k < 32; ++k) {
+                const int32_t tok = (int32_t)(j + 32 * c + k);
+                if (!((bits >> k & 1u) && tok <= row.pos && (uint32_t)row.pos - (uint32_t)tok < (uint32_t)a.window)) x[k] = -INFINITY;
+              }
+            }
+          };
+          float x[32], high = -INFINITY;
+#pragma unroll 1
+          for (uint32_t c = 0; c < KT / 32; ++c) {
+            scores(c, x);
+            float h4[4] = {x[0], x[1], x[2], x[3]};
+#pragma unroll
+            for (uint32_t k = 4; k < 28; k += 8)
+#pragma unroll
+              for (uint32_t i = 0; i < 4; ++i) h4[i] = max3(h4[i], x[k + i], x[k + 4 + i]);
+#pragma unroll
+            for (uint32_t i = 0; i < 4; ++i) h4[i] = fmaxf(h4[i], x[28 + i]);
+            high = max3(high, fmaxf(h4[0], h4[1]), fmaxf(h4[2], h4[3]));
+          }
+          high = high == -INFINITY ? high : high * mul;      // (NaN from a poisoned query: its weights are NaN below)
+          float soft = 1.f, values = 1.f;
+          if (high > ref + kSlack) { soft = exp2_fast(ref - high); ref = high; }
+          if (tops.y != v_top) { values = power_of_two(max(v_top - tops.y, -126)); v_top = tops.y; }
+          sum *= soft;
+          if (u > 0 && __any_sync(0xffffffffu, soft * values != 1.f)) {
+            if (!bar_wait(o_done(t), (turn - 1) & 1, failed)) { ok = false; break; }
+            tc_fence_after();
+            const float f = soft * values;
+#pragma unroll 1
+            for (uint32_t c = 0; c < DP / 32; ++c) {
+              tensor_read(o_at + 32 * c, x);
+#pragma unroll
+              for (uint32_t k = 0; k < 32; ++k) x[k] *= f;
+              tensor_write(o_at + 32 * c, x);
+            }
+          }
+          const float less = (float)kWeightBits - (ref == -INFINITY ? 0.f : ref);
+          float sums[2] = {0.f, 0.f};
+#pragma unroll 1
+          for (uint32_t c = 0; c < KT / 32; ++c) {
+            scores(c, x);
+            uint32_t seen = 0xffffffffu;
+            if (!every) {
+#pragma unroll
+              for (uint32_t k = 0; k < 32; ++k)
+                if (x[k] == -INFINITY) seen &= ~(1u << k);
+            }
+#pragma unroll
+            for (uint32_t k = 0; k < 32; k += 2) fma2(x[k], x[k + 1], mul, less);
+#pragma unroll
+            for (uint32_t k = 0; k < 32; ++k) x[k] = exp2_fast(x[k]);
+#pragma unroll
+            for (uint32_t k = 0; k < 32; k += 2) add2(sums[0], sums[1], x[k], x[k + 1]);
+            if (!MX) {
+#pragma unroll
+              for (uint32_t k = 0; k < 8; ++k) {
+                const float4 f = v_scale[8 * c + k];
+                mul2(x[4 * k], x[4 * k + 1], f.x, f.y);
+                mul2(x[4 * k + 2], x[4 * k + 3], f.z, f.w);
+              }
+              if (!every) {
+#pragma unroll
+                for (uint32_t k = 0; k < 32; ++k)
+                  if (!(seen >> k & 1u)) x[k] = 0.f;         // not zero times a poisoned scale
+              }
+            } else if (poisoned) {
+              const uint32_t nan = bad[c] & seen;
+#pragma unroll
+              for (uint32_t k = 0; k < 32; ++k)
+                if (nan >> k & 1u) x[k] = __uint_as_float(0x7fc00000u);
+            }
+            uint32_t h[16];
+#pragma unroll
+            for (uint32_t k = 0; k < 16; ++k) h[k] = pack_half(x[2 * k], x[2 * k + 1]);
+            tensor_write16(s_at + 16 * c, h);
+          }
+          sum += sums[0] + sums[1];
+          tensor_write_wait();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) bar_arrive(p_full(t));
+        }
+        if (!ok) break;
+      }
       tiles_before += n_units;
-    } while (at.next(p));
-  } else if (warp >= 8 && warp < 12) {
+    }
+  } else if (warp < 12) {
     // ---------------------------------------------------------------------------------- codes into operands
     constexpr uint32_t TOK = F::TOK, LOADS = F::LOADS, HIGH = F::HIGH, WORDS = F::SCALE_WORDS, PACKS = MX ? (NB + 3) / 4 : 1;
     const uint32_t part = warp - 8, first = part * TOK;                      // this warp's tokens of a tile
@@ -452,150 +556,168 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
     uint4 code[2][LOADS];
     uint32_t scale_word[2][WORDS];
     uint32_t lead = 0;                                                       // where the scales begin in their first word, keys' and values'
-    uint32_t n = 0;                                                          // tiles so far
-    bool ok = true;
-    do {
-      const uint32_t n_units = at.unit1 - at.unit;
-      const int32_t* const pages = a.table + at.seq * a.table_ld;
-      auto token = [&](uint32_t u) { return (uint64_t)at.t.j0 + (uint64_t)(at.unit + u) * KT + first + lane; };
-      auto page_of = [&](uint32_t u) -> int32_t {                            // of this lane's token of a tile; negative: no such token
-        const uint64_t j = token(u);
-        if (u >= n_units || lane >= TOK || j >= at.t.j1) return -1;
-        const int32_t id = __ldg(pages + p.page.div((uint32_t)j));
-        return id >= 0 && (uint32_t)id < a.c.pages ? id : -1;
-      };
-      auto fetch = [&](uint32_t u, int32_t id) {
-        const uint32_t j = (uint32_t)token(u), off = j - p.page.div(j) * p.page.d;
-        const uint64_t row = id < 0 ? 0 : ((uint64_t)(uint32_t)id * p.page.d + off) * a.c.heads + at.kv;
+    auto page_of = [&](uint32_t u) -> int32_t {                              // of this lane's token of unit u of the item; negative: no such token
+      const uint64_t j = (uint64_t)at.t.j0 + (uint64_t)u * KT + first + lane;
+      if (u >= at.unit1 || lane >= TOK || j >= at.t.j1) return -1;
+      const int32_t id = __ldg(a.table + at.seq * a.table_ld + p.page.div((uint32_t)j));
+      return id >= 0 && (uint32_t)id < a.c.pages ? id : -1;
+    };
+    uint64_t row = 0;                                                        // of this lane's token in the cache
+    auto fetch_scales = [&](uint32_t u, int32_t id) {
+      const uint32_t j = at.t.j0 + u * KT + first + lane, off = j - p.page.div(j) * p.page.d;
+      row = id < 0 ? 0 : ((uint64_t)(uint32_t)id * p.page.d + off) * a.c.heads + at.kv;
+      lead = 0;
 #pragma unroll
-        for (int w = 0; w < 2; ++w)
+      for (int w = 0; w < 2; ++w) {
 #pragma unroll
-          for (uint32_t k = 0; k < WORDS; ++k) scale_word[w][k] = 0;
-        lead = 0;
-        if (id >= 0) {
+        for (uint32_t k = 0; k < WORDS; ++k) scale_word[w][k] = 0;
+        if (id < 0) continue;
+        if (MX) {                                                            // whole words, each of which holds a wanted byte
+          const uintptr_t from = (uintptr_t)a.c.scales[w] + row * blocks;
+          const uint32_t l = (uint32_t)(from & 3u);
+          lead |= l << (4 * w);
 #pragma unroll
-          for (int w = 0; w < 2; ++w) {
-            if (MX) {                                                        // whole words, each of which holds a wanted byte
-              const uintptr_t from = (uintptr_t)a.c.scales[w] + row * blocks;
-              const uint32_t l = (uint32_t)(from & 3u);
-              lead |= l << (4 * w);
+          for (uint32_t k = 0; k < WORDS; ++k)
+            if (4 * k < l + blocks) scale_word[w][k] = __ldg(reinterpret_cast<const uint32_t*>(from & ~(uintptr_t)3u) + k);
+        } else scale_word[w][0] = __ldg(reinterpret_cast<const uint32_t*>(a.c.scales[w]) + row);
+      }
+    };
+    auto fetch = [&](int w, int32_t id) {
 #pragma unroll
-              for (uint32_t k = 0; k < WORDS; ++k)
-                if (4 * k < l + blocks) scale_word[w][k] = __ldg(reinterpret_cast<const uint32_t*>(from & ~(uintptr_t)3u) + k);
-            } else scale_word[w][0] = __ldg(reinterpret_cast<const uint32_t*>(a.c.scales[w]) + row);
+      for (uint32_t i = 0; i < LOADS; ++i) {
+        const uint32_t r = (i % (TOK / HIGH)) * HIGH + lane % HIGH, c16 = 16 * ((i / (TOK / HIGH)) * F::WIDE + lane / HIGH);
+        const uint64_t src = __shfl_sync(0xffffffffu, row, r) * row_bytes + c16;
+        const bool there = __shfl_sync(0xffffffffu, id, r) >= 0 && c16 < row_bytes;
+        code[w][i] = make_uint4(0, 0, 0, 0);
+        if (there && (MX || p.vec_codes)) code[w][i] = __ldg(reinterpret_cast<const uint4*>(a.c.codes[w] + src));
+      }
+      if (MX || p.vec_codes) return;
+#pragma unroll 1
+      for (uint32_t i = 0; i < LOADS; ++i) {                                 // rows on any address
+        const uint32_t r = (i % (TOK / HIGH)) * HIGH + lane % HIGH, c16 = 16 * ((i / (TOK / HIGH)) * F::WIDE + lane / HIGH);
+        const uint64_t src = __shfl_sync(0xffffffffu, row, r) * row_bytes + c16;
+        const bool there = __shfl_sync(0xffffffffu, id, r) >= 0 && c16 < row_bytes;
+        uint32_t v[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (uint32_t b = 0; b < 16; ++b)
+          if (there && c16 + b < row_bytes) v[b / 4] |= (uint32_t)__ldg(a.c.codes[w] + src + b) << (8 * (b % 4));
+#pragma unroll
+        for (uint32_t k = 0; k < LOADS; ++k)
+          if (k == i) code[w][k] = make_uint4(v[0], v[1], v[2], v[3]);
+      }
+    };
+    uint32_t u = at.unit;
+    int32_t id = page_of(u), id_next = page_of(u + 1);
+    fetch_scales(u, id);
+    fetch(0, id);
+    fetch(1, id);
+    int v_top = -126;
+    bool more = true;
+#pragma unroll 1
+    for (uint32_t n = 0; more; ++n) {
+      const uint32_t s = n % F::STAGES, phase = (n / F::STAGES & 1) ^ 1;
+      // scales, a token to a lane: the row's, and (4 bits) how far below it each block's is
+      float scale[2] = {0.f, 0.f};
+      uint32_t bytes[2][PACKS], high_byte[2] = {0, 0};                       // 4 bits: scales of the blocks, and the largest
+      const uint32_t real = __ballot_sync(0xffffffffu, id >= 0);
+#pragma unroll
+      for (int w = 0; w < 2; ++w) {
+        if (MX) {
+          const uint32_t shift = 8 * (lead >> (4 * w) & 3u);
+#pragma unroll
+          for (uint32_t k = 0; k < PACKS; ++k) {
+            bytes[w][k] = __funnelshift_r(scale_word[w][k], k + 1 < WORDS ? scale_word[w][k + 1 < WORDS ? k + 1 : 0] : 0u, shift);
+            const uint32_t have = blocks - min(blocks, 4 * k);
+            if (have < 4) bytes[w][k] &= (1u << (8 * have)) - 1u;
+#pragma unroll
+            for (uint32_t b = 0; b < 4; ++b) high_byte[w] = max(high_byte[w], bytes[w][k] >> (8 * b) & 255u);
           }
+        } else scale[w] = __uint_as_float(scale_word[w][0]);
+      }
+      // the largest exponents: 4 bits, of the tile's keys, as bytes; of the values (8 bits: finite scales are positive)
+      const uint32_t field = MX ? (high_byte[1] == 255u ? 0u : high_byte[1]) : (__float_as_uint(scale[1]) >> 23 & 255u);
+      const int v_most = __reduce_max_sync(0xffffffffu, field == 255u ? -126 : min(max((int)field - 127, -126), 126));
+      const int k_most = MX ? __reduce_max_sync(0xffffffffu, high_byte[0] == 255u ? 0u : high_byte[0]) : 0;
+      const uint32_t poisoned = __ballot_sync(0xffffffffu, MX && high_byte[1] == 255u);
+      if (lane == 0) { highest[n & 1][0][part] = k_most; highest[n & 1][1][part] = v_most; }
+      bool ok = bar_wait(k_empty(s), phase, failed);
+      ok = bar_wait(v_empty(s), phase, failed) && ok;
+      if (!all_converting(ok)) break;
+      int k_top = 1;
+#pragma unroll
+      for (uint32_t k = 0; k < 4; ++k) { k_top = max(k_top, highest[n & 1][0][k]); v_top = max(v_top, highest[n & 1][1][k]); }
+      uint8_t* const m = meta + s * F::META;
+      if (!MX && lane < TOK) {
+        reinterpret_cast<float*>(m)[first + lane] = scale[0];
+        reinterpret_cast<float*>(m + 4 * KT)[first + lane] = scale[1] * power_of_two(-v_top);
+      }
+      if (lane == 0) {
+        if (TOK == 32) {
+          reinterpret_cast<uint32_t*>(m + 8 * KT)[part] = real;
+          reinterpret_cast<uint32_t*>(m + 8 * KT + 16)[part] = poisoned;
+        } else {
+          reinterpret_cast<uint16_t*>(m + 8 * KT)[part] = (uint16_t)real;
+          reinterpret_cast<uint16_t*>(m + 8 * KT + 16)[part] = (uint16_t)poisoned;
         }
+        if (part == 0) *reinterpret_cast<int2*>(m + 8 * KT + 32) = make_int2(k_top - 127, v_top);
+      }
+      // 4 bits: how far below the largest each block is, 255 where the values are left out
+      uint32_t below[2][PACKS];
+#pragma unroll
+      for (uint32_t k = 0; k < PACKS; ++k) {
+        below[0][k] = MX ? __vsubus4((uint32_t)k_top * 0x01010101u, bytes[0][MX ? k : 0]) : 0;
+        below[1][k] = !MX ? 0 : high_byte[1] == 255u ? ~0u : __vsubus4((uint32_t)(v_top + 127) * 0x01010101u, bytes[1][MX ? k : 0]);
+      }
+      const uint32_t nan_key = __ballot_sync(0xffffffffu, MX && high_byte[0] == 255u);
+      // on to the next tile: its scales and codes are fetched while this one's are converted
+      if (++u == at.unit1) {
+        more = at.next(p);
+        u = at.unit; v_top = -126;
+        id = more ? page_of(u) : -1;
+        id_next = more ? page_of(u + 1) : -1;
+      } else {
+        id = id_next;
+        id_next = page_of(u + 1);
+      }
+      fetch_scales(u, id);
+#pragma unroll
+      for (int w = 0; w < 2; ++w) {
+        const uint32_t tile = (w ? v_at : k_at) + s * F::KV_TILE;
 #pragma unroll
         for (uint32_t i = 0; i < LOADS; ++i) {
-          const uint32_t r = (i % (TOK / HIGH)) * HIGH + lane % HIGH, c16 = 16 * ((i / (TOK / HIGH)) * F::WIDE + lane / HIGH);
-          const uint64_t src = __shfl_sync(0xffffffffu, row, r) * row_bytes + c16;
-          const bool there = __shfl_sync(0xffffffffu, id, r) >= 0 && c16 < row_bytes;
-#pragma unroll
-          for (int w = 0; w < 2; ++w) {
-            code[w][i] = make_uint4(0, 0, 0, 0);
-            if (!there) continue;
-            if (MX || p.vec_codes) code[w][i] = __ldg(reinterpret_cast<const uint4*>(a.c.codes[w] + src));
-            else {
-              uint32_t v[4] = {0, 0, 0, 0};
-#pragma unroll
-              for (uint32_t b = 0; b < 16; ++b)
-                if (c16 + b < row_bytes) v[b / 4] |= (uint32_t)__ldg(a.c.codes[w] + src + b) << (8 * (b % 4));
-              code[w][i] = make_uint4(v[0], v[1], v[2], v[3]);
-            }
-          }
-        }
-      };
-      int32_t id = page_of(0), id_next = page_of(1);
-      fetch(0, id);
-      int v_top = -126;
-#pragma unroll 1
-      for (uint32_t u = 0; u < n_units; ++u, ++n) {
-        const uint32_t s = n % F::STAGES, phase = (n / F::STAGES & 1) ^ 1;
-        // scales, a token to a lane: the row's, and (4 bits) how far below it each block's is
-        float scale[2] = {0.f, 0.f};
-        uint32_t below[2][PACKS];
-        const uint32_t real = __ballot_sync(0xffffffffu, id >= 0);
-#pragma unroll
-        for (int w = 0; w < 2; ++w) {
+          const uint32_t r = (i % (TOK / HIGH)) * HIGH + lane % HIGH, piece = (i / (TOK / HIGH)) * F::WIDE + lane / HIGH;
+          const uint32_t in = first + r;
+          auto put = [&](uint32_t d, uint32_t x, uint32_t y, uint32_t z, uint32_t t) {
+            const uint32_t to = tile + (d / 64) * F::PANEL + in * 128 + (((d / 8) ^ in) & 7) * 16;
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(x), "r"(y), "r"(z), "r"(t) : "memory");
+          };
+          const uint32_t word[4] = {code[w][i].x, code[w][i].y, code[w][i].z, code[w][i].w};
           if (MX) {
-            const uint32_t shift = 8 * (lead >> (4 * w) & 3u);
-            uint32_t bytes[PACKS], most = 0;
+            uint32_t pack = __shfl_sync(0xffffffffu, below[w][0], r);
+            if (PACKS > 1) { const uint32_t other = __shfl_sync(0xffffffffu, below[w][PACKS - 1], r); if (piece >= 4) pack = other; }
+            const int f = kChunkFactor - (int)(pack >> (8 * (piece & 3u)) & 255u);
+            const uint32_t h = w == 0 && (nan_key >> r & 1u) ? 0x7e00u : f < -24 ? 0u : f >= -14 ? (uint32_t)(f + 15) << 10 : 1u << (f + 24), factor = h | h << 16;
 #pragma unroll
-            for (uint32_t k = 0; k < PACKS; ++k) {
-              bytes[k] = __funnelshift_r(scale_word[w][k], k + 1 < WORDS ? scale_word[w][k + 1 < WORDS ? k + 1 : 0] : 0u, shift);
-              const uint32_t have = blocks - min(blocks, 4 * k);
-              if (have < 4) bytes[k] &= (1u << (8 * have)) - 1u;
-#pragma unroll
-              for (uint32_t b = 0; b < 4; ++b) most = max(most, bytes[k] >> (8 * b) & 255u);
+            for (uint32_t k = 0; k < 4; ++k) {
+              uint32_t c[4];
+              four_bits(word[k], c);
+              put(32 * piece + 8 * k, half_mul(c[0], factor), half_mul(c[1], factor), half_mul(c[2], factor), half_mul(c[3], factor));
             }
-            scale[w] = id >= 0 ? mx_scale(most) : 0.f;                       // NaN if any block is poisoned
-#pragma unroll
-            for (uint32_t k = 0; k < PACKS; ++k) below[w][k] = most == 255u || id < 0 ? ~0u : __vsubus4(most * 0x01010101u, bytes[k]);
           } else {
-            scale[w] = __uint_as_float(scale_word[w][0]);
-            below[w][0] = 0;
-          }
-        }
-        const uint32_t field = __float_as_uint(scale[1]) >> 23 & 255u;       // finite scales are positive
-        const int most = __reduce_max_sync(0xffffffffu, field == 255u ? -126 : min(max((int)field - 127, -126), 126));
-        if (lane == 0) highest[n & 1][part] = most;
-        ok = bar_wait(k_empty(s), phase, failed);
-        ok = bar_wait(v_empty(s), phase, failed) && ok;
-        ok = all_converting(ok);
-        if (!ok) break;
 #pragma unroll
-        for (uint32_t k = 0; k < 4; ++k) v_top = max(v_top, highest[n & 1][k]);
-        uint8_t* const m = meta + s * F::META;
-        if (lane < TOK) {
-          reinterpret_cast<float*>(m)[first + lane] = scale[0];
-          reinterpret_cast<float*>(m + 4 * KT)[first + lane] = scale[1] * power_of_two(-v_top) * (float)(1 << kChunkBits);
-        }
-        if (lane == 0) {
-          if (TOK == 32) reinterpret_cast<uint32_t*>(m + 8 * KT)[part] = real;
-          else reinterpret_cast<uint16_t*>(m + 8 * KT)[part] = (uint16_t)real;
-          if (part == 0) *reinterpret_cast<int32_t*>(m + 8 * KT + 16) = v_top;
-        }
-#pragma unroll
-        for (int w = 0; w < 2; ++w) {
-          const uint32_t tile = (w ? v_at : k_at) + s * F::KV_TILE;
-#pragma unroll
-          for (uint32_t i = 0; i < LOADS; ++i) {
-            const uint32_t r = (i % (TOK / HIGH)) * HIGH + lane % HIGH, piece = (i / (TOK / HIGH)) * F::WIDE + lane / HIGH;
-            const uint32_t row = first + r;
-            auto put = [&](uint32_t d, uint32_t x, uint32_t y, uint32_t z, uint32_t t) {
-              const uint32_t to = tile + (d / 64) * F::PANEL + row * 128 + (((d / 8) ^ row) & 7) * 16;
-              asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(x), "r"(y), "r"(z), "r"(t) : "memory");
-            };
-            const uint32_t word[4] = {code[w][i].x, code[w][i].y, code[w][i].z, code[w][i].w};
-            if (MX) {
-              uint32_t pack = __shfl_sync(0xffffffffu, below[w][0], r);
-              if (PACKS > 1) { const uint32_t more = __shfl_sync(0xffffffffu, below[w][PACKS - 1], r); if (piece >= 4) pack = more; }
-              const int f = kChunkFactor - (int)(pack >> (8 * (piece & 3u)) & 255u);
-              const uint32_t h = f < -24 ? 0u : f >= -14 ? (uint32_t)(f + 15) << 10 : 1u << (f + 24), factor = h | h << 16;
-#pragma unroll
-              for (uint32_t k = 0; k < 4; ++k) {
-                uint32_t c[4];
-                four_bits(word[k], c);
-                put(32 * piece + 8 * k, half_mul(c[0], factor), half_mul(c[1], factor), half_mul(c[2], factor), half_mul(c[3], factor));
-              }
-            } else {
-#pragma unroll
-              for (uint32_t k = 0; k < 4; k += 2) {
-                const uint32_t x = word[k] ^ 0x80808080u, y = word[k + 1] ^ 0x80808080u;
-                put(16 * piece + 4 * k, eight_bits<0x4140>(x), eight_bits<0x4342>(x), eight_bits<0x4140>(y), eight_bits<0x4342>(y));
-              }
+            for (uint32_t k = 0; k < 4; k += 2) {
+              const uint32_t x = word[k] ^ 0x80808080u, y = word[k + 1] ^ 0x80808080u;
+              put(16 * piece + 4 * k, eight_bits<0x4140>(x), eight_bits<0x4342>(x), eight_bits<0x4140>(y), eight_bits<0x4342>(y));
             }
           }
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-          __syncwarp();
-          if (lane == 0) bar_arrive(w ? v_full(s) : k_full(s));
         }
-        id = id_next;
-        id_next = page_of(u + 2);
-        if (u + 1 < n_units) fetch(u + 1, id);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) bar_arrive(w ? v_full(s) : k_full(s));
+        if (more) fetch(w, id);
       }
-    } while (ok && at.next(p));
-  } else if (warp == 12) {
+    }
+  } else {
     // ---------------------------------------------------------------------------------- products
     uint32_t n = 0, q_turn[2] = {0, 0}, p_turn[2] = {0, 0};
     auto scores = [&](uint32_t t, uint32_t s) {                              // by one lane
@@ -685,11 +807,11 @@ cudaError_t launch_chunk(const Launch& l, ChunkArgs p, const AttendRun& run, uin
   return launch_attend_join(l, p.a, p.parts, p.pieces, run.chunk_ctas, 0, F::ROWS, F::DP, launches);
 }
 
-template <int FORMAT>
+template <int FORMAT, bool PLAIN>
 cudaError_t launch_dim(const Launch& l, const ChunkArgs& p, const AttendRun& run, uint64_t* launches) {
-  if (run.dp == 64) return launch_chunk<Chunk<FORMAT, 64>>(l, p, run, launches);
-  if (run.dp == 128) return launch_chunk<Chunk<FORMAT, 128>>(l, p, run, launches);
-  return launch_chunk<Chunk<FORMAT, 256>>(l, p, run, launches);
+  if (run.dp == 64) return launch_chunk<Chunk<FORMAT, 64, PLAIN>>(l, p, run, launches);
+  if (run.dp == 128) return launch_chunk<Chunk<FORMAT, 128, PLAIN>>(l, p, run, launches);
+  return launch_chunk<Chunk<FORMAT, 256, PLAIN>>(l, p, run, launches);
 }
 
 }  // namespace
@@ -698,8 +820,10 @@ cudaError_t launch_attend_chunk(const Launch& l, const AttendArgs& a, const Atte
   ChunkArgs p;
   p.a = a; p.page = FastDiv(a.c.page_size); p.group = FastDiv(a.group); p.few = run.few;
   p.vec_codes = a.c.dim % 16 == 0 && ((uintptr_t)a.c.codes[0] | (uintptr_t)a.c.codes[1]) % 16 == 0;
-  p.vec_out = attend_vec_out(a); p.fault = run.fault;
-  return a.c.format == QV2_KV_MX4 ? launch_dim<QV2_KV_MX4>(l, p, run, launches) : launch_dim<QV2_KV_I8>(l, p, run, launches);
+  p.vec_q = a.c.dim % 8 == 0 && ((uintptr_t)a.q | a.q_token_ld * 2 | a.q_head_ld * 2) % 16 == 0;
+  p.vec_out = a.c.dim % 8 == 0 && (uintptr_t)a.out % 16 == 0; p.fault = run.fault;
+  if (!(a.cap > 0.f) && !a.slopes) return a.c.format == QV2_KV_MX4 ? launch_dim<QV2_KV_MX4, true>(l, p, run, launches) : launch_dim<QV2_KV_I8, true>(l, p, run, launches);
+  return a.c.format == QV2_KV_MX4 ? launch_dim<QV2_KV_MX4, false>(l, p, run, launches) : launch_dim<QV2_KV_I8, false>(l, p, run, launches);
 }
 
 }  // namespace qv2
