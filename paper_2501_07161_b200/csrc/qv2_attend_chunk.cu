@@ -3,8 +3,9 @@
 // A CTA takes 256 query rows (two tiles of 128; one tile where a head has more than 128 elements) against tiles of 128 (64) tokens:
 //   warps 0-3, 4-7   the softmax of one tile each, a thread to a row: scores from tensor memory, weights back into it in
 //                    binary16, where the second product reads them; results out at the end,
-//   warps 8-11       turn codes and scales of keys and values into operands in shared memory, once for both tiles,
-//   warp 12          issues the products (tcgen05.mma): scores S = Q K^T, results O += P V.
+//   warps 12, 13     look up the tokens of a tile ahead: where their rows lie, what their scales come to,
+//   warps 8-11       turn codes of keys and values into operands in shared memory, once for both tiles,
+//   warp 14          issues the products (tcgen05.mma): scores S = Q K^T, results O += P V.
 // While one tile's softmax runs the tensor cores are at the other tile's products.  Bound by the exponentials (16 a cycle and SM: 2048
 // cycles for 2 x 128 x 128 scores) next to the products (2 x 2 x 512 cycles for 128 elements).
 //
@@ -21,7 +22,9 @@ namespace qv2 {
 
 namespace {
 
-constexpr uint32_t kChunkThreads = 13 * 32;
+constexpr uint32_t kConvert = 4, kScout = 2;                         // converting and looking-up warps
+constexpr uint32_t kFirstScout = 8 + kConvert, kProducts = kFirstScout + kScout, kChunkThreads = (kProducts + 1) * 32;
+constexpr uint32_t kSetup = 4;              // what an item costs besides its tiles, in tiles
 constexpr int kChunkFactor = 13;            // 4 bits: operands stand 2^13 above code * scale / (largest scale): 6 * 2^13 at most
 constexpr float kSlack = 4.f;               // a row's largest weight is 2^kSlack at most ...
 constexpr int kWeightBits = 10;             // ... and weights stand 2^10 above that: at most 2^15 (8 bits: times up to 2), and what binary16 loses below 2^-35
@@ -74,10 +77,10 @@ __device__ __forceinline__ void fma2(float& x, float& y, float f, float c) {
       : "+f"(x), "+f"(y) : "f"(f), "f"(c));
 }
 __device__ __forceinline__ float max3(float a, float b, float c) { float r; asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c)); return r; }
-// Whether all 128 threads of the four converting warps say yes.
-__device__ __forceinline__ bool all_converting(bool ok) {
+// Whether all threads of the looking-up warps say yes.
+__device__ __forceinline__ bool all_scouts(bool ok) {
   uint32_t r;
-  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, 1, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(r) : "r"((uint32_t)ok) : "memory");
+  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, 1, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(r) : "r"((uint32_t)ok), "n"(32 * kScout) : "memory");
   return r != 0;
 }
 
@@ -103,13 +106,17 @@ struct Chunk {
   static constexpr uint32_t Q_PANEL = 128 * 128, Q_TILE = Q_PANEL * (DP / 64);
   static constexpr uint32_t PANEL = KT * 128, KV_TILE = PANEL * (DP / 64);
   static constexpr uint32_t STAGES = 2;
-  static constexpr uint32_t META = 2 * 4 * KT + 16 + 16 + 16;         // 8 bits: scales of keys, of values; which tokens there are; whose value is poisoned; largest exponents
-  static constexpr uint32_t SMEM = 1024 + QT * Q_TILE + STAGES * (2 * KV_TILE + META) + 256;
+  // What is known of a tile's tokens: where each row lies; 4 bits: factors of keys' and values' blocks [2][block][token], 8 bits: scales of keys, of
+  // values [2][token]; then which tokens there are, whose value is poisoned (4 words each), the largest exponents and flags.
+  static constexpr uint32_t INFO = 4;                                 // tiles ahead
+  static constexpr uint32_t FACTOR_LD = KT + 8;                       // (blocks of a token in different banks)
+  static constexpr uint32_t AT_SCALES = 8 * KT, AT_BITS = AT_SCALES + (MX ? 2 * 2 * NB * FACTOR_LD : 2 * 4 * KT), META = AT_BITS + 48;
+  static constexpr uint32_t SMEM = 1024 + QT * Q_TILE + STAGES * 2 * KV_TILE + INFO * META;
   static constexpr uint32_t O_COL = QT * KT;                          // tensor memory: scores of the tiles, then their results
   static_assert(O_COL + QT * DP <= 512, "tensor memory");
   static constexpr uint32_t S_IDESC = (1u << 4) | ((KT / 8) << 17) | (8u << 24);                    // binary16 x binary16, binary32 sums
   static constexpr uint32_t O_IDESC = (1u << 4) | (1u << 16) | ((DP / 8) << 17) | (8u << 24);       // second operand across its rows
-  static constexpr uint32_t TOK = KT / 4;                             // tokens of a converting warp
+  static constexpr uint32_t TOK = KT / kConvert;                             // tokens of a converting warp
   static constexpr uint32_t PIECES = RB / 16, WIDE = PIECES < 4 ? PIECES : 4;   // 16-byte pieces of a row; how many of a row in one instruction
   static constexpr uint32_t HIGH = 32 / WIDE;                         // rows in one instruction
   static constexpr uint32_t LOADS = TOK * PIECES / 32;                // of a lane, for keys or values
@@ -151,29 +158,36 @@ __device__ __forceinline__ uint32_t chunk_tiles(const ChunkArgs& p, const Attend
   return rows <= p.few ? 0 : (uint32_t)((rows + F::ROWS - 1) / F::ROWS);
 }
 
-// Where a CTA stands in the row of all units: sequence, row tile, key head, unit of that item.  Every warp keeps one of its own.
+// Where a CTA stands in the row of all items: sequence, row tile, key head, and its part of that item.  An item takes kSetup + units;
+// what a CTA has of the setup alone is nothing.  Every warp keeps one of its own.
 template <class F>
 struct Walk {
-  uint32_t seq, tile, tiles, kv, unit, unit1;    // units unit .. unit1 - 1 of the item are this CTA's
-  uint64_t left;                                 // units of this CTA from here on
+  uint32_t seq, tile, tiles, kv;
+  uint32_t x0, x1, unit, unit1;                  // the part in those terms, and its units unit .. unit1 - 1
+  uint64_t left;                                 // of this CTA, from x0 on
   AttendSeq s;
   ChunkTile t;
   __device__ __forceinline__ void enter(const ChunkArgs& p) {
     t = chunk_tile<F>(p, s, tile);
-    unit1 = (uint32_t)min((uint64_t)t.units, unit + left);
+    const uint32_t all = t.units + kSetup;
+    x1 = (uint32_t)min((uint64_t)all, x0 + left);
+    unit = max(x0, kSetup) - kSetup;
+    unit1 = max(x1, kSetup) - kSetup;
   }
-  __device__ __forceinline__ bool next(const ChunkArgs& p) {       // on to the next item
-    left -= unit1 - unit;
-    if (left == 0) return false;
-    unit = 0;
-    if (++kv == p.a.c.heads) {
-      kv = 0;
-      if (++tile == tiles) {
-        tile = 0;
-        do { s = attend_seq(p.a, ++seq); tiles = chunk_tiles<F>(p, s); } while (tiles == 0);
+  __device__ __forceinline__ bool next(const ChunkArgs& p) {       // on to the next item of which this CTA has a unit
+    do {
+      left -= x1 - x0;
+      if (left == 0) return false;
+      x0 = 0;
+      if (++kv == p.a.c.heads) {
+        kv = 0;
+        if (++tile == tiles) {
+          tile = 0;
+          do { s = attend_seq(p.a, ++seq); tiles = chunk_tiles<F>(p, s); } while (tiles == 0);
+        }
       }
-    }
-    enter(p);
+      enter(p);
+    } while (unit == unit1);
     return true;
   }
 };
@@ -185,9 +199,9 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
   extern __shared__ uint8_t raw[];
   __shared__ uint64_t scan[kChunkThreads / 32];
   __shared__ struct { uint64_t before; uint32_t seq; } found;
-  __shared__ uint64_t bars[17];
+  __shared__ uint64_t bars[17 + 8];
   __shared__ uint32_t tmem_slot, failed_flag;
-  __shared__ int32_t highest[2][2][4];
+  __shared__ int32_t highest[2][2][kScout];
   const AttendArgs& a = p.a;
   const uint32_t tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
   uint8_t* const base = raw + ((1024u - (smem_addr(raw) & 1023u)) & 1023u);
@@ -203,16 +217,19 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
   auto p_full = [&](uint32_t t) { return bar0 + 8 * (12 + t); };
   auto o_done = [&](uint32_t t) { return bar0 + 8 * (14 + t); };
   const uint32_t drained = bar0 + 8 * 16;
+  auto m_full = [&](uint32_t s) { return bar0 + 8 * (17 + s); };
+  auto m_empty = [&](uint32_t s) { return bar0 + 8 * (21 + s); };
   volatile uint32_t* const failed = &failed_flag;
   dependency_wait();
   allow_dependents();
 
   if (tid == 0) {
     for (uint32_t s = 0; s < 2; ++s) {
-      bar_init(k_full(s), 4); bar_init(k_empty(s), 1); bar_init(v_full(s), 4); bar_init(v_empty(s), 1);
+      bar_init(k_full(s), kConvert); bar_init(k_empty(s), 1); bar_init(v_full(s), kConvert); bar_init(v_empty(s), 1);
       bar_init(q_full(s), 4); bar_init(s_full(s), 1); bar_init(p_full(s), 4); bar_init(o_done(s), 1);
     }
     bar_init(drained, 1);
+    for (uint32_t s = 0; s < F::INFO; ++s) { bar_init(m_full(s), kScout); bar_init(m_empty(s), 1); }
     *failed = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -223,7 +240,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
     const AttendSeq q = attend_seq(a, s);
     const uint32_t tiles = chunk_tiles<F>(p, q);
     uint64_t sum = 0;
-    for (uint32_t t = 0; t < tiles; ++t) sum += chunk_tile<F>(p, q, t).units;
+    for (uint32_t t = 0; t < tiles; ++t) sum += chunk_tile<F>(p, q, t).units + kSetup;
     return sum * a.c.heads;
   };
   uint64_t all = 0;
@@ -255,7 +272,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
     before += whole;
     if (u_begin < before) break;
   }
-  if (warp == 12) {
+  if (warp == kProducts) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(&tmem_slot)) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
@@ -270,18 +287,20 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
   at.tiles = chunk_tiles<F>(p, at.s);
   uint64_t in_seq = u_begin - found.before;
   for (;; ++at.tile) {
-    const uint64_t n = (uint64_t)chunk_tile<F>(p, at.s, at.tile).units * a.c.heads;
+    const uint64_t n = (uint64_t)(chunk_tile<F>(p, at.s, at.tile).units + kSetup) * a.c.heads;
     if (in_seq < n) break;
     in_seq -= n;
   }
   {
-    const uint32_t units = chunk_tile<F>(p, at.s, at.tile).units;
-    at.kv = (uint32_t)(in_seq / units);
-    at.unit = (uint32_t)(in_seq % units);
+    const uint32_t n = chunk_tile<F>(p, at.s, at.tile).units + kSetup;
+    at.kv = (uint32_t)(in_seq / n);
+    at.x0 = (uint32_t)(in_seq % n);
     at.enter(p);
   }
+  const bool any = at.unit < at.unit1 || at.next(p);         // (a CTA that has nothing but the beginning of a setup has no unit)
 
-  if (warp < 8) {
+  if (!any) {
+  } else if (warp < 8) {
     // ---------------------------------------------------------------------------------- softmax
     const uint32_t t = warp / 4, lanes = ((warp % 4) * 32) << 16, r_in = 128 * t + (warp % 4) * 32 + lane;
     const uint32_t s_at = tmem + t * KT + lanes, o_at = tmem + F::O_COL + t * DP + lanes;
@@ -312,53 +331,51 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
         ahead.pos = to.t.pos0 + (int32_t)i;
         ahead.pos_first = __shfl_sync(0xffffffffu, ahead.pos, 0);
         ahead.pos_last = __shfl_sync(0xffffffffu, ahead.pos, 31);
+        // A row by DP / 8 lanes, ROUND rows in one round of loads; rows that are not there take another's elements, times zero.
         const uint64_t from = (uint64_t)ahead.out_row * a.q_token_ld + (uint64_t)ahead.head * a.q_head_ld;
-        uint32_t top = 0;
-        int e = 0;
-        // (rows that are not there take another's elements, times zero)
+        uint32_t top = 0;                                    // bits of the largest magnitude of this lane's row
         auto bring = [&](auto zero, const auto* q) {
-          constexpr uint32_t HELD = DP == 64 ? 8 : 16;                 // groups of 8 elements in flight
-          decltype(zero) c[HELD];
-          auto load = [&](uint32_t d0) {
+          constexpr uint32_t LPR = DP / 8, ROUND = 32 / LPR, HELD = 8;       // lanes of a row, rows and rounds in flight
+          const uint32_t c8 = 8 * (lane % LPR), in = lane / LPR;
+#pragma unroll 1
+          for (uint32_t r0 = 0; r0 < 32; r0 += HELD * ROUND) {
+            decltype(zero) c[HELD];
             if (p.vec_q) {
 #pragma unroll
-              for (uint32_t k = 0; k < HELD; ++k) c[k].load_vec(q + from + min(d0 + 8 * k, a.c.dim - 8));
+              for (uint32_t k = 0; k < HELD; ++k) c[k].load_vec(q + __shfl_sync(0xffffffffu, from, r0 + k * ROUND + in) + min(c8, a.c.dim - 8));
             } else {
 #pragma unroll
               for (uint32_t k = 0; k < HELD; ++k) {
-                const uint32_t d = d0 + 8 * k;
+                const uint64_t row_at = __shfl_sync(0xffffffffu, from, r0 + k * ROUND + in);
                 c[k].zero();
-                if (d + 8 <= a.c.dim) c[k].load_any(q + from + d);
-                else if (d < a.c.dim) c[k].load_some(q + from + d, a.c.dim - d);
+                if (c8 + 8 <= a.c.dim) c[k].load_any(q + row_at + c8);
+                else if (c8 < a.c.dim) c[k].load_some(q + row_at + c8, a.c.dim - c8);
               }
             }
-          };
-#pragma unroll 1
-          for (uint32_t d0 = 0; d0 < DP; d0 += 8 * HELD) {
-            load(d0);
-#pragma unroll
-            for (uint32_t k = 0; k < HELD; ++k) top = max(top, c[k].top_bits());
-          }
-          e = top ? max((int)(top >> 23) - 127, -100) : 0;
-          const float up = ahead.there ? copysignf(power_of_two(14 - min(e, 127)), a.scale) : 0.f;
-#pragma unroll 1
-          for (uint32_t d0 = 0; d0 < DP; d0 += 8 * HELD) {
-            if (DP > 8 * HELD) load(d0);
 #pragma unroll
             for (uint32_t k = 0; k < HELD; ++k) {
-              const uint32_t d = d0 + 8 * k, in = r_in % 128, where = q_at + t * F::Q_TILE + (d / 64) * F::Q_PANEL + in * 128 + (((d / 8) ^ in) & 7) * 16;
-              const float f = d < a.c.dim ? up : 0.f;
+              uint32_t high = c[k].top_bits();
+#pragma unroll
+              for (uint32_t o = LPR / 2; o > 0; o >>= 1) high = max(high, __shfl_xor_sync(0xffffffffu, high, o));
+              const uint32_t r = r0 + k * ROUND + in;                        // this lane's row of the round, of the warp's 32
+              const uint32_t mine = __shfl_sync(0xffffffffu, high, (lane % ROUND) * LPR);
+              if (lane / ROUND == r0 / ROUND + k) top = mine;
+              const bool there = __shfl_sync(0xffffffffu, (uint32_t)ahead.there, r) != 0;
+              const int e = high ? max((int)(high >> 23) - 127, -100) : 0;
+              const float up = there && c8 < a.c.dim ? copysignf(power_of_two(14 - min(e, 127)), a.scale) : 0.f;
               float v[8];
               c[k].widen(v);
               uint32_t h[4];
 #pragma unroll
-              for (int i2 = 0; i2 < 4; ++i2) h[i2] = pack_half(v[2 * i2] * f, v[2 * i2 + 1] * f);
+              for (int i2 = 0; i2 < 4; ++i2) h[i2] = pack_half(v[2 * i2] * up, v[2 * i2 + 1] * up);
+              const uint32_t row_in = (warp % 4) * 32 + r, where = q_at + t * F::Q_TILE + (c8 / 64) * F::Q_PANEL + row_in * 128 + (((c8 / 8) ^ row_in) & 7) * 16;
               asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(where), "r"(h[0]), "r"(h[1]), "r"(h[2]), "r"(h[3]) : "memory");
             }
           }
         };
         if (a.dtype == kBF16) bring(Chunk8<__nv_bfloat16>(), (const __nv_bfloat16*)a.q);
         else bring(Chunk8<__half>(), (const __half*)a.q);
+        const int e = top ? max((int)(top >> 23) - 127, -100) : 0;
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
         if (lane == 0) bar_arrive(q_full(t));
@@ -404,7 +421,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
           }
         }
         if (!whole && place == 1 && tid == 0) {
-          const uint64_t last = u_end - at.left + at.t.units - 1;     // u_end - left: the item's first unit
+          const uint64_t last = u_end - at.left - at.x0 + at.t.units + kSetup - 1;
           uint32_t c = (uint32_t)(last * ctas / all);
           while (all * c / ctas > last) --c;
           while (all * (c + 1) / ctas <= last) ++c;
@@ -423,21 +440,16 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
         ref = -INFINITY; sum = 0.f; v_top = -126;
 #pragma unroll 1
         for (uint32_t u = 0; u < n_units; ++u, ++turn) {
-          const uint8_t* const m = meta + (tiles_before + u) % F::STAGES * F::META;
-          const float4* const k_scale = reinterpret_cast<const float4*>(m);
-          const float4* const v_scale = reinterpret_cast<const float4*>(m + 4 * KT);
-          const uint32_t* const real = reinterpret_cast<const uint32_t*>(m + 8 * KT);
+          const uint8_t* const m = meta + (tiles_before + u) % F::INFO * F::META;
+          const float4* const k_scale = reinterpret_cast<const float4*>(m + F::AT_SCALES);
+          const float4* const v_scale = reinterpret_cast<const float4*>(m + F::AT_SCALES + 4 * KT);
+          const uint32_t* const real = reinterpret_cast<const uint32_t*>(m + F::AT_BITS);
           const uint32_t* const bad = real + 4;
           const uint32_t j = at.t.j0 + (at.unit + u) * KT;
           if (!bar_wait(s_full(t), turn & 1, failed)) { ok = false; break; }
           tc_fence_after();
-          const int2 tops = *reinterpret_cast<const int2*>(m + 8 * KT + 32);         // exponents of the tile's keys (4 bits), of the values so far
-          bool every = (int32_t)(j + KT - 1) <= row.pos_first && row.pos_last - (int32_t)j < a.window;
-#pragma unroll
-          for (uint32_t k = 0; k < KT / 32; ++k) every &= real[k] == 0xffffffffu;
-          bool poisoned = false;
-#pragma unroll
-          for (uint32_t k = 0; k < KT / 32; ++k) poisoned |= MX && bad[k] != 0;
+          const int4 tops = *reinterpret_cast<const int4*>(m + F::AT_BITS + 32);     // exponents of the tile's keys (4 bits), of the values so far; flags
+          const bool every = (tops.z & 1) && (int32_t)(j + KT - 1) <= row.pos_first && row.pos_last - (int32_t)j < a.window, poisoned = MX && (tops.z & 2);
           // what turns a score of the product into one to powers of two; not 0, since it multiplies minus infinity, too
           const float unit = MX ? row.back * power_of_two(tops.x) : row.back, mul = !F::PLAIN ? 1.f : unit < 1.2e-38f ? 1.2e-38f : unit;
           // scores of 32 tokens, up to mul
@@ -548,155 +560,65 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
       }
       tiles_before += n_units;
     }
-  } else if (warp < 12) {
+  } else if (warp < kFirstScout) {
     // ---------------------------------------------------------------------------------- codes into operands
-    constexpr uint32_t TOK = F::TOK, LOADS = F::LOADS, HIGH = F::HIGH, WORDS = F::SCALE_WORDS, PACKS = MX ? (NB + 3) / 4 : 1;
-    const uint32_t part = warp - 8, first = part * TOK;                      // this warp's tokens of a tile
-    const uint32_t blocks = (a.c.dim + 31) / 32, row_bytes = MX ? 16 * blocks : a.c.dim;
+    constexpr uint32_t TOK = F::TOK, LOADS = F::LOADS, HIGH = F::HIGH;
+    const uint32_t first = (warp - 8) * TOK;                                 // this warp's tokens of a tile
+    const uint32_t row_bytes = MX ? 16 * ((a.c.dim + 31) / 32) : a.c.dim;
     uint4 code[2][LOADS];
-    uint32_t scale_word[2][WORDS];
-    uint32_t lead = 0;                                                       // where the scales begin in their first word, keys' and values'
-    auto page_of = [&](uint32_t u) -> int32_t {                              // of this lane's token of unit u of the item; negative: no such token
-      const uint64_t j = (uint64_t)at.t.j0 + (uint64_t)u * KT + first + lane;
-      if (u >= at.unit1 || lane >= TOK || j >= at.t.j1) return -1;
-      const int32_t id = __ldg(a.table + at.seq * a.table_ld + p.page.div((uint32_t)j));
-      return id >= 0 && (uint32_t)id < a.c.pages ? id : -1;
+    auto at_load = [&](uint32_t i, uint32_t* in, uint32_t* piece) {          // token of the tile, 16-byte piece of its row
+      *in = first + (i % (TOK / HIGH)) * HIGH + lane % HIGH;
+      *piece = (i / (TOK / HIGH)) * F::WIDE + lane / HIGH;
     };
-    uint64_t row = 0;                                                        // of this lane's token in the cache
-    auto fetch_scales = [&](uint32_t u, int32_t id) {
-      const uint32_t j = at.t.j0 + u * KT + first + lane, off = j - p.page.div(j) * p.page.d;
-      row = id < 0 ? 0 : ((uint64_t)(uint32_t)id * p.page.d + off) * a.c.heads + at.kv;
-      lead = 0;
-#pragma unroll
-      for (int w = 0; w < 2; ++w) {
-#pragma unroll
-        for (uint32_t k = 0; k < WORDS; ++k) scale_word[w][k] = 0;
-        if (id < 0) continue;
-        if (MX) {                                                            // whole words, each of which holds a wanted byte
-          const uintptr_t from = (uintptr_t)a.c.scales[w] + row * blocks;
-          const uint32_t l = (uint32_t)(from & 3u);
-          lead |= l << (4 * w);
-#pragma unroll
-          for (uint32_t k = 0; k < WORDS; ++k)
-            if (4 * k < l + blocks) scale_word[w][k] = __ldg(reinterpret_cast<const uint32_t*>(from & ~(uintptr_t)3u) + k);
-        } else scale_word[w][0] = __ldg(reinterpret_cast<const uint32_t*>(a.c.scales[w]) + row);
-      }
-    };
-    auto fetch = [&](int w, int32_t id) {
+    auto fetch = [&](int w, const uint8_t* m) {
 #pragma unroll
       for (uint32_t i = 0; i < LOADS; ++i) {
-        const uint32_t r = (i % (TOK / HIGH)) * HIGH + lane % HIGH, c16 = 16 * ((i / (TOK / HIGH)) * F::WIDE + lane / HIGH);
-        const uint64_t src = __shfl_sync(0xffffffffu, row, r) * row_bytes + c16;
-        const bool there = __shfl_sync(0xffffffffu, id, r) >= 0 && c16 < row_bytes;
+        uint32_t in, piece;
+        at_load(i, &in, &piece);
+        const int64_t row = reinterpret_cast<const int64_t*>(m)[in];
         code[w][i] = make_uint4(0, 0, 0, 0);
-        if (there && (MX || p.vec_codes)) code[w][i] = __ldg(reinterpret_cast<const uint4*>(a.c.codes[w] + src));
+        if (row >= 0 && 16 * piece < row_bytes && (MX || p.vec_codes)) code[w][i] = __ldg(reinterpret_cast<const uint4*>(a.c.codes[w] + row + 16 * piece));
       }
-      if (MX || p.vec_codes) return;
-#pragma unroll 1
+      if constexpr (MX) return;
+      else if (p.vec_codes) return;
+#pragma unroll
       for (uint32_t i = 0; i < LOADS; ++i) {                                 // rows on any address
-        const uint32_t r = (i % (TOK / HIGH)) * HIGH + lane % HIGH, c16 = 16 * ((i / (TOK / HIGH)) * F::WIDE + lane / HIGH);
-        const uint64_t src = __shfl_sync(0xffffffffu, row, r) * row_bytes + c16;
-        const bool there = __shfl_sync(0xffffffffu, id, r) >= 0 && c16 < row_bytes;
-        uint32_t v[4] = {0, 0, 0, 0};
+        uint32_t in, piece, v[4] = {0, 0, 0, 0};
+        at_load(i, &in, &piece);
+        const int64_t row = reinterpret_cast<const int64_t*>(m)[in];
+#pragma unroll 1
+        for (uint32_t b = 0; b < 16 && row >= 0 && 16 * piece + b < row_bytes; ++b) {
+          const uint32_t byte = (uint32_t)__ldg(a.c.codes[w] + row + 16 * piece + b) << (8 * (b % 4));
 #pragma unroll
-        for (uint32_t b = 0; b < 16; ++b)
-          if (there && c16 + b < row_bytes) v[b / 4] |= (uint32_t)__ldg(a.c.codes[w] + src + b) << (8 * (b % 4));
-#pragma unroll
-        for (uint32_t k = 0; k < LOADS; ++k)
-          if (k == i) code[w][k] = make_uint4(v[0], v[1], v[2], v[3]);
+          for (uint32_t k = 0; k < 4; ++k) if (b / 4 == k) v[k] |= byte;
+        }
+        code[w][i] = make_uint4(v[0], v[1], v[2], v[3]);
       }
     };
-    uint32_t u = at.unit;
-    int32_t id = page_of(u), id_next = page_of(u + 1);
-    fetch_scales(u, id);
-    fetch(0, id);
-    fetch(1, id);
-    int v_top = -126;
-    bool more = true;
+    bool ok = bar_wait(m_full(0), 0, failed);
+    if (ok) { fetch(0, meta); fetch(1, meta); }
 #pragma unroll 1
-    for (uint32_t n = 0; more; ++n) {
+    for (uint32_t n = 0; ok; ++n) {
       const uint32_t s = n % F::STAGES, phase = (n / F::STAGES & 1) ^ 1;
-      // scales, a token to a lane: the row's, and (4 bits) how far below it each block's is
-      float scale[2] = {0.f, 0.f};
-      uint32_t bytes[2][PACKS], high_byte[2] = {0, 0};                       // 4 bits: scales of the blocks, and the largest
-      const uint32_t real = __ballot_sync(0xffffffffu, id >= 0);
+      const uint8_t* const m = meta + n % F::INFO * F::META;
+      const uint8_t* const m_next = meta + (n + 1) % F::INFO * F::META;
+      const bool more = !(*reinterpret_cast<const int32_t*>(m + F::AT_BITS + 40) & 4);
 #pragma unroll
       for (int w = 0; w < 2; ++w) {
-        if (MX) {
-          const uint32_t shift = 8 * (lead >> (4 * w) & 3u);
-#pragma unroll
-          for (uint32_t k = 0; k < PACKS; ++k) {
-            bytes[w][k] = __funnelshift_r(scale_word[w][k], k + 1 < WORDS ? scale_word[w][k + 1 < WORDS ? k + 1 : 0] : 0u, shift);
-            const uint32_t have = blocks - min(blocks, 4 * k);
-            if (have < 4) bytes[w][k] &= (1u << (8 * have)) - 1u;
-#pragma unroll
-            for (uint32_t b = 0; b < 4; ++b) high_byte[w] = max(high_byte[w], bytes[w][k] >> (8 * b) & 255u);
-          }
-        } else scale[w] = __uint_as_float(scale_word[w][0]);
-      }
-      // the largest exponents: 4 bits, of the tile's keys, as bytes; of the values (8 bits: finite scales are positive)
-      const uint32_t field = MX ? (high_byte[1] == 255u ? 0u : high_byte[1]) : (__float_as_uint(scale[1]) >> 23 & 255u);
-      const int v_most = __reduce_max_sync(0xffffffffu, field == 255u ? -126 : min(max((int)field - 127, -126), 126));
-      const int k_most = MX ? __reduce_max_sync(0xffffffffu, high_byte[0] == 255u ? 0u : high_byte[0]) : 0;
-      const uint32_t poisoned = __ballot_sync(0xffffffffu, MX && high_byte[1] == 255u);
-      if (lane == 0) { highest[n & 1][0][part] = k_most; highest[n & 1][1][part] = v_most; }
-      bool ok = bar_wait(k_empty(s), phase, failed);
-      ok = bar_wait(v_empty(s), phase, failed) && ok;
-      if (!all_converting(ok)) break;
-      int k_top = 1;
-#pragma unroll
-      for (uint32_t k = 0; k < 4; ++k) { k_top = max(k_top, highest[n & 1][0][k]); v_top = max(v_top, highest[n & 1][1][k]); }
-      uint8_t* const m = meta + s * F::META;
-      if (!MX && lane < TOK) {
-        reinterpret_cast<float*>(m)[first + lane] = scale[0];
-        reinterpret_cast<float*>(m + 4 * KT)[first + lane] = scale[1] * power_of_two(-v_top);
-      }
-      if (lane == 0) {
-        if (TOK == 32) {
-          reinterpret_cast<uint32_t*>(m + 8 * KT)[part] = real;
-          reinterpret_cast<uint32_t*>(m + 8 * KT + 16)[part] = poisoned;
-        } else {
-          reinterpret_cast<uint16_t*>(m + 8 * KT)[part] = (uint16_t)real;
-          reinterpret_cast<uint16_t*>(m + 8 * KT + 16)[part] = (uint16_t)poisoned;
-        }
-        if (part == 0) *reinterpret_cast<int2*>(m + 8 * KT + 32) = make_int2(k_top - 127, v_top);
-      }
-      // 4 bits: how far below the largest each block is, 255 where the values are left out
-      uint32_t below[2][PACKS];
-#pragma unroll
-      for (uint32_t k = 0; k < PACKS; ++k) {
-        below[0][k] = MX ? __vsubus4((uint32_t)k_top * 0x01010101u, bytes[0][MX ? k : 0]) : 0;
-        below[1][k] = !MX ? 0 : high_byte[1] == 255u ? ~0u : __vsubus4((uint32_t)(v_top + 127) * 0x01010101u, bytes[1][MX ? k : 0]);
-      }
-      const uint32_t nan_key = __ballot_sync(0xffffffffu, MX && high_byte[0] == 255u);
-      // on to the next tile: its scales and codes are fetched while this one's are converted
-      if (++u == at.unit1) {
-        more = at.next(p);
-        u = at.unit; v_top = -126;
-        id = more ? page_of(u) : -1;
-        id_next = more ? page_of(u + 1) : -1;
-      } else {
-        id = id_next;
-        id_next = page_of(u + 1);
-      }
-      fetch_scales(u, id);
-#pragma unroll
-      for (int w = 0; w < 2; ++w) {
+        ok = ok && bar_wait(w ? v_empty(s) : k_empty(s), phase, failed);
+        if (!ok) break;
         const uint32_t tile = (w ? v_at : k_at) + s * F::KV_TILE;
 #pragma unroll
         for (uint32_t i = 0; i < LOADS; ++i) {
-          const uint32_t r = (i % (TOK / HIGH)) * HIGH + lane % HIGH, piece = (i / (TOK / HIGH)) * F::WIDE + lane / HIGH;
-          const uint32_t in = first + r;
+          uint32_t in, piece;
+          at_load(i, &in, &piece);
+          const uint32_t to = tile + in * 128;
           auto put = [&](uint32_t d, uint32_t x, uint32_t y, uint32_t z, uint32_t t) {
-            const uint32_t to = tile + (d / 64) * F::PANEL + in * 128 + (((d / 8) ^ in) & 7) * 16;
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(x), "r"(y), "r"(z), "r"(t) : "memory");
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + (d / 64) * F::PANEL + (((d / 8) ^ in) & 7) * 16), "r"(x), "r"(y), "r"(z), "r"(t) : "memory");
           };
           const uint32_t word[4] = {code[w][i].x, code[w][i].y, code[w][i].z, code[w][i].w};
           if (MX) {
-            uint32_t pack = __shfl_sync(0xffffffffu, below[w][0], r);
-            if (PACKS > 1) { const uint32_t other = __shfl_sync(0xffffffffu, below[w][PACKS - 1], r); if (piece >= 4) pack = other; }
-            const int f = kChunkFactor - (int)(pack >> (8 * (piece & 3u)) & 255u);
-            const uint32_t h = w == 0 && (nan_key >> r & 1u) ? 0x7e00u : f < -24 ? 0u : f >= -14 ? (uint32_t)(f + 15) << 10 : 1u << (f + 24), factor = h | h << 16;
+            const uint32_t h = reinterpret_cast<const uint16_t*>(m + F::AT_SCALES)[(w * NB + piece) * F::FACTOR_LD + in], factor = h | h << 16;
 #pragma unroll
             for (uint32_t k = 0; k < 4; ++k) {
               uint32_t c[4];
@@ -714,8 +636,150 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
         if (lane == 0) bar_arrive(w ? v_full(s) : k_full(s));
-        if (more) fetch(w, id);
+        if (more) {
+          if (w == 0) ok = bar_wait(m_full((n + 1) % F::INFO), (n + 1) / F::INFO & 1, failed);
+          if (ok) fetch(w, m_next);
+        }
       }
+      if (!more) break;
+    }
+  } else if (warp < kProducts) {
+    // ---------------------------------------------------------------------------------- tokens
+    constexpr uint32_t PER = KT / (32 * kScout), WORDS = F::SCALE_WORDS, PACKS = MX ? (NB + 3) / 4 : 1;
+    const uint32_t part = warp - kFirstScout, first = part * 32 * PER + lane;     // this lane's tokens of a tile: first, first + 32
+    const uint32_t blocks = (a.c.dim + 31) / 32, row_bytes = MX ? 16 * blocks : a.c.dim;
+    struct Token {
+      int32_t id, id_next;                                                   // its page in this tile and in the next; negative: no such token
+      uint32_t scale_word[2][WORDS], lead;                                   // its scales, where they begin in their first word (keys, values)
+      uint64_t row;                                                          // in the cache
+    } tok[PER];
+    auto page_of = [&](uint32_t u, uint32_t q) -> int32_t {
+      const uint64_t j = (uint64_t)at.t.j0 + (uint64_t)u * KT + first + 32 * q;
+      if (u >= at.unit1 || j >= at.t.j1) return -1;
+      const int32_t id = __ldg(a.table + at.seq * a.table_ld + p.page.div((uint32_t)j));
+      return id >= 0 && (uint32_t)id < a.c.pages ? id : -1;
+    };
+    auto fetch_scales = [&](uint32_t u, uint32_t q) {
+      Token& k = tok[q];
+      const uint32_t j = at.t.j0 + u * KT + first + 32 * q, off = j - p.page.div(j) * p.page.d;
+      k.row = k.id < 0 ? 0 : ((uint64_t)(uint32_t)k.id * p.page.d + off) * a.c.heads + at.kv;
+      k.lead = 0;
+#pragma unroll
+      for (int w = 0; w < 2; ++w) {
+#pragma unroll
+        for (uint32_t i = 0; i < WORDS; ++i) k.scale_word[w][i] = 0;
+        if (k.id < 0) continue;
+        if (MX) {                                                            // whole words, each of which holds a wanted byte
+          const uintptr_t from = (uintptr_t)a.c.scales[w] + k.row * blocks;
+          const uint32_t l = (uint32_t)(from & 3u);
+          k.lead |= l << (4 * w);
+#pragma unroll
+          for (uint32_t i = 0; i < WORDS; ++i)
+            if (4 * i < l + blocks) k.scale_word[w][i] = __ldg(reinterpret_cast<const uint32_t*>(from & ~(uintptr_t)3u) + i);
+        } else k.scale_word[w][0] = __ldg(reinterpret_cast<const uint32_t*>(a.c.scales[w]) + k.row);
+      }
+    };
+    uint32_t u = at.unit;
+    auto begin_item = [&] {
+#pragma unroll
+      for (uint32_t q = 0; q < PER; ++q) { tok[q].id = page_of(u, q); tok[q].id_next = page_of(u + 1, q); }
+    };
+    begin_item();
+#pragma unroll
+    for (uint32_t q = 0; q < PER; ++q) fetch_scales(u, q);
+    int v_top = -126;
+    bool more = true;
+#pragma unroll 1
+    for (uint32_t n = 0; more; ++n) {
+      const uint32_t s = n % F::INFO, phase = (n / F::INFO & 1) ^ 1;
+      float scale[PER][2];
+      uint32_t bytes[PER][2][PACKS], high_byte[PER][2], real[PER], poisoned[PER];      // 4 bits: scales of the blocks, and the largest
+      int64_t here[PER];
+      int v_most = -126, flags = 0;
+      uint32_t k_most = 0;
+#pragma unroll
+      for (uint32_t q = 0; q < PER; ++q) {
+        const Token& k = tok[q];
+        real[q] = __ballot_sync(0xffffffffu, k.id >= 0);
+        here[q] = k.id >= 0 ? (int64_t)(k.row * row_bytes) : -1;
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+          high_byte[q][w] = 0;
+          scale[q][w] = MX ? 0.f : __uint_as_float(k.scale_word[w][0]);
+          if (!MX) continue;
+          const uint32_t shift = 8 * (k.lead >> (4 * w) & 3u);
+#pragma unroll
+          for (uint32_t i = 0; i < PACKS; ++i) {
+            bytes[q][w][i] = __funnelshift_r(k.scale_word[w][i], i + 1 < WORDS ? k.scale_word[w][i + 1 < WORDS ? i + 1 : 0] : 0u, shift);
+            const uint32_t have = blocks - min(blocks, 4 * i);
+            if (have < 4) bytes[q][w][i] &= (1u << (8 * have)) - 1u;
+#pragma unroll
+            for (uint32_t b = 0; b < 4; ++b) high_byte[q][w] = max(high_byte[q][w], bytes[q][w][i] >> (8 * b) & 255u);
+          }
+        }
+        // the largest exponents: 4 bits, of the tile's keys, as bytes; of the values (8 bits: finite scales are positive)
+        const uint32_t field = MX ? (high_byte[q][1] == 255u ? 0u : high_byte[q][1]) : (__float_as_uint(scale[q][1]) >> 23 & 255u);
+        if (field != 255u) v_most = max(v_most, min((int)field - 127, 126));
+        if (high_byte[q][0] != 255u) k_most = max(k_most, high_byte[q][0]);
+        poisoned[q] = __ballot_sync(0xffffffffu, MX && high_byte[q][1] == 255u);
+        flags |= (real[q] != 0xffffffffu) | (poisoned[q] != 0) << 1;         // some token is not there; some value is poisoned
+      }
+      v_most = __reduce_max_sync(0xffffffffu, v_most);
+      k_most = MX ? __reduce_max_sync(0xffffffffu, k_most) : 0;
+      if (lane == 0) { highest[n & 1][0][part] = (int)k_most | flags << 16; highest[n & 1][1][part] = v_most; }
+      // on to the next tile: its scales are fetched meanwhile
+      const bool new_item = ++u == at.unit1;
+      if (new_item) {
+        more = at.next(p);
+        u = at.unit;
+        if (more) begin_item();
+      } else {
+#pragma unroll
+        for (uint32_t q = 0; q < PER; ++q) { tok[q].id = tok[q].id_next; tok[q].id_next = page_of(u + 1, q); }
+      }
+      if (more) {
+#pragma unroll
+        for (uint32_t q = 0; q < PER; ++q) fetch_scales(u, q);
+      }
+      if (!all_scouts(bar_wait(m_empty(s), phase, failed))) break;
+      int k_top = 1, any_flag = 0;
+#pragma unroll
+      for (uint32_t k = 0; k < kScout; ++k) {
+        const int v = highest[n & 1][0][k];
+        k_top = max(k_top, v & 0xffff); any_flag |= v >> 16;
+        v_top = max(v_top, highest[n & 1][1][k]);
+      }
+      uint8_t* const m = meta + s * F::META;
+#pragma unroll
+      for (uint32_t q = 0; q < PER; ++q) {
+        const uint32_t in = first + 32 * q;
+        reinterpret_cast<int64_t*>(m)[in] = here[q];
+        if (MX) {
+          const bool nan_key = high_byte[q][0] == 255u, no_value = high_byte[q][1] == 255u;
+#pragma unroll
+          for (uint32_t b = 0; b < NB; ++b)
+#pragma unroll
+            for (int w = 0; w < 2; ++w) {
+              // 2^(own - largest + kChunkFactor) in binary16, down to its smallest number 2^-24
+              const int f = (int)(bytes[q][w][MX ? b / 4 : 0] >> (8 * (b % 4)) & 255u) - (w ? v_top + 127 : k_top) + kChunkFactor;
+              uint32_t h = f < -24 ? 0u : f >= -14 ? (uint32_t)(min(f, kChunkFactor) + 15) << 10 : 1u << (f + 24);
+              if (w == 0 && nan_key) h = 0x7e00u;
+              if (w == 1 && no_value) h = 0;
+              reinterpret_cast<uint16_t*>(m + F::AT_SCALES)[(w * NB + b) * F::FACTOR_LD + in] = (uint16_t)h;
+            }
+        } else {
+          reinterpret_cast<float*>(m + F::AT_SCALES)[in] = scale[q][0];
+          reinterpret_cast<float*>(m + F::AT_SCALES + 4 * KT)[in] = scale[q][1] * power_of_two(-v_top);
+        }
+        if (lane == 0) {
+          reinterpret_cast<uint32_t*>(m + F::AT_BITS)[part * PER + q] = real[q];
+          reinterpret_cast<uint32_t*>(m + F::AT_BITS + 16)[part * PER + q] = poisoned[q];
+        }
+      }
+      if (part == 0 && lane == 0) *reinterpret_cast<int4*>(m + F::AT_BITS + 32) = make_int4(k_top - 127, v_top, (any_flag ^ 1) | (more ? 0 : 4), 0);
+      __syncwarp();
+      if (lane == 0) bar_arrive(m_full(s));
+      if (new_item) v_top = -126;
     }
   } else {
     // ---------------------------------------------------------------------------------- products
@@ -755,7 +819,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
           tc_fence_after();
           if (elect_one()) {
             results(t, n % 2, u > 0);
-            if (t + 1 == nt) tensor_commit(v_empty(n % 2));
+            if (t + 1 == nt) { tensor_commit(v_empty(n % 2)); tensor_commit(m_empty(n % F::INFO)); }
           }
           __syncwarp();
           if (!more) continue;
@@ -782,7 +846,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
   __syncthreads();
   tc_fence_after();
   if (tid == 0 && *failed) { *p.fault = 1; __threadfence_system(); }
-  if (warp == 12) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+  if (warp == kProducts) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
 }
 
 constexpr int kDevices = 64;
