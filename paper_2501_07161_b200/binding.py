@@ -745,33 +745,39 @@ class Context:
             raise ValueError("free_count must be one int64")
         seqs, (_, width) = lens.shape[0], table.shape
         same = self._on_stream(lens, fresh, table, free_pages, free_count)
-        sizes = {"lens": seqs, "q_starts": seqs + 1, "starts": seqs + 1, "slots": total, "positions": total, "free_count": 1, "missing": 1}
-        if out is None:
-            out = PagePlan(*(self._new(same, (n,), torch.int64) for n in sizes.values()))
+        sizes = (seqs, seqs + 1, seqs + 1, total, total, 1, 1)           # in PagePlan's order
+        if out is None:                                                  # parts of one allocation
+            whole = self._new(same, (3 * seqs + 2 * total + 4,), torch.int64)
+            out = PagePlan(*whole.split_with_sizes(sizes))
+            a = whole.data_ptr()
+            where = (a, a + 8 * seqs, a + 16 * seqs + 8, a + 24 * seqs + 16, a + 24 * seqs + 16 + 8 * total, a + 24 * seqs + 16 + 16 * total,
+                     a + 24 * seqs + 24 + 16 * total)
         else:
-            for name, n in sizes.items():
-                t = getattr(out, name)
+            given = (out.lens, out.q_starts, out.starts, out.slots, out.positions, out.free_count, out.missing)
+            for t, n in zip(given, sizes):
                 if t.dtype != torch.int64 or t.shape != (n,) or not t.is_contiguous():
-                    raise ValueError(f"out.{name} must be dense int64 [{n}]")
-            self._on_stream(*(getattr(out, name) for name in sizes))
+                    raise ValueError("out's tensors must be dense int64 of the plan's sizes")
+            self._on_stream(*given)
+            where = [t.data_ptr() for t in given]
         p = PagePlanC(lens.data_ptr(), fresh.data_ptr(), table.data_ptr(), max(table.stride(0), width), width, free_pages.data_ptr(), free_pages.numel(),
-                      free_count.data_ptr(), out.lens.data_ptr(), out.q_starts.data_ptr(), out.starts.data_ptr(), out.slots.data_ptr(),
-                      out.positions.data_ptr(), out.free_count.data_ptr(), out.missing.data_ptr(), total, seqs, page_size)
+                      free_count.data_ptr(), *where, total, seqs, page_size)
         _check(lib().qv2_kv_plan(self._h, p), "qv2_kv_plan")
         return out
 
-    def _head_rows(self, x, weight, out, same, dim):
-        if x is None:
-            return None, None
+    def _head_rows(self, x, weight, out, same, shape):
+        dim = shape[2]
         if weight is not None and (weight.dtype != torch.float32 or weight.shape != (dim,) or not weight.is_contiguous()):
             raise ValueError("weights must be dense float32 [dim]")
+        t, h, one = x.stride()
         if out is None:
-            out = self._new(same, x.shape, x.dtype)
-        elif out.shape != x.shape or out.dtype != x.dtype:
-            raise ValueError("an output must have its input's shape and type")
-        if dim > 1 and (x.stride(2) != 1 or out.stride(2) != 1):
+            out, u, v, unit = self._new(same, shape, x.dtype), shape[1] * dim, dim, 1
+        else:
+            if out.shape != shape or out.dtype != x.dtype:
+                raise ValueError("an output must have its input's shape and type")
+            u, v, unit = out.stride()
+        if dim > 1 and (one != 1 or unit != 1):
             raise ValueError("the elements of a head must be consecutive")
-        return out, HeadRowsC(x.data_ptr(), out.data_ptr(), x.stride(0), x.stride(1), out.stride(0), out.stride(1), _ptr(weight), x.shape[1])
+        return out, HeadRowsC(x.data_ptr(), out.data_ptr(), t, h, u, v, None if weight is None else weight.data_ptr(), shape[1])
 
     def norm_rotate(self, q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Tensor, freqs: Optional[torch.Tensor],
                     q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6, pairs: bool = False,
@@ -780,22 +786,31 @@ class Context:
         weight (float32 [dim]) is given, then the first 2 * len(freqs) elements of each head turned by positions (int64 [tokens])
         times freqs (float32), in pairs (i, i + len(freqs)) or, with `pairs`, (2i, 2i + 1).  -> (q, k), new
         tensors unless `out` = (q, k) gives them; they may be the inputs themselves."""
-        if q.dim() != 3 or (k is not None and (k.dim() != 3 or k.shape[0] != q.shape[0] or k.shape[2] != q.shape[2] or k.dtype != q.dtype)):
-            raise ValueError("queries and keys must be [tokens, heads, dim] of the same tokens, size and type")
-        type_ = _DTYPE_FLAG.get(q.dtype)
+        type_, shape = _DTYPE_FLAG.get(q.dtype), q.shape
         if type_ is None:
             raise TypeError("queries and keys must be float32, float16 or bfloat16")
-        tokens, _, dim = q.shape
+        if len(shape) != 3:
+            raise ValueError("queries must be [tokens, heads, dim]")
+        tokens, _, dim = shape
+        if k is not None:
+            k_shape = k.shape
+            if len(k_shape) != 3 or k_shape[0] != tokens or k_shape[2] != dim or k.dtype != q.dtype:
+                raise ValueError("queries and keys must be [tokens, heads, dim] of the same tokens, size and type")
         if positions.dtype != torch.int64 or positions.shape != (tokens,) or not positions.is_contiguous():
             raise ValueError("positions must be dense int64 [tokens]")
-        if freqs is not None and (freqs.dtype != torch.float32 or freqs.dim() != 1 or not freqs.is_contiguous()):
-            raise ValueError("freqs must be dense float32")
-        yq, yk = out if out is not None else (None, None)
+        rot = 0
+        if freqs is not None:
+            if freqs.dtype != torch.float32 or freqs.dim() != 1 or not freqs.is_contiguous():
+                raise ValueError("freqs must be dense float32")
+            rot = 2 * freqs.numel()
+        yq, yk = (None, None) if out is None else out
         same = self._on_stream(q, k, positions, freqs, q_weight, k_weight, yq, yk)
-        yq, qc = self._head_rows(q, q_weight, yq, same, dim)
-        yk, kc = self._head_rows(k, k_weight, yk, same, dim)
-        _check(lib().qv2_norm_rotate(self._h, qc, kc, type_, dim, 0 if freqs is None else 2 * freqs.numel(), ROTATE_PAIRS if pairs else ROTATE_HALVES, eps,
-                                     tokens, positions.data_ptr(), _ptr(freqs)), "qv2_norm_rotate")
+        yq, qc = self._head_rows(q, q_weight, yq, same, shape)
+        kc = None
+        if k is not None:
+            yk, kc = self._head_rows(k, k_weight, yk, same, k_shape)
+        _check(lib().qv2_norm_rotate(self._h, qc, kc, type_, dim, rot, ROTATE_PAIRS if pairs else ROTATE_HALVES, eps, tokens, positions.data_ptr(),
+                                     None if freqs is None else freqs.data_ptr()), "qv2_norm_rotate")
         return yq, yk
 
     def kv_attend(self, cache: KvCache, q: torch.Tensor, q_starts: torch.Tensor, lens: torch.Tensor, table: torch.Tensor,

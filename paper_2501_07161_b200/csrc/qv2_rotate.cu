@@ -1,9 +1,11 @@
 // RMS norm of every head and the rotation by position, queries and keys in one launch.
 //
-// Bound by its bytes, each read and written once.  Eight elements to a lane, so 8, 16 or 32 lanes hold a row of up to 64, 128
-// or 256; the sum of squares stays in their registers.  A CTA takes all heads of a few tokens and works out the sines and cosines
-// of those tokens once for all heads: the angle is a product of binary64, reduced there to a part of a turn, and only then
-// narrowed, so that positions in the millions keep their phase.
+// Bound by its bytes, each read and written once.  A lane has eight elements of a row that are four pairs of the rotation: neighbours, or
+// (halves) four elements and the four rot / 2 further on, so nothing but the sum of squares leaves the lane; 8, 16 or 32 lanes hold
+// a row of up to 64, 128 or 256.  (Eight neighbouring elements to a lane and the other half by shuffles took 260 instructions for
+// them, and the time that those take: 129 us for 16384 tokens of 40 heads x 128 in 16 bits.)  A CTA takes all heads of a few
+// tokens and works out the sines and cosines of those tokens once for all heads: the angle is a product of binary64, reduced there to
+// a part of a turn, and only then narrowed, so that positions in the millions keep their phase.
 #include "qv2_serve.cuh"
 
 namespace qv2 {
@@ -12,134 +14,188 @@ namespace {
 
 constexpr int kRotateThreads = 256, kRotateRows = 4;       // rows in flight per lane
 constexpr uint32_t kRotateMaxTokens = 8;                   // tokens of a CTA
-enum { kPairs = 0, kHalvesChunk = 1, kHalvesAny = 2 };     // where the other element of a pair is: same lane, same place of another lane, anywhere
 
-template <class T, int LPR, int MODE>
-__global__ void __launch_bounds__(kRotateThreads)
-norm_rotate_kernel(HeadRows h, Rotation r, uint32_t tokens_per_cta, FastDiv heads, FastDiv half_div, uint32_t vec_in, uint32_t vec_out) {
-  extern __shared__ float2 turns[];                        // [token][rot / 2], then (kHalvesAny) a row of binary32 per group of lanes
+// Four consecutive elements as loaded, and back.
+template <class T> struct Quad;
+template <> struct Quad<float> {
+  float4 a;
+  __device__ __forceinline__ void load(const float* p) { a = Chunk8<float>::load4(p); }
+  __device__ __forceinline__ void gather(const float* p) { a = make_float4(__ldg(p), __ldg(p + 1), __ldg(p + 2), __ldg(p + 3)); }
+  __device__ __forceinline__ void widen(float* v) const { v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; }
+  static __device__ __forceinline__ void store(float* p, const float* v) { *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]); }
+};
+template <class T> struct Quad {
+  uint32_t w[2];
+  __device__ __forceinline__ void load(const T* p) {
+    asm volatile("ld.global.nc.L1::no_allocate.v2.u32 {%0,%1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(p));      // volatile: stays behind dependency_wait()
+  }
+  __device__ __forceinline__ void gather(const T* p) {
+    const unsigned short* q = reinterpret_cast<const unsigned short*>(p);
+    w[0] = __ldg(q) | (uint32_t)__ldg(q + 1) << 16; w[1] = __ldg(q + 2) | (uint32_t)__ldg(q + 3) << 16;
+  }
+  __device__ __forceinline__ void widen(float* v) const {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      if constexpr (std::is_same<T, __half>::value) {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+        v[2 * i] = f.x; v[2 * i + 1] = f.y;
+      } else { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+    }
+  }
+  static __device__ __forceinline__ void store(T* p, const float* v) { *reinterpret_cast<uint2*>(p) = make_uint2(Chunk8<T>::pack(v[0], v[1]), Chunk8<T>::pack(v[2], v[3])); }
+};
+
+// QUADS: rows of a multiple of 8 elements, rot / 2 of 4.  Otherwise a lane has eight neighbouring elements and halves meet in shared memory.
+// VEC: rows on 16-byte addresses, in and out, strides below 2^20.  (How rows lie changes nothing of what is added to what.)
+template <class T, int LPR, bool PAIRS, bool QUADS, bool VEC>
+__global__ void __launch_bounds__(kRotateThreads, VEC && LPR == 16 ? 4 : 1)
+norm_rotate_kernel(HeadRows h, Rotation r, uint32_t tokens_per_cta, FastDiv heads_q, FastDiv heads_k, FastDiv half_div) {
+  extern __shared__ float4 turns_raw[];                    // [token][rot / 2] cosines and sines, then (halves, not QUADS) a row of binary32 per group of lanes
+  float2* const turns = reinterpret_cast<float2*>(turns_raw);
   constexpr uint32_t GROUPS = kRotateThreads / LPR;
-  const uint32_t half = r.rot / 2, c = threadIdx.x % LPR, group = threadIdx.x / LPR, d0 = 8 * c;
+  const uint32_t half = r.rot / 2, c = threadIdx.x % LPR, group = threadIdx.x / LPR;
   const uint64_t token0 = (uint64_t)blockIdx.x * tokens_per_cta;
-  const uint32_t tokens = (uint32_t)min((uint64_t)tokens_per_cta, r.tokens - token0), n_rows = tokens * heads.d;
-  float* const row_buf = reinterpret_cast<float*>(turns + tokens_per_cta * half) + group * LPR * 8;
+  const uint32_t tokens = (uint32_t)min((uint64_t)tokens_per_cta, r.tokens - token0);
+  const uint32_t pitch = half + (half & 1u);               // rows of turns start on 16-byte addresses
+  float* const row_buf = reinterpret_cast<float*>(turns + tokens_per_cta * pitch) + group * LPR * 8;
+  // this lane's elements: d0 .. d0 + 3 and d1 .. d1 + 3
+  const bool turned = QUADS ? (PAIRS ? 8 * c < r.rot : 4 * c < half) : false;
+  const uint32_t d0 = !QUADS || PAIRS ? 8 * c : turned ? 4 * c : r.rot + 8 * (c - half / 4), d1 = QUADS && !PAIRS && turned ? half + 4 * c : d0 + 4;
+  const bool in = d0 < r.dim;
   dependency_wait();
   allow_dependents();
 
-  Chunk8<T> e[kRotateRows];
-  uint32_t which[kRotateRows], token[kRotateRows], head[kRotateRows];
-  auto load = [&](uint32_t base) {
-#pragma unroll
-    for (int u = 0; u < kRotateRows; ++u) {
-      const uint32_t row = base + u * GROUPS + group;
-      e[u].zero();
-      which[u] = token[u] = head[u] = 0;
-      if (row >= n_rows) continue;
-      token[u] = heads.div(row);
-      head[u] = row - token[u] * heads.d;
-      which[u] = head[u] >= h.heads[0];
-      if (which[u]) head[u] -= h.heads[0];
-      const T* p = (const T*)h.x[which[u]] + (token0 + token[u]) * h.x_token_ld[which[u]] + head[u] * h.x_head_ld[which[u]] + d0;
-      if (d0 + 8 <= r.dim) { if (vec_in >> which[u] & 1) e[u].load_vec(p); else e[u].load_any(p); }
-      else if (d0 < r.dim) e[u].load_some(p, r.dim - d0);
-    }
-  };
-  load(0);
-  float w[2][8];
-#pragma unroll
-  for (int a = 0; a < 2; ++a)
-#pragma unroll
-    for (uint32_t k = 0; k < 8; ++k) w[a][k] = h.weight[a] && d0 + k < r.dim ? __ldg(h.weight[a] + d0 + k) : 1.f;
   for (uint32_t i = threadIdx.x; i < tokens * half; i += kRotateThreads) {
-    const uint32_t t = half_div.div(i);
-    const double turn = (double)__ldg(r.positions + token0 + t) * (double)__ldg(r.freqs + (i - t * half)) * 0.15915494309189535;   // 1 / (2 pi)
+    const uint32_t t = half_div.div(i), k = i - t * half;
+    const double turn = (double)__ldg(r.positions + token0 + t) * (double)__ldg(r.freqs + k) * 0.15915494309189535;   // 1 / (2 pi)
     float s, co;
     sincospif((float)(2.0 * (turn - rint(turn))), &s, &co);
-    turns[i] = make_float2(co, s);
+    turns[t * pitch + k] = make_float2(co, s);
   }
   __syncthreads();
-  for (uint32_t base = 0; base < n_rows; ) {
+  const float per = 1.f / (float)r.dim;
+  auto run = [&](const int a, const FastDiv& heads) {      // queries, keys
+    const uint32_t n_rows = tokens * h.heads[a];
+    if (n_rows == 0) return;
+    const T* const x = (const T*)h.x[a] + token0 * h.x_token_ld[a];
+    T* const y = (T*)h.y[a] + token0 * h.y_token_ld[a];
+    using Step = typename std::conditional<VEC, uint32_t, uint64_t>::type;
+    const Step xt = (Step)h.x_token_ld[a], xh = (Step)h.x_head_ld[a], yt = (Step)h.y_token_ld[a], yh = (Step)h.y_head_ld[a];
+    const float* const weight = h.weight[a];
+    float w[8];
 #pragma unroll
-    for (int u = 0; u < kRotateRows; ++u) {
-      if (base + u * GROUPS >= n_rows) continue;           // the same for all lanes of the CTA
-      const bool keys = which[u] != 0;
-      float v[8];
-      e[u].widen(v);
-      if (h.weight[0] || h.weight[1]) {
-        float sum = 0.f;
+    for (uint32_t k = 0; k < 8; ++k) {
+      const uint32_t d = (k < 4 ? d0 : d1 - 4) + k;
+      w[k] = weight && d < r.dim ? __ldg(weight + d) : 1.f;
+    }
+    for (uint32_t base = 0; base < n_rows; base += kRotateRows * GROUPS) {
+      Quad<T> lo[kRotateRows], hi[kRotateRows];
+      Chunk8<T> e[kRotateRows];
+      uint32_t token[kRotateRows], head[kRotateRows];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) sum = fmaf(v[k], v[k], sum);
-#pragma unroll
-        for (int o = LPR / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        if (h.weight[keys]) {
-          const float f = 1.f / sqrtf(sum / (float)r.dim + r.eps);
-#pragma unroll
-          for (int k = 0; k < 8; ++k) v[k] = v[k] * f * (keys ? w[1][k] : w[0][k]);
+      for (int u = 0; u < kRotateRows; ++u) {
+        // Loads without a branch stay in flight together: rows and elements that are not there take others' (elements become zeros below).
+        const uint32_t row = min(base + u * GROUPS + group, n_rows - 1);
+        token[u] = heads.div(row);
+        head[u] = row - token[u] * heads.d;
+        const T* p = x + token[u] * xt + head[u] * xh;
+        if (VEC) { lo[u].load(p + (in ? d0 : 0)); hi[u].load(p + (in ? d1 : 0)); }
+        else if (QUADS) { lo[u].gather(p + (in ? d0 : 0)); hi[u].gather(p + (in ? d1 : 0)); }
+        else {
+          e[u].zero();
+          if (d0 + 8 <= r.dim) e[u].load_any(p + d0);
+          else if (in) e[u].load_some(p + d0, r.dim - d0);
         }
       }
-      const float2* cs = turns + token[u] * half;
-      if (MODE == kPairs) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-          if (d0 + 2 * k < r.rot) {
-            const float2 t = cs[d0 / 2 + k];
-            const float a = v[2 * k], b = v[2 * k + 1];
-            v[2 * k] = a * t.x - b * t.y;
-            v[2 * k + 1] = b * t.x + a * t.y;
-          }
-      } else if (MODE == kHalvesChunk) {
-        const uint32_t hc = half / 8;
-        const bool first = c < hc, in = c < 2 * hc;
-        const uint32_t other = first ? c + hc : in ? c - hc : c;
+      for (int u = 0; u < kRotateRows; ++u) {
+        if (base + u * GROUPS >= n_rows) continue;         // the same for all lanes of the CTA
+        float v[8];
+        if (QUADS) { lo[u].widen(v); hi[u].widen(v + 4); }
+        else e[u].widen(v);
+        if (weight) {
+          float sum = 0.f;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const float b = __shfl_sync(0xffffffffu, v[k], other, LPR);
-          if (in) {
-            const float2 t = cs[(first ? d0 : d0 - half) + k];
-            v[k] = first ? v[k] * t.x - b * t.y : v[k] * t.x + b * t.y;
-          }
+          for (int k = 0; k < 8; ++k) sum = fmaf(v[k], v[k], sum);
+          if (QUADS && !in) sum = 0.f;
+#pragma unroll
+          for (int o = LPR / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+          const float f = rsqrtf(fmaf(sum, per, r.eps));
+#pragma unroll
+          for (int k = 0; k < 8; ++k) v[k] = v[k] * f * w[k];
         }
-      } else {
+        const float2* cs = turns + token[u] * pitch;
+        if (QUADS) {
+          if (turned) {
+            const float4* t4 = reinterpret_cast<const float4*>(cs + 4 * c);
+            const float4 t0 = t4[0], t1 = t4[1];
+            const float co[4] = {t0.x, t0.z, t1.x, t1.z}, s[4] = {t0.y, t0.w, t1.y, t1.w};
 #pragma unroll
-        for (int k = 0; k < 8; ++k) row_buf[d0 + k] = v[k];
-        __syncwarp();
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const uint32_t d = d0 + k;
-          if (d < r.rot) {
-            const bool first = d < half;
-            const float2 t = cs[first ? d : d - half];
-            const float b = row_buf[first ? d + half : d - half];
-            v[k] = first ? v[k] * t.x - b * t.y : v[k] * t.x + b * t.y;
+            for (int k = 0; k < 4; ++k) {
+              float &a0 = v[PAIRS ? 2 * k : k], &b0 = v[PAIRS ? 2 * k + 1 : k + 4];
+              const float p = a0, q = b0;
+              a0 = p * co[k] - q * s[k];
+              b0 = q * co[k] + p * s[k];
+            }
           }
+        } else if (PAIRS) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (d0 + 2 * k < r.rot) {
+              const float2 t = cs[d0 / 2 + k];
+              const float p = v[2 * k], q = v[2 * k + 1];
+              v[2 * k] = p * t.x - q * t.y;
+              v[2 * k + 1] = q * t.x + p * t.y;
+            }
+        } else {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) row_buf[d0 + k] = v[k];
+          __syncwarp();
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const uint32_t d = d0 + k;
+            if (d < r.rot) {
+              const bool first = d < half;
+              const float2 t = cs[first ? d : d - half];
+              const float q = row_buf[first ? d + half : d - half];
+              v[k] = first ? v[k] * t.x - q * t.y : v[k] * t.x + q * t.y;
+            }
+          }
+          __syncwarp();
         }
-        __syncwarp();
-      }
-      if (base + u * GROUPS + group < n_rows && d0 < r.dim) {
-        T* p = (T*)h.y[keys] + (token0 + token[u]) * h.y_token_ld[keys] + head[u] * h.y_head_ld[keys] + d0;
-        if (vec_out >> which[u] & 1) Chunk8<T>::store_vec(p, v);
-        else store_some(p, v, r.dim - d0);
+        if (base + u * GROUPS + group < n_rows && in) {
+          T* p = y + token[u] * yt + head[u] * yh;
+          if (VEC) { Quad<T>::store(p + d0, v); Quad<T>::store(p + d1, v + 4); }
+          else if (QUADS) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) p[(k < 4 ? d0 : d1 - 4) + k] = Chunk8<T>::narrow(v[k]);
+          } else store_some(p + d0, v, r.dim - d0);
+        }
       }
     }
-    base += kRotateRows * GROUPS;
-    if (base < n_rows) load(base);
-  }
+  };
+  run(0, heads_q);
+  run(1, heads_k);
 }
 
 template <class T, int LPR>
 cudaError_t rotate_rows(const Launch& l, const HeadRows& h, const Rotation& r, uint64_t* launches) {
-  const uint32_t heads = h.heads[0] + h.heads[1], half = r.rot / 2;
-  uint32_t vec_in = 0, vec_out = 0;
-  for (int a = 0; a < 2; ++a) {
-    if ((uintptr_t)h.x[a] % 16 == 0 && h.x_token_ld[a] * sizeof(T) % 16 == 0 && h.x_head_ld[a] * sizeof(T) % 16 == 0) vec_in |= 1u << a;
-    if (r.dim % 8 == 0 && (uintptr_t)h.y[a] % 16 == 0 && h.y_token_ld[a] * sizeof(T) % 16 == 0 && h.y_head_ld[a] * sizeof(T) % 16 == 0) vec_out |= 1u << a;
-  }
+  const uint32_t half = r.rot / 2;
+  const bool quads = r.dim % 8 == 0 && half % 4 == 0;
+  uintptr_t where = quads ? 0 : 1;
+  for (int a = 0; a < 2; ++a)
+    if (h.heads[a]) {
+      if ((h.x_token_ld[a] | h.x_head_ld[a] | h.y_token_ld[a] | h.y_head_ld[a]) >> 20 || h.heads[a] > 2048) where |= 1;
+      where |= (uintptr_t)h.x[a] | (uintptr_t)h.y[a] | (h.x_token_ld[a] | h.x_head_ld[a] | h.y_token_ld[a] | h.y_head_ld[a]) * sizeof(T);
+    }
+  const bool vec = where % 16 == 0;
   const uint64_t spread = r.tokens / (8 * (uint64_t)l.sm_count);                 // eight CTAs per SM where there are tokens for them
   const uint32_t tokens = (uint32_t)(spread < 1 ? 1 : spread > kRotateMaxTokens ? kRotateMaxTokens : spread);
-  const int mode = r.pairs ? kPairs : half % 8 == 0 ? kHalvesChunk : kHalvesAny;
-  const size_t smem = sizeof(float2) * tokens * half + (mode == kHalvesAny ? sizeof(float) * kRotateThreads * 8 : 0);
-  auto* kernel = mode == kPairs ? norm_rotate_kernel<T, LPR, kPairs> : mode == kHalvesChunk ? norm_rotate_kernel<T, LPR, kHalvesChunk> : norm_rotate_kernel<T, LPR, kHalvesAny>;
-  cudaError_t e = launch_grid(l, kernel, dim3((uint32_t)((r.tokens + tokens - 1) / tokens)), kRotateThreads, smem, h, r, tokens, FastDiv(heads), FastDiv(half ? half : 1), vec_in, vec_out);
+  const size_t smem = sizeof(float2) * tokens * (half + half % 2) + (!quads && !r.pairs ? sizeof(float) * kRotateThreads * 8 : 0);
+  auto* kernel = r.pairs ? (vec ? norm_rotate_kernel<T, LPR, true, true, true> : quads ? norm_rotate_kernel<T, LPR, true, true, false> : norm_rotate_kernel<T, LPR, true, false, false>)
+                         : (vec ? norm_rotate_kernel<T, LPR, false, true, true> : quads ? norm_rotate_kernel<T, LPR, false, true, false> : norm_rotate_kernel<T, LPR, false, false, false>);
+  auto heads = [&](int a) { return FastDiv(h.heads[a] ? h.heads[a] : 1); };
+  cudaError_t e = launch_grid(l, kernel, dim3((uint32_t)((r.tokens + tokens - 1) / tokens)), kRotateThreads, smem, h, r, tokens, heads(0), heads(1), FastDiv(half ? half : 1));
   if (e == cudaSuccess) ++*launches;
   return e;
 }

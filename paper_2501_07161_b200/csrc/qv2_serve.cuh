@@ -1,6 +1,8 @@
 // Page planning and norm with rotation: what their kernels are given, and the launch wrappers.
 #pragma once
 
+#include <type_traits>
+
 #include "qv2_mx.cuh"
 
 namespace qv2 {
