@@ -50,14 +50,14 @@ template <class T> struct Quad {
 template <class T, int LPR, bool PAIRS, bool QUADS, bool VEC>
 __global__ void __launch_bounds__(kRotateThreads, VEC && LPR == 16 ? 4 : 1)
 norm_rotate_kernel(HeadRows h, Rotation r, uint32_t tokens_per_cta, FastDiv heads_q, FastDiv heads_k, FastDiv half_div) {
-  extern __shared__ float4 turns_raw[];                    // [token][rot / 2] cosines and sines, then (halves, not QUADS) a row of binary32 per group of lanes
-  float2* const turns = reinterpret_cast<float2*>(turns_raw);
+  extern __shared__ float4 turns_raw[];                    // [token][cosines, sines][pitch], then (halves, not QUADS) a row of binary32 per group of lanes
+  float* const turns = reinterpret_cast<float*>(turns_raw);
   constexpr uint32_t GROUPS = kRotateThreads / LPR;
   const uint32_t half = r.rot / 2, c = threadIdx.x % LPR, group = threadIdx.x / LPR;
   const uint64_t token0 = (uint64_t)blockIdx.x * tokens_per_cta;
   const uint32_t tokens = (uint32_t)min((uint64_t)tokens_per_cta, r.tokens - token0);
-  const uint32_t pitch = half + (half & 1u);               // rows of turns start on 16-byte addresses
-  float* const row_buf = reinterpret_cast<float*>(turns + tokens_per_cta * pitch) + group * LPR * 8;
+  const uint32_t pitch = (half + 3) / 4 * 4;               // 16-byte addresses
+  float* const row_buf = turns + 2 * tokens_per_cta * pitch + group * LPR * 8;
   // this lane's elements: d0 .. d0 + 3 and d1 .. d1 + 3
   const bool turned = QUADS ? (PAIRS ? 8 * c < r.rot : 4 * c < half) : false;
   const uint32_t d0 = !QUADS || PAIRS ? 8 * c : turned ? 4 * c : r.rot + 8 * (c - half / 4), d1 = QUADS && !PAIRS && turned ? half + 4 * c : d0 + 4;
@@ -70,7 +70,8 @@ norm_rotate_kernel(HeadRows h, Rotation r, uint32_t tokens_per_cta, FastDiv head
     const double turn = (double)__ldg(r.positions + token0 + t) * (double)__ldg(r.freqs + k) * 0.15915494309189535;   // 1 / (2 pi)
     float s, co;
     sincospif((float)(2.0 * (turn - rint(turn))), &s, &co);
-    turns[t * pitch + k] = make_float2(co, s);
+    turns[2 * t * pitch + k] = co;
+    turns[(2 * t + 1) * pitch + k] = s;
   }
   __syncthreads();
   const float per = 1.f / (float)r.dim;
@@ -113,39 +114,46 @@ norm_rotate_kernel(HeadRows h, Rotation r, uint32_t tokens_per_cta, FastDiv head
         float v[8];
         if (QUADS) { lo[u].widen(v); hi[u].widen(v + 4); }
         else e[u].widen(v);
+        float f = 1.f;
         if (weight) {
-          float sum = 0.f;
+          float sum = v[0] * v[0], more = v[1] * v[1];
 #pragma unroll
-          for (int k = 0; k < 8; ++k) sum = fmaf(v[k], v[k], sum);
+          for (int k = 2; k < 8; k += 2) { sum = fmaf(v[k], v[k], sum); more = fmaf(v[k + 1], v[k + 1], more); }
+          sum += more;
           if (QUADS && !in) sum = 0.f;
 #pragma unroll
           for (int o = LPR / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-          const float f = rsqrtf(fmaf(sum, per, r.eps));
+          f = rsqrtf(fmaf(sum, per, r.eps));
 #pragma unroll
-          for (int k = 0; k < 8; ++k) v[k] = v[k] * f * w[k];
+          for (int k = 0; k < 8; k += 2) mul2(v[k], v[k + 1], w[k], w[k + 1]);
         }
-        const float2* cs = turns + token[u] * pitch;
+        const float *const co = turns + 2 * token[u] * pitch, *const si = co + pitch;
         if (QUADS) {
           if (turned) {
-            const float4* t4 = reinterpret_cast<const float4*>(cs + 4 * c);
-            const float4 t0 = t4[0], t1 = t4[1];
-            const float co[4] = {t0.x, t0.z, t1.x, t1.z}, s[4] = {t0.y, t0.w, t1.y, t1.w};
+            const float4 c4 = *reinterpret_cast<const float4*>(co + 4 * c), s4 = *reinterpret_cast<const float4*>(si + 4 * c);
+            if (PAIRS) {
+              const float ck[4] = {c4.x, c4.y, c4.z, c4.w}, sk[4] = {s4.x, s4.y, s4.z, s4.w};
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              float &a0 = v[PAIRS ? 2 * k : k], &b0 = v[PAIRS ? 2 * k + 1 : k + 4];
-              const float p = a0, q = b0;
-              a0 = p * co[k] - q * s[k];
-              b0 = q * co[k] + p * s[k];
+              for (int k = 0; k < 4; ++k) {
+                const float p = v[2 * k], q = v[2 * k + 1];
+                v[2 * k] = fmaf(p, ck[k], -(q * sk[k]));
+                v[2 * k + 1] = fmaf(q, ck[k], p * sk[k]);
+              }
+            } else {                                       // p cos - q sin, q cos + p sin
+              float ps[4] = {v[0], v[1], v[2], v[3]}, qs[4] = {-v[4], -v[5], -v[6], -v[7]};
+              mul2(ps[0], ps[1], s4.x, s4.y); mul2(ps[2], ps[3], s4.z, s4.w);
+              mul2(qs[0], qs[1], s4.x, s4.y); mul2(qs[2], qs[3], s4.z, s4.w);
+              fma2(v[0], v[1], c4.x, c4.y, qs[0], qs[1]); fma2(v[2], v[3], c4.z, c4.w, qs[2], qs[3]);
+              fma2(v[4], v[5], c4.x, c4.y, ps[0], ps[1]); fma2(v[6], v[7], c4.z, c4.w, ps[2], ps[3]);
             }
           }
         } else if (PAIRS) {
 #pragma unroll
           for (int k = 0; k < 4; ++k)
             if (d0 + 2 * k < r.rot) {
-              const float2 t = cs[d0 / 2 + k];
-              const float p = v[2 * k], q = v[2 * k + 1];
-              v[2 * k] = p * t.x - q * t.y;
-              v[2 * k + 1] = q * t.x + p * t.y;
+              const float ck = co[d0 / 2 + k], sk = si[d0 / 2 + k], p = v[2 * k], q = v[2 * k + 1];
+              v[2 * k] = fmaf(p, ck, -(q * sk));
+              v[2 * k + 1] = fmaf(q, ck, p * sk);
             }
         } else {
 #pragma unroll
@@ -156,12 +164,15 @@ norm_rotate_kernel(HeadRows h, Rotation r, uint32_t tokens_per_cta, FastDiv head
             const uint32_t d = d0 + k;
             if (d < r.rot) {
               const bool first = d < half;
-              const float2 t = cs[first ? d : d - half];
-              const float q = row_buf[first ? d + half : d - half];
-              v[k] = first ? v[k] * t.x - q * t.y : v[k] * t.x + q * t.y;
+              const float ck = co[first ? d : d - half], sk = si[first ? d : d - half], q = row_buf[first ? d + half : d - half];
+              v[k] = fmaf(v[k], ck, first ? -(q * sk) : q * sk);
             }
           }
           __syncwarp();
+        }
+        if (weight) {
+#pragma unroll
+          for (int k = 0; k < 8; k += 2) mul2(v[k], v[k + 1], f, f);
         }
         if (base + u * GROUPS + group < n_rows && in) {
           T* p = y + token[u] * yt + head[u] * yh;
@@ -191,7 +202,7 @@ cudaError_t rotate_rows(const Launch& l, const HeadRows& h, const Rotation& r, u
   const bool vec = where % 16 == 0;
   const uint64_t spread = r.tokens / (8 * (uint64_t)l.sm_count);                 // eight CTAs per SM where there are tokens for them
   const uint32_t tokens = (uint32_t)(spread < 1 ? 1 : spread > kRotateMaxTokens ? kRotateMaxTokens : spread);
-  const size_t smem = sizeof(float2) * tokens * (half + half % 2) + (!quads && !r.pairs ? sizeof(float) * kRotateThreads * 8 : 0);
+  const size_t smem = 2 * sizeof(float) * tokens * ((half + 3) / 4 * 4) + (!quads && !r.pairs ? sizeof(float) * kRotateThreads * 8 : 0);
   auto* kernel = r.pairs ? (vec ? norm_rotate_kernel<T, LPR, true, true, true> : quads ? norm_rotate_kernel<T, LPR, true, true, false> : norm_rotate_kernel<T, LPR, true, false, false>)
                          : (vec ? norm_rotate_kernel<T, LPR, false, true, true> : quads ? norm_rotate_kernel<T, LPR, false, true, false> : norm_rotate_kernel<T, LPR, false, false, false>);
   auto heads = [&](int a) { return FastDiv(h.heads[a] ? h.heads[a] : 1); };
