@@ -47,6 +47,14 @@ __device__ __forceinline__ void load_words(uint32_t (&w)[N], const uint8_t* p) {
     for (uint32_t i = 0; i < N; i += 4) { const uint4 v = *reinterpret_cast<const uint4*>(p + 4 * i); w[i] = v.x; w[i + 1] = v.y; w[i + 2] = v.z; w[i + 3] = v.w; }
 }
 
+template <uint32_t N>
+__device__ __forceinline__ void load_floats(float (&f)[N], const float* p) {
+  if constexpr (N == 2) { const float2 v = *reinterpret_cast<const float2*>(p); f[0] = v.x; f[1] = v.y; }
+  else
+#pragma unroll
+    for (uint32_t i = 0; i < N; i += 4) { const float4 v = *reinterpret_cast<const float4*>(p + i); f[i] = v.x; f[i + 1] = v.y; f[i + 2] = v.z; f[i + 3] = v.w; }
+}
+
 template <int FORMAT_, int DP_, int NT_, int TERMS_>
 struct Form {
   static constexpr int FORMAT = FORMAT_, DP = DP_, NT = NT_, TERMS = TERMS_;
@@ -75,7 +83,7 @@ struct RowsArgs {
   FastDiv page, group;
   uint32_t hw, hw_log;                                     // key heads of a CTA (a power of two), warps / hw warps share the tokens
   uint32_t row_limit;                                      // sequences of more rows are not this kernel's
-  uint32_t vec_codes, vec_out;                             // codes by 16 bytes, results by four elements
+  uint32_t vec_q, vec_codes, vec_out;                      // queries and codes by 16 bytes, results by four elements
   float* parts;
   AttendPiece* pieces;
 };
@@ -178,29 +186,42 @@ __global__ void __launch_bounds__(kThreads, F::RESIDENT) attend_rows_kernel(cons
     float slope[NT][2];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      const uint32_t r = row0 + 8 * n + g, i = p.group.div(r);
+      const uint32_t r = row0 + 8 * n + g;
       const bool there = r < row1;
       float v[NB][8];
       uint32_t top = 0;
-      const uint64_t q_at = (uint64_t)(s.row0 + i) * a.q_token_ld + (uint64_t)(kv * a.group + (r - i * a.group)) * a.q_head_ld;
+      const uint32_t rc = min(r, row1 - 1), ic = p.group.div(rc);                // (rows that are not there take another's elements, times zero)
+      const uint64_t q_at = (uint64_t)(s.row0 + ic) * a.q_token_ld + (uint64_t)(kv * a.group + (rc - ic * a.group)) * a.q_head_ld;
+      auto bring = [&](auto zero, const auto* from) {
+        decltype(zero) chunk[NB];
+        if (p.vec_q) {
 #pragma unroll
-      for (uint32_t b = 0; b < NB; ++b) {
-        const uint32_t d = 32 * b + 8 * t;
-        auto bring = [&](auto chunk, const auto* from) {
-          chunk.zero();
-          if (there && d + 8 <= a.c.dim) chunk.load_any(from + q_at + d);
-          else if (there && d < a.c.dim) chunk.load_some(from + q_at + d, a.c.dim - d);
-          chunk.widen(v[b]);
-          top = max(top, chunk.top_bits());
-        };
-        if (a.dtype == kBF16) bring(Chunk8<__nv_bfloat16>(), (const __nv_bfloat16*)a.q);
-        else if (a.dtype == kF16) bring(Chunk8<__half>(), (const __half*)a.q);
-        else bring(Chunk8<float>(), (const float*)a.q);
-      }
+          for (uint32_t b = 0; b < NB; ++b) chunk[b].load_vec(from + q_at + min(32 * b + 8 * t, a.c.dim - 8));
+        } else {
+#pragma unroll
+          for (uint32_t b = 0; b < NB; ++b) {
+            const uint32_t d = 32 * b + 8 * t;
+            chunk[b].zero();
+            if (d + 8 <= a.c.dim) chunk[b].load_any(from + q_at + d);
+            else if (d < a.c.dim) chunk[b].load_some(from + q_at + d, a.c.dim - d);
+          }
+        }
+#pragma unroll
+        for (uint32_t b = 0; b < NB; ++b) {
+          chunk[b].widen(v[b]);
+          top = max(top, chunk[b].top_bits());
+          if (32 * b + 8 * t >= a.c.dim)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[b][k] = 0.f;
+        }
+      };
+      if (a.dtype == kBF16) bring(Chunk8<__nv_bfloat16>(), (const __nv_bfloat16*)a.q);
+      else if (a.dtype == kF16) bring(Chunk8<__half>(), (const __half*)a.q);
+      else bring(Chunk8<float>(), (const float*)a.q);
       top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
       top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
       const int e = top ? max((int)(top >> 23) - 127, -100) : 0;                // the largest element is 2^e to 2^(e+1)
-      const float up = power_of_two(14 - min(e, 127));
+      const float up = there ? power_of_two(14 - min(e, 127)) : 0.f;
 #pragma unroll
       for (uint32_t b = 0; b < NB; ++b)
 #pragma unroll
@@ -241,25 +262,31 @@ __global__ void __launch_bounds__(kThreads, F::RESIDENT) attend_rows_kernel(cons
       const int32_t id = __ldg(pages + p.page.div((uint32_t)j));
       return id >= 0 && (uint32_t)id < a.c.pages ? id : -1;
     };
+    constexpr uint32_t CH = F::RB / 16, PER = 32 / CH;                           // 16-byte pieces of a row, rows of one instruction
+    const uint32_t c16 = 16 * (lane % CH), tok0 = lane / CH;
+    const bool piece = c16 < row_bytes;
+    const uint8_t *const k_src = a.c.codes[0] + c16, *const v_src = a.c.codes[1] + c16;
+    const uint32_t k_dst = tok0 * F::KS + c16, v_dst = TOK * F::KS + tok0 * F::VS + c16;
     auto fetch = [&](uint32_t k, int32_t id) {                                   // codes and scales of a stage into its place of the ring
       const uint32_t place = (k % kDepth) * F::STAGE;
       if (k < n_stages) {
         const uint32_t j = (uint32_t)stage_token(k) + lane, off = j - p.page.div(j) * p.page.d;
         const uint64_t at = id < 0 ? 0 : ((uint64_t)(uint32_t)id * p.page.d + off) * a.c.heads + kv;
-        constexpr uint32_t CH = F::RB / 16, PER = 32 / CH;                       // 16-byte pieces of a row, rows of one instruction
+        const int64_t bytes = id < 0 ? -1 : (int64_t)(at * row_bytes);
 #pragma unroll
         for (uint32_t i = 0; i < TOK / PER; ++i) {
-          const uint32_t tok = i * PER + lane / CH, c16 = 16 * (lane % CH);
-          const uint64_t row = __shfl_sync(0xffffffffu, at, tok);
-          const bool there = __shfl_sync(0xffffffffu, id, tok) >= 0 && c16 < row_bytes;
-#pragma unroll
-          for (int w = 0; w < 2; ++w) {
-            const uint32_t dst = place + (w ? TOK * F::KS + tok * F::VS : tok * F::KS) + c16;
-            const uint8_t* src = a.c.codes[w] + (there ? row * row_bytes + c16 : 0);
-            if (MX || p.vec_codes) copy16(ring + dst, src, there);
-            else
-              for (uint32_t b = 0; b < 16; ++b) mine[dst + b] = there && c16 + b < row_bytes ? __ldg(src + b) : (uint8_t)0;
-          }
+          const int64_t row = __shfl_sync(0xffffffffu, bytes, i * PER + tok0);
+          const bool there = row >= 0 && piece;
+          const uint64_t from = there ? (uint64_t)row : 0;
+          if (MX || p.vec_codes) {
+            copy16(ring + place + k_dst + i * PER * F::KS, k_src + from, there);
+            copy16(ring + place + v_dst + i * PER * F::VS, v_src + from, there);
+          } else
+            for (uint32_t b = 0; b < 16; ++b) {
+              const bool has = there && c16 + b < row_bytes;
+              mine[place + k_dst + i * PER * F::KS + b] = has ? __ldg(k_src + from + b) : (uint8_t)0;
+              mine[place + v_dst + i * PER * F::VS + b] = has ? __ldg(v_src + from + b) : (uint8_t)0;
+            }
         }
         const uint32_t raw = place + TOK * (F::KS + F::VS);
         if (lane < TOK) {
@@ -306,29 +333,37 @@ __global__ void __launch_bounds__(kThreads, F::RESIDENT) attend_rows_kernel(cons
       if (lane < TOK) meta = *reinterpret_cast<const uint32_t*>(mine + raw + 2 * TOK * F::RAW + 4 * lane);
       const uint32_t real = __ballot_sync(0xffffffffu, meta != ~0u);             // tokens that there are
       float v_row = 0.f;                                                         // scale of this lane's value
-      uint32_t v_bytes[MX ? NB : 1];
-      int v_most = 0;
       if (MX) {
-        const uint8_t* kb = mine + raw + lane * F::RAW + (meta & 3u);
-        const uint8_t* vb = mine + raw + TOK * F::RAW + lane * F::RAW + (meta >> 8 & 3u);
+        constexpr uint32_t PACKS = (NB + 3) / 4, WORDS = F::RAW / 4;
+        const uint32_t *kw = reinterpret_cast<const uint32_t*>(mine + raw + lane * F::RAW), *vw = reinterpret_cast<const uint32_t*>(mine + raw + TOK * F::RAW + lane * F::RAW);
+        uint32_t kb[PACKS], vb[PACKS], v_most = 0;                               // bytes of the row's blocks; 0 where there is none
+        float ks[NB];
+        if (lane < TOK) {
 #pragma unroll
-        for (uint32_t b = 0; b < NB; ++b) {
-          v_bytes[MX ? b : 0] = 0;
-          float ks = 0.f;
-          if (meta != ~0u && b < blocks) {
-            ks = mx_scale(kb[b]);
-            v_bytes[MX ? b : 0] = vb[b];
-            v_most = max(v_most, (int)vb[b]);
+          for (uint32_t i = 0; i < PACKS; ++i) {
+            const uint32_t have = blocks - min(blocks, 4 * i), keep = meta == ~0u ? 0u : have < 4 ? (1u << (8 * have)) - 1u : ~0u;
+            kb[i] = __funnelshift_r(kw[i], i + 1 < WORDS ? kw[i + 1] : 0u, 8 * (meta & 3u)) & keep;
+            vb[i] = __funnelshift_r(vw[i], i + 1 < WORDS ? vw[i + 1] : 0u, 8 * (meta >> 8 & 3u)) & keep;
+            const uint32_t two = __vmaxu2(vb[i] & 0x00ff00ffu, vb[i] >> 8 & 0x00ff00ffu);
+            v_most = max(v_most, max(two & 0xffffu, two >> 16));
           }
-          if (lane < TOK) k_scale[lane * NB + b] = ks;
-        }
-        v_row = meta == ~0u ? 0.f : mx_scale((uint32_t)v_most);                   // NaN if any block is poisoned
 #pragma unroll
-        for (uint32_t b = 0; b < NB; ++b) {
+          for (uint32_t b = 0; b < NB; ++b) {
+            const uint32_t byte = kb[b / 4] >> (8 * (b % 4)) & 255u;
+            ks[b] = __uint_as_float(byte << 23 | (byte + 1) >> 8 << 22);         // 2^(byte - 127); 255: NaN; 0: none, for the 2^-127 that it means
+          }
+          if constexpr (NB == 2) *reinterpret_cast<float2*>(k_scale + lane * NB) = make_float2(ks[0], ks[1]);
+          else
+#pragma unroll
+            for (uint32_t b = 0; b < NB; b += 4) *reinterpret_cast<float4*>(k_scale + lane * NB + b) = make_float4(ks[b], ks[b + 1], ks[b + 2], ks[b + 3]);
+          v_row = meta == ~0u ? 0.f : mx_scale(v_most);                          // NaN if any block is poisoned
           // 2^(own - row's largest + kFactorBits) in binary16, down to its smallest number 2^-24
-          const int f = (int)v_bytes[MX ? b : 0] - v_most + kFactorBits;
-          const uint32_t h = v_most == 255 || f < -24 ? 0u : f >= -14 ? (uint32_t)(f + 15) << 10 : 1u << (f + 24);
-          if (lane < TOK) v_factor[b * TOK + lane] = __ushort_as_half((unsigned short)h);
+          const uint32_t base = (uint32_t)(127 + kFactorBits) - v_most;
+#pragma unroll
+          for (uint32_t b = 0; b < NB; ++b) {
+            const int e = (int)((vb[b / 4] >> (8 * (b % 4)) & 255u) + base);
+            v_factor[b * TOK + lane] = __float2half_rn(v_most == 255u ? 0.f : __uint_as_float((uint32_t)max(e, 0) << 23));
+          }
         }
       } else if (lane < TOK) {
         k_scale[lane] = *reinterpret_cast<const float*>(mine + raw + 4 * lane);
@@ -357,6 +392,11 @@ __global__ void __launch_bounds__(kThreads, F::RESIDENT) attend_rows_kernel(cons
         for (int n = 0; n < NT; ++n)
 #pragma unroll
           for (int i = 0; i < 4; ++i) x[l][n][i] = 0.f;
+        float s0[MX ? NB : 1], s1[MX ? NB : 1];
+        if constexpr (MX) {
+          load_floats<NB>(s0, k_scale + (16 * l + g) * NB);
+          load_floats<NB>(s1, k_scale + (16 * l + g + 8) * NB);
+        } else { s0[0] = k_scale[16 * l + g]; s1[0] = k_scale[16 * l + g + 8]; }
         const uint8_t* k0 = mine + place + (16 * l + g) * F::KS;
         const uint8_t* k1 = k0 + 8 * F::KS;
 #pragma unroll
@@ -382,16 +422,15 @@ __global__ void __launch_bounds__(kThreads, F::RESIDENT) attend_rows_kernel(cons
               mma16816(into, c0[2], c1[2], c0[3], c1[3], qf[term][n][4 * b + 2], qf[term][n][4 * b + 3]);
             }
             if (MX) {
-              const float s0 = k_scale[(16 * l + g) * NB + b], s1 = k_scale[(16 * l + g + 8) * NB + b];
-              x[l][n][0] = fmaf(acc[0], s0, x[l][n][0]); x[l][n][1] = fmaf(acc[1], s0, x[l][n][1]);
-              x[l][n][2] = fmaf(acc[2], s1, x[l][n][2]); x[l][n][3] = fmaf(acc[3], s1, x[l][n][3]);
+              const float f0 = s0[MX ? b : 0], f1 = s1[MX ? b : 0];
+              x[l][n][0] = fmaf(acc[0], f0, x[l][n][0]); x[l][n][1] = fmaf(acc[1], f0, x[l][n][1]);
+              x[l][n][2] = fmaf(acc[2], f1, x[l][n][2]); x[l][n][3] = fmaf(acc[3], f1, x[l][n][3]);
             }
           }
         }
         if (!MX) {
-          const float s0 = k_scale[16 * l + g], s1 = k_scale[16 * l + g + 8];
 #pragma unroll
-          for (int n = 0; n < NT; ++n) { x[l][n][0] *= s0; x[l][n][1] *= s0; x[l][n][2] *= s1; x[l][n][3] *= s1; }
+          for (int n = 0; n < NT; ++n) { x[l][n][0] *= s0[0]; x[l][n][1] *= s0[0]; x[l][n][2] *= s1[0]; x[l][n][3] *= s1[0]; }
         }
       }
 
@@ -750,6 +789,7 @@ cudaError_t launch_kv_attend(const Launch& l, const AttendArgs& a, const AttendR
     p.a = a; p.page = FastDiv(a.c.page_size); p.group = FastDiv(a.group);
     p.hw = 1u << run.hw_log; p.hw_log = run.hw_log; p.row_limit = run.few;
     p.vec_codes = a.c.dim % 16 == 0 && ((uintptr_t)a.c.codes[0] | (uintptr_t)a.c.codes[1]) % 16 == 0;
+    p.vec_q = a.c.dim % 8 == 0 && ((uintptr_t)a.q | a.q_token_ld * dtype_size(a.dtype) | a.q_head_ld * dtype_size(a.dtype)) % 16 == 0;
     p.vec_out = attend_vec_out(a);
     cudaError_t e = a.c.format == QV2_KV_MX4 ? launch_dim<QV2_KV_MX4>(l, p, run, launches) : launch_dim<QV2_KV_I8>(l, p, run, launches);
     if (e != cudaSuccess || run.few == 0xffffffffu) return e;
