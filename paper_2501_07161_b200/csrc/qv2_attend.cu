@@ -17,7 +17,6 @@ namespace qv2 {
 
 namespace {
 
-constexpr uint32_t kWarps = 8, kThreads = 32 * kWarps;
 constexpr uint32_t kDepth = 2;                             // stages of a warp's ring
 constexpr int kWeightBits = 13;                            // weights stand 2^13 above p * scale / (largest scale)
 constexpr int kFactorBits = 12;                            // 4 bits: block factors stand 2^12 above scale / (largest of the row)
@@ -71,11 +70,12 @@ struct Form {
   static constexpr uint32_t STAGE = TOK * (KS + VS + 2 * RAW + 4);  // ... and a word that says where they begin, or that there is no such token
   static constexpr uint32_t READY = MX ? TOK * (4 * NB + 4) + TOK * 2 * NB : TOK * 8;   // scales as the products want them
   static constexpr uint32_t WARP = (kDepth * STAGE + READY + 15) / 16 * 16;
-  static constexpr uint32_t EXCHANGE = kWarps * ROWS * (DP + 2) * 4;
-  static constexpr uint32_t SMEM = kWarps * WARP > EXCHANGE ? kWarps * WARP : EXCHANGE;
+  // One CTA per SM: sixteen warps where a thread's accumulators and operands leave room in 128 registers, else eight.
+  static constexpr uint32_t WARPS = (DP / 16) * 4 * NT + 4 * NB * NT * TERMS > 64 ? 8 : 16, THREADS = 32 * WARPS;
+  static constexpr uint32_t EXCHANGE = WARPS * ROWS * DP * 4;
+  static constexpr uint32_t SMEM = WARPS * WARP > EXCHANGE ? WARPS * WARP : EXCHANGE;
+  static_assert(SMEM + 4096 <= 232448, "shared memory");
   static constexpr uint32_t PIECE = ROWS * (DP + 2);       // floats of a head of a partial result
-  // CTAs per SM.  Where the accumulators and operands of a thread leave no room in 128 registers, one.
-  static constexpr int RESIDENT = (DP / 16) * 4 * NT + 4 * NB * NT * TERMS > 64 || SMEM > 113000 ? 1 : 2;
 };
 
 struct RowsArgs {
@@ -94,15 +94,15 @@ __device__ __forceinline__ void units_of(const RowsArgs& p, const AttendSeq& s, 
   const uint64_t rows = (uint64_t)s.n * p.a.group;
   *tiles = rows > p.row_limit ? 0 : (uint32_t)((rows + F::ROWS - 1) / F::ROWS);
   const uint32_t sees = (uint32_t)p.a.window + (F::ROWS + p.a.group - 1) / p.a.group;       // tokens that a tile of rows sees at most
-  const uint32_t wide = min(min((uint32_t)s.len, p.a.room), sees), unit = F::TOK * (kWarps >> p.hw_log);
+  const uint32_t wide = min(min((uint32_t)s.len, p.a.room), sees), unit = F::TOK * (F::WARPS >> p.hw_log);
   *units = max(1u, (wide + unit - 1) / unit);
 }
 
 template <class F>
-__global__ void __launch_bounds__(kThreads, F::RESIDENT) attend_rows_kernel(const RowsArgs p) {
+__global__ void __launch_bounds__(F::THREADS, 1) attend_rows_kernel(const RowsArgs p) {
   constexpr bool MX = F::MX;
   constexpr int NT = F::NT, DP = F::DP, TERMS = F::TERMS;
-  constexpr uint32_t NB = F::NB, TOK = F::TOK, TILES = F::TILES, ROWS = F::ROWS;
+  constexpr uint32_t kWarps = F::WARPS, kThreads = F::THREADS, NB = F::NB, TOK = F::TOK, TILES = F::TILES, ROWS = F::ROWS;
   extern __shared__ __align__(16) uint8_t smem[];
   __shared__ uint64_t scan[kWarps];
   __shared__ AttendUnits found;
@@ -499,7 +499,11 @@ __global__ void __launch_bounds__(kThreads, F::RESIDENT) attend_rows_kernel(cons
           for (int r = 0; r < 2; ++r) {
             const float vs = v_scale[16 * l + g + 8 * r];
             const uint32_t bit = 4 * (l * NT + n) + 2 * r;
-            const float w0 = seen >> bit & 1u ? x[l][n][2 * r] * vs : 0.f, w1 = seen >> (bit + 1) & 1u ? x[l][n][2 * r + 1] * vs : 0.f;
+            float w0 = x[l][n][2 * r] * vs, w1 = x[l][n][2 * r + 1] * vs;
+            if (!every) {                                                        // not zero times a poisoned scale
+              if (!(seen >> bit & 1u)) w0 = 0.f;
+              if (!(seen >> (bit + 1) & 1u)) w1 = 0.f;
+            }
             const uint32_t h = pack_half(w0, w1);
             wf[0][l][n][r] = transpose8x8(h);
             if (TERMS == 2) {
@@ -625,52 +629,66 @@ __global__ void __launch_bounds__(kThreads, F::RESIDENT) attend_rows_kernel(cons
   }
 }
 
-// Adds up the items that were cut.  CTA (c, y) has every kJoinRows-th row of the item that main CTA c began; its warps share the pieces.
+// Adds up the items that were cut.  CTA (c, y) has every kJoinRows-th (row, key head) of the item that main CTA c began, all of them at once:
+// its warps are dealt out to them and share their pieces.
 constexpr uint32_t kJoinThreads = 256, kJoinRows = 8;
 __global__ void __launch_bounds__(kJoinThreads)
-attend_join_kernel(const AttendArgs a, FastDiv group, const float* parts, const AttendPiece* pieces, uint32_t hw, uint32_t hw_log, uint32_t tile_rows, uint32_t dp, uint32_t vec_out) {
-  __shared__ float4 sums[kJoinThreads / 32][64];
-  __shared__ float2 top_sum[kJoinThreads / 32];
+attend_join_kernel(const AttendArgs a, FastDiv group, const float* parts, const AttendPiece* pieces, uint32_t hw_log, uint32_t tile_rows, uint32_t dp, uint32_t vec_out) {
+  constexpr uint32_t WARPS = kJoinThreads / 32;
+  __shared__ float4 sums[WARPS][64];
+  __shared__ float2 top_sum[WARPS];
   dependency_wait();
   allow_dependents();
   const AttendPiece h = pieces[blockIdx.x];
   if (h.followers == 0) return;
-  const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32, quads = dp / 4, n_rows = min(tile_rows, h.rows - h.tile * tile_rows);
-  const uint64_t piece = (uint64_t)hw * tile_rows * (dp + 2);
-  for (uint32_t i = blockIdx.y; i < n_rows << hw_log; i += kJoinRows) {
-    const uint32_t r = i >> hw_log, head = i & (hw - 1);
+  const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32, quads = dp / 4, n_rows = min(tile_rows, h.rows - h.tile * tile_rows), pairs = n_rows << hw_log;
+  const uint64_t piece = (uint64_t)(tile_rows << hw_log) * (dp + 2);
+  uint32_t share = WARPS;                                    // warps of a pair: a power of two
+  while (share > 1 && (WARPS / share) * kJoinRows < pairs) share /= 2;
+  const uint32_t sub = warp & (share - 1);
+  for (uint32_t i0 = blockIdx.y; i0 < pairs; i0 += kJoinRows * (WARPS / share)) {
+    const uint32_t i = i0 + kJoinRows * (warp / share);
+    const bool there = i < pairs;
+    const uint32_t r = i >> hw_log, head = i & ((1u << hw_log) - 1), at = head * tile_rows + r;
     float top = -INFINITY, total = 0.f;
     float4 v[2] = {};
-#pragma unroll 4
-    for (uint32_t f = warp; f <= h.followers; f += kJoinThreads / 32) {
-      const float* from = parts + ((uint64_t)(blockIdx.x + f) * 2 + (f == 0 ? 1 : 0)) * piece;
-      const float2 ts = *reinterpret_cast<const float2*>(from + hw * tile_rows * dp + 2 * (head * tile_rows + r));
-      const float m = fmaxf(top, ts.x), base = m == -INFINITY ? 0.f : m, was = exp2_fast(top - base), is = exp2_fast(ts.x - base);
-      top = m;
-      total = total * was + ts.y * is;
+    if (there) {
+#pragma unroll 8
+      for (uint32_t f = sub; f <= h.followers; f += share) {
+        const float* from = parts + ((uint64_t)(blockIdx.x + f) * 2 + (f == 0 ? 1 : 0)) * piece;
+        const float2 ts = *reinterpret_cast<const float2*>(from + (tile_rows << hw_log) * dp + 2 * at);
+        const float m = fmaxf(top, ts.x), base = m == -INFINITY ? 0.f : m, was = exp2_fast(top - base), is = exp2_fast(ts.x - base);
+        top = m;
+        total = total * was + ts.y * is;
 #pragma unroll
-      for (uint32_t k = 0; k < 2; ++k)
-        if (lane + 32 * k < quads) {
-          const float4 x = *reinterpret_cast<const float4*>(from + (head * tile_rows + r) * dp + 4 * (lane + 32 * k));
-          v[k].x = v[k].x * was + x.x * is; v[k].y = v[k].y * was + x.y * is; v[k].z = v[k].z * was + x.z * is; v[k].w = v[k].w * was + x.w * is;
-        }
+        for (uint32_t k = 0; k < 2; ++k)
+          if (lane + 32 * k < quads) {
+            const float4 x = *reinterpret_cast<const float4*>(from + at * dp + 4 * (lane + 32 * k));
+            v[k].x = v[k].x * was + x.x * is; v[k].y = v[k].y * was + x.y * is; v[k].z = v[k].z * was + x.z * is; v[k].w = v[k].w * was + x.w * is;
+          }
+      }
     }
 #pragma unroll
     for (uint32_t k = 0; k < 2; ++k) sums[warp][lane + 32 * k] = v[k];
     if (lane == 0) top_sum[warp] = make_float2(top, total);
     __syncthreads();
-    if (threadIdx.x < quads) {
+    if (there && sub == 0) {
       top = -INFINITY; total = 0.f;
-      for (uint32_t w = 0; w < kJoinThreads / 32; ++w) top = fmaxf(top, top_sum[w].x);
+      for (uint32_t w = 0; w < share; ++w) top = fmaxf(top, top_sum[warp + w].x);
       const float base = top == -INFINITY ? 0.f : top;
-      float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (uint32_t w = 0; w < kJoinThreads / 32; ++w) {
-        const float f = exp2_fast(top_sum[w].x - base);
-        const float4 x = sums[w][threadIdx.x];
-        total = fmaf(top_sum[w].y, f, total);
-        y.x = fmaf(x.x, f, y.x); y.y = fmaf(x.y, f, y.y); y.z = fmaf(x.z, f, y.z); y.w = fmaf(x.w, f, y.w);
+      v[0] = v[1] = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (uint32_t w = 0; w < share; ++w) {
+        const float f = exp2_fast(top_sum[warp + w].x - base);
+        total = fmaf(top_sum[warp + w].y, f, total);
+#pragma unroll
+        for (uint32_t k = 0; k < 2; ++k) {
+          const float4 x = sums[warp + w][lane + 32 * k];
+          v[k].x = fmaf(x.x, f, v[k].x); v[k].y = fmaf(x.y, f, v[k].y); v[k].z = fmaf(x.z, f, v[k].z); v[k].w = fmaf(x.w, f, v[k].w);
+        }
       }
-      attend_store(a, h.row0, h.tile * tile_rows + r, group, (h.heads << hw_log) + head, 4 * threadIdx.x, y, top, total, vec_out);
+#pragma unroll
+      for (uint32_t k = 0; k < 2; ++k)
+        if (lane + 32 * k < quads) attend_store(a, h.row0, h.tile * tile_rows + r, group, (h.heads << hw_log) + head, 4 * (lane + 32 * k), v[k], top, total, vec_out);
     }
     __syncthreads();
   }
@@ -723,7 +741,7 @@ cudaError_t launch_rows(const Launch& l, RowsArgs p, const AttendRun& run, uint6
   }
   p.parts = reinterpret_cast<float*>(run.scratch);
   p.pieces = reinterpret_cast<AttendPiece*>(run.scratch + attend_parts_bytes(run.ctas, p.hw, F::ROWS, F::DP));
-  e = launch_grid(l, attend_rows_kernel<F>, dim3(run.ctas), kThreads, F::SMEM, p);
+  e = launch_grid(l, attend_rows_kernel<F>, dim3(run.ctas), F::THREADS, F::SMEM, p);
   if (e != cudaSuccess) return e;
   ++*launches;
   return launch_attend_join(l, p.a, p.parts, p.pieces, run.ctas, p.hw_log, F::ROWS, F::DP, launches);
@@ -751,7 +769,7 @@ cudaError_t launch_dim(const Launch& l, const RowsArgs& p, const AttendRun& run,
 cudaError_t launch_attend_join(const Launch& l, const AttendArgs& a, const float* parts, const AttendPiece* pieces, uint32_t ctas, uint32_t hw_log, uint32_t tile_rows,
                                uint32_t dp, uint64_t* launches) {
   cudaError_t e = tile_rows >= 128 ? launch_grid(l, attend_join_rows_kernel, dim3(ctas, 8), kJoinThreads, 0, a, FastDiv(a.group), parts, pieces, tile_rows, dp, attend_vec_out(a))
-                                   : launch_grid(l, attend_join_kernel, dim3(ctas, kJoinRows), kJoinThreads, 0, a, FastDiv(a.group), parts, pieces, 1u << hw_log, hw_log,
+                                   : launch_grid(l, attend_join_kernel, dim3(ctas, kJoinRows), kJoinThreads, 0, a, FastDiv(a.group), parts, pieces, hw_log,
                                                  tile_rows, dp, attend_vec_out(a));
   if (e == cudaSuccess) ++*launches;
   return e;
@@ -768,9 +786,9 @@ AttendRun plan_kv_attend(const AttendArgs& a, int sm_count) {
   r.few = r.terms == 2 || most <= 16 ? 0xffffffffu : a.seqs == 1 ? 0 : 16;
   r.hw_log = 0;
   while (r.hw_log < 3 && a.c.heads % (2u << r.hw_log) == 0) ++r.hw_log;
-  // Two CTAs per SM, fewer where there cannot be a unit of 16 tokens for each
+  // A CTA per SM, fewer where there cannot be a unit of 16 tokens for each
   const uint64_t tiles = (uint64_t)a.total * a.group / r.rows + a.seqs, units = tiles * (a.c.heads >> r.hw_log) * (a.room / 16 + 1);
-  const uint64_t ctas = 2 * (uint64_t)sm_count;
+  const uint64_t ctas = (uint64_t)sm_count;
   r.ctas = (uint32_t)(units < ctas ? units : ctas);
   uint64_t most_bytes = r.few == 0 ? 0 : attend_parts_bytes(r.ctas, 1u << r.hw_log, r.rows, r.dp) + r.ctas * sizeof(AttendPiece);
   if (r.few != 0xffffffffu) {

@@ -80,18 +80,37 @@ __global__ void __launch_bounds__(kPlanThreads) kv_plan_kernel(qv2_page_plan p, 
       }
     }
     __syncthreads();
-    for (int64_t t = max(t_begin, tok0) + tid; t < min(t_end, tok0 + whole[0]); t += kPlanThreads) {
-      const uint32_t i = last_at_most(tok, n, t - tok0);
-      const int64_t at = held[i] + (t - tok0 - tok[i]);
-      int64_t slot = -1;
-      if (at < span) {
-        const uint32_t pg = page.div((uint32_t)at);
-        const int64_t have = pages_of(held[i]);
-        const int32_t id = pg < have ? __ldg(p.table + (base + i) * p.table_ld + pg) : page_number(pag0 + pag[i] + pg - have);
-        if (id >= 0) slot = (int64_t)id * page.d + ((uint32_t)at - pg * page.d);
+    // Four tokens of a thread at a time: a token is a chain of look-ups.
+    const int64_t stop = min(t_end, tok0 + whole[0]);
+    for (int64_t t0 = max(t_begin, tok0) + tid; t0 < stop; t0 += 4 * kPlanThreads) {
+      uint32_t i[4], b[4];
+      int64_t at[4], slot[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) { i[k] = 0; b[k] = n; }
+      for (uint32_t wide = n; wide > 1; wide = (wide + 1) / 2) {                // as last_at_most
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const uint32_t mid = (i[k] + b[k]) / 2;
+          if (b[k] - i[k] > 1) { if (tok[mid] <= t0 + k * kPlanThreads - tok0) i[k] = mid; else b[k] = mid; }
+        }
       }
-      p.slots[t] = slot;
-      p.positions[t] = at;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int64_t t = t0 + k * kPlanThreads;
+        at[k] = held[i[k]] + (t - tok0 - tok[i[k]]);
+        slot[k] = -1;
+        if (t < stop && at[k] < span) {
+          const uint32_t pg = page.div((uint32_t)at[k]);
+          const int64_t have = pages_of(held[i[k]]);
+          const int32_t id = pg < have ? __ldg(p.table + (base + i[k]) * p.table_ld + pg) : page_number(pag0 + pag[i[k]] + pg - have);
+          if (id >= 0) slot[k] = (int64_t)id * page.d + ((uint32_t)at[k] - pg * page.d);
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int64_t t = t0 + k * kPlanThreads;
+        if (t < stop) { p.slots[t] = slot[k]; p.positions[t] = at[k]; }
+      }
     }
     for (int64_t a = blockIdx.x * kPlanThreads + tid; a < whole[1]; a += gridDim.x * kPlanThreads) {
       const uint32_t i = last_at_most(pag, n, a);
