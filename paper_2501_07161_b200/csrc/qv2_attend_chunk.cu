@@ -24,7 +24,7 @@ namespace {
 
 constexpr uint32_t kConvert = 4, kScout = 2;                         // converting and looking-up warps
 constexpr uint32_t kFirstScout = 8 + kConvert, kProducts = kFirstScout + kScout, kChunkThreads = (kProducts + 1) * 32;
-constexpr uint32_t kSetup = 4;              // what an item costs besides its tiles, in tiles
+constexpr uint32_t kSetup = 8;              // what an item costs besides its tiles, in tiles
 constexpr int kChunkFactor = 13;            // 4 bits: operands stand 2^13 above code * scale / (largest scale): 6 * 2^13 at most
 constexpr float kSlack = 4.f;               // a row's largest weight is 2^kSlack at most ...
 constexpr int kWeightBits = 10;             // ... and weights stand 2^10 above that: at most 2^15 (8 bits: times up to 2), and what binary16 loses below 2^-35
@@ -51,13 +51,22 @@ __device__ __forceinline__ void tensor_read(uint32_t at, float (&v)[32]) {
                  "=f"(v[30]), "=f"(v[31])
                : "r"(at) : "memory");
 }
-__device__ __forceinline__ void tensor_write(uint32_t at, const float (&v)[32]) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
-               "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};"
-               ::"f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]), "f"(v[8]), "f"(v[9]),
-                 "f"(v[10]), "f"(v[11]), "f"(v[12]), "f"(v[13]), "f"(v[14]), "f"(v[15]), "f"(v[16]), "f"(v[17]), "f"(v[18]), "f"(v[19]),
-                 "f"(v[20]), "f"(v[21]), "f"(v[22]), "f"(v[23]), "f"(v[24]), "f"(v[25]), "f"(v[26]), "f"(v[27]), "f"(v[28]), "f"(v[29]),
-                 "f"(v[30]), "f"(v[31]), "r"(at) : "memory");
+// The same, but they are there only after tc_load_wait().
+__device__ __forceinline__ void tensor_read_begin(uint32_t at, float* v) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+               "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+               : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]),
+                 "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]), "=f"(v[16]), "=f"(v[17]), "=f"(v[18]), "=f"(v[19]),
+                 "=f"(v[20]), "=f"(v[21]), "=f"(v[22]), "=f"(v[23]), "=f"(v[24]), "=f"(v[25]), "=f"(v[26]), "=f"(v[27]), "=f"(v[28]), "=f"(v[29]),
+                 "=f"(v[30]), "=f"(v[31])
+               : "r"(at) : "memory");
+}
+__device__ __forceinline__ void tensor_read16(uint32_t at, float (&v)[16]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n\t"
+               "tcgen05.wait::ld.sync.aligned;"
+               : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]),
+                 "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15])
+               : "r"(at) : "memory");
 }
 __device__ __forceinline__ void tensor_write16(uint32_t at, const uint32_t (&v)[16]) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};"
@@ -65,6 +74,7 @@ __device__ __forceinline__ void tensor_write16(uint32_t at, const uint32_t (&v)[
                  "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(at) : "memory");
 }
 __device__ __forceinline__ void tensor_write_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ float reciprocal_fast(float x) { float r; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
 __device__ __forceinline__ float max3(float a, float b, float c) { float r; asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c)); return r; }
 // Whether all threads of the looking-up warps say yes.
 __device__ __forceinline__ bool all_scouts(bool ok) {
@@ -90,18 +100,19 @@ struct Chunk {
   static constexpr bool MX = FORMAT == QV2_KV_MX4;
   static constexpr uint32_t QT = DP == 256 ? 1 : 2;                   // query tiles
   static constexpr uint32_t ROWS = 128 * QT;
-  static constexpr uint32_t KT = DP == 256 ? 64 : 128;                // tokens of a tile
+  static constexpr uint32_t KT = 64;                                  // tokens of a tile
   static constexpr uint32_t NB = DP / 32, RB = MX ? DP / 2 : DP;      // blocks of a row, bytes of its codes
   static constexpr uint32_t Q_PANEL = 128 * 128, Q_TILE = Q_PANEL * (DP / 64);
   static constexpr uint32_t PANEL = KT * 128, KV_TILE = PANEL * (DP / 64);
-  static constexpr uint32_t STAGES = 2;
+  static constexpr uint32_t STAGES = DP == 256 ? 2 : 4;
   // What is known of a tile's tokens: where each row lies; 4 bits: factors of keys' and values' blocks [2][block][token], 8 bits: scales of keys, of
   // values [2][token]; then which tokens there are, whose value is poisoned (4 words each), the largest exponents and flags.
-  static constexpr uint32_t INFO = 4;                                 // tiles ahead
+  static constexpr uint32_t INFO = 8;                                 // tiles ahead
+  static_assert(INFO == 8 && STAGES <= 4, "barriers");
   static constexpr uint32_t FACTOR_LD = KT + 8;                       // (blocks of a token in different banks)
   static constexpr uint32_t AT_SCALES = 8 * KT, AT_BITS = AT_SCALES + (MX ? 2 * 2 * NB * FACTOR_LD : 2 * 4 * KT), META = AT_BITS + 48;
   static constexpr uint32_t SMEM = 1024 + QT * Q_TILE + STAGES * 2 * KV_TILE + INFO * META;
-  static constexpr uint32_t O_COL = QT * KT;                          // tensor memory: scores of the tiles, then their results
+  static constexpr uint32_t O_COL = QT * 2 * KT;                      // tensor memory: scores, two tiles of tokens ahead, then the results
   static_assert(O_COL + QT * DP <= 512, "tensor memory");
   static constexpr uint32_t S_IDESC = (1u << 4) | ((KT / 8) << 17) | (8u << 24);                    // binary16 x binary16, binary32 sums
   static constexpr uint32_t O_IDESC = (1u << 4) | (1u << 16) | ((DP / 8) << 17) | (8u << 24);       // second operand across its rows
@@ -188,37 +199,34 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
   extern __shared__ uint8_t raw[];
   __shared__ uint64_t scan[kChunkThreads / 32];
   __shared__ struct { uint64_t before; uint32_t seq; } found;
-  __shared__ uint64_t bars[17 + 8];
-  __shared__ uint32_t tmem_slot, failed_flag;
+  __shared__ uint64_t bars[36];
   __shared__ int32_t highest[2][2][kScout];
+  __shared__ uint32_t tmem_slot, failed_flag;
   const AttendArgs& a = p.a;
   const uint32_t tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
   uint8_t* const base = raw + ((1024u - (smem_addr(raw) & 1023u)) & 1023u);
   const uint32_t q_at = smem_addr(base), k_at = q_at + QT * F::Q_TILE, v_at = k_at + F::STAGES * F::KV_TILE;
   uint8_t* const meta = base + QT * F::Q_TILE + 2 * F::STAGES * F::KV_TILE;
   const uint32_t bar0 = smem_addr(bars);
+  // Of tile n (counted over all items): operands are there (k_full, v_full, by stage), its tokens are known (m_full); the products for the scores of both
+  // query tiles, for the results, are done (s_done, o_done: eight in turn, so that whoever waits is never two rounds late); the weights are there (p_full, two
+  // in turn).
   auto k_full = [&](uint32_t s) { return bar0 + 8 * s; };
-  auto k_empty = [&](uint32_t s) { return bar0 + 8 * (2 + s); };
   auto v_full = [&](uint32_t s) { return bar0 + 8 * (4 + s); };
-  auto v_empty = [&](uint32_t s) { return bar0 + 8 * (6 + s); };
-  auto q_full = [&](uint32_t t) { return bar0 + 8 * (8 + t); };
-  auto s_full = [&](uint32_t t) { return bar0 + 8 * (10 + t); };
-  auto p_full = [&](uint32_t t) { return bar0 + 8 * (12 + t); };
-  auto o_done = [&](uint32_t t) { return bar0 + 8 * (14 + t); };
-  const uint32_t drained = bar0 + 8 * 16;
-  auto m_full = [&](uint32_t s) { return bar0 + 8 * (17 + s); };
-  auto m_empty = [&](uint32_t s) { return bar0 + 8 * (21 + s); };
+  auto m_full = [&](uint32_t n) { return bar0 + 8 * (8 + n % 8); };
+  auto s_done = [&](uint32_t n) { return bar0 + 8 * (16 + n % 8); };
+  auto o_done = [&](uint32_t n) { return bar0 + 8 * (24 + n % 8); };
+  auto p_full = [&](uint32_t n) { return bar0 + 8 * (32 + n % 2); };
+  const uint32_t q_full = bar0 + 8 * 34, drained = bar0 + 8 * 35;
   volatile uint32_t* const failed = &failed_flag;
   dependency_wait();
   allow_dependents();
 
   if (tid == 0) {
-    for (uint32_t s = 0; s < 2; ++s) {
-      bar_init(k_full(s), kConvert); bar_init(k_empty(s), 1); bar_init(v_full(s), kConvert); bar_init(v_empty(s), 1);
-      bar_init(q_full(s), 4); bar_init(s_full(s), 1); bar_init(p_full(s), 4); bar_init(o_done(s), 1);
-    }
+    for (uint32_t s = 0; s < 4; ++s) { bar_init(k_full(s), kConvert); bar_init(v_full(s), kConvert); }
+    for (uint32_t s = 0; s < 8; ++s) { bar_init(m_full(s), kScout); bar_init(s_done(s), 1); bar_init(o_done(s), 1); }
+    bar_init(p_full(0), 4 * QT); bar_init(p_full(1), 4 * QT); bar_init(q_full, 4 * QT);
     bar_init(drained, 1);
-    for (uint32_t s = 0; s < F::INFO; ++s) { bar_init(m_full(s), kScout); bar_init(m_empty(s), 1); }
     *failed = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -292,9 +300,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
   } else if (warp < 8) {
     // ---------------------------------------------------------------------------------- softmax
     const uint32_t t = warp / 4, lanes = ((warp % 4) * 32) << 16, r_in = 128 * t + (warp % 4) * 32 + lane;
-    const uint32_t s_at = tmem + t * KT + lanes, o_at = tmem + F::O_COL + t * DP + lanes;
-    uint32_t turn = 0;                                       // tiles that this query tile took part in: phases of s_full, o_done
-    uint32_t tiles_before = 0;                               // all tiles so far: stage of the metadata
+    const uint32_t s_tile = tmem + t * 2 * KT + lanes, o_at = tmem + F::O_COL + t * DP + lanes;
+    uint32_t n = 0;                                          // tiles so far
     // What a thread knows about its row of an item.
     struct Row {
       int32_t pos, pos_first, pos_last;                      // of the row, and of the first and last one of the warp
@@ -366,14 +373,14 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
         else bring(Chunk8<__half>(), (const __half*)a.q);
         const int e = top ? max((int)(top >> 23) - 127, -100) : 0;
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        __syncwarp();
-        if (lane == 0) bar_arrive(q_full(t));
         ahead.back = top >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : power_of_two(min(e, 127) - 14) * power_of_two(MX ? -kChunkFactor : 0) * fabsf(a.scale) * (!F::PLAIN && a.cap > 0.f ? 1.f : kLog2e);
         ahead.slope = !F::PLAIN && a.slopes ? kLog2e * __ldg(a.slopes + ahead.head) : 0.f;
       }
+      __syncwarp();
+      if (more && lane == 0) bar_arrive(q_full);
       if (!begin && row.part) {
         // ---- results of the item that is done
-        if (!bar_wait(o_done(t), (turn - 1) & 1, failed)) break;
+        if (!bar_wait(o_done(n - 1), (n - 1) / 8 & 1, failed)) break;
         tc_fence_after();
         const bool whole = at.unit == 0 && at.unit1 == at.t.units;
         const uint32_t place = at.unit == 0 ? 1 : 0;
@@ -425,148 +432,169 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
       at = to;
       row = ahead;
       const uint32_t n_units = at.unit1 - at.unit;
-      if (row.part) {
-        ref = -INFINITY; sum = 0.f; v_top = -126;
+      ref = -INFINITY; sum = 0.f; v_top = -126;
 #pragma unroll 1
-        for (uint32_t u = 0; u < n_units; ++u, ++turn) {
-          const uint8_t* const m = meta + (tiles_before + u) % F::INFO * F::META;
-          const float4* const k_scale = reinterpret_cast<const float4*>(m + F::AT_SCALES);
-          const float4* const v_scale = reinterpret_cast<const float4*>(m + F::AT_SCALES + 4 * KT);
-          const uint32_t* const real = reinterpret_cast<const uint32_t*>(m + F::AT_BITS);
-          const uint32_t* const bad = real + 4;
-          const uint32_t j = at.t.j0 + (at.unit + u) * KT;
-          if (!bar_wait(s_full(t), turn & 1, failed)) { ok = false; break; }
+      for (uint32_t u = 0; u < n_units; ++u, ++n) {
+        const uint8_t* const m = meta + n % F::INFO * F::META;
+        const float4* const k_scale = reinterpret_cast<const float4*>(m + F::AT_SCALES);
+        const float4* const v_scale = reinterpret_cast<const float4*>(m + F::AT_SCALES + 4 * KT);
+        const uint32_t* const real = reinterpret_cast<const uint32_t*>(m + F::AT_BITS);
+        const uint32_t* const bad = real + 4;
+        const uint32_t j = at.t.j0 + (at.unit + u) * KT, s_at = s_tile + (n & 1) * KT;
+        if (!bar_wait(m_full(n), n / 8 & 1, failed)) { ok = false; break; }
+        const int4 tops = *reinterpret_cast<const int4*>(m + F::AT_BITS + 32);       // exponents of the tile's keys (4 bits), of the values so far; flags
+        const bool every = (tops.z & 1) && (int32_t)(j + KT - 1) <= row.pos_first && row.pos_last - (int32_t)j < a.window, poisoned = MX && (tops.z & 2);
+        // what turns a score of the product into one to powers of two; not 0, since it multiplies minus infinity, too
+        const float unit = MX ? row.back * power_of_two(tops.x) : row.back, mul = !F::PLAIN ? 1.f : unit < 1.2e-38f ? 1.2e-38f : unit;
+        if (!bar_wait(s_done(n), n / 8 & 1, failed)) { ok = false; break; }
+        // EVERY: all tokens are seen by all rows of the warp, and none is poisoned.  (Two bodies instead of branches in one: jumping over the unused code cost
+        // more than the softmax itself.)
+        auto weights = [&](auto every_) -> bool {
+          constexpr bool EVERY = decltype(every_)::value;
           tc_fence_after();
-          const int4 tops = *reinterpret_cast<const int4*>(m + F::AT_BITS + 32);     // exponents of the tile's keys (4 bits), of the values so far; flags
-          const bool every = (tops.z & 1) && (int32_t)(j + KT - 1) <= row.pos_first && row.pos_last - (int32_t)j < a.window, poisoned = MX && (tops.z & 2);
-          // what turns a score of the product into one to powers of two; not 0, since it multiplies minus infinity, too
-          const float unit = MX ? row.back * power_of_two(tops.x) : row.back, mul = !F::PLAIN ? 1.f : unit < 1.2e-38f ? 1.2e-38f : unit;
-          // scores of 32 tokens, up to mul
-          auto scores = [&](uint32_t c, float (&x)[32]) {
-            tensor_read(s_at + 32 * c, x);
-            if (!MX) {
+          float x[KT];
+          tensor_read_begin(s_at, x);
+          tensor_read_begin(s_at + 32, x + 32);
+          tc_load_wait();
+          if (!MX) {
 #pragma unroll
-              for (uint32_t k = 0; k < 8; ++k) {
-                const float4 f = k_scale[8 * c + k];
-                mul2(x[4 * k], x[4 * k + 1], f.x, f.y);
-                mul2(x[4 * k + 2], x[4 * k + 3], f.z, f.w);
-              }
+            for (uint32_t k = 0; k < KT / 4; ++k) {
+              const float4 f = k_scale[k];
+              mul2(x[4 * k], x[4 * k + 1], f.x, f.y);
+              mul2(x[4 * k + 2], x[4 * k + 3], f.z, f.w);
             }
-            if (!F::PLAIN) {
-#pragma unroll
-              for (uint32_t k = 0; k < 32; ++k) {
-                float v = x[k] * unit;
-                if (a.cap > 0.f) v = kLog2e * capped_fast(v, a.cap);
-                x[k] = fmaf(row.slope, (float)(int32_t)(j + 32 * c + k - (uint32_t)row.pos), v);
-              }
-            }
-            if (!every) {
-              const uint32_t bits = real[c];
-#pragma unroll
-              for (uint32_t k = 0; k < 32; ++k) {
-                const int32_t tok = (int32_t)(j + 32 * c + k);
-                if (!((bits >> k & 1u) && tok <= row.pos && (uint32_t)row.pos - (uint32_t)tok < (uint32_t)a.window)) x[k] = -INFINITY;
-              }
-            }
-          };
-          float x[32], high = -INFINITY;
-#pragma unroll 1
-          for (uint32_t c = 0; c < KT / 32; ++c) {
-            scores(c, x);
-            float h4[4] = {x[0], x[1], x[2], x[3]};
-#pragma unroll
-            for (uint32_t k = 4; k < 28; k += 8)
-#pragma unroll
-              for (uint32_t i = 0; i < 4; ++i) h4[i] = max3(h4[i], x[k + i], x[k + 4 + i]);
-#pragma unroll
-            for (uint32_t i = 0; i < 4; ++i) h4[i] = fmaxf(h4[i], x[28 + i]);
-            high = max3(high, fmaxf(h4[0], h4[1]), fmaxf(h4[2], h4[3]));
           }
+          if (!F::PLAIN) {
+            if (a.cap > 0.f) {                               // cap * tanh(y / cap) = cap - 2 cap / (1 + e^(2 y / cap)), off by some 2^-22 of cap
+              const float cap_in = 2.f * kLog2e * unit / a.cap, cap_out = kLog2e * a.cap;
+#pragma unroll
+              for (uint32_t k = 0; k < KT; k += 2) {
+                mul2(x[k], x[k + 1], cap_in, cap_in);
+                x[k] = 1.f + exp2_fast(x[k]);
+                x[k + 1] = 1.f + exp2_fast(x[k + 1]);
+                x[k] = reciprocal_fast(x[k]);
+                x[k + 1] = reciprocal_fast(x[k + 1]);
+                fma2(x[k], x[k + 1], -2.f * cap_out, cap_out);
+              }
+            } else {
+#pragma unroll
+              for (uint32_t k = 0; k < KT; k += 2) mul2(x[k], x[k + 1], unit, unit);
+            }
+            if (a.slopes) {
+#pragma unroll
+              for (uint32_t k = 0; k < KT; ++k) x[k] = fmaf(row.slope, (float)(int32_t)(j + k - (uint32_t)row.pos), x[k]);
+            }
+          }
+          uint32_t seen[2] = {~0u, ~0u};
+          if constexpr (!EVERY) {
+            // tokens that there are, up to the row's position, within its window
+            const int32_t upto = row.pos - (int32_t)j, from = upto - a.window;      // first unseen one on either side, relative to the tile
+#pragma unroll
+            for (uint32_t c = 0; c < 2; ++c) {
+              const int32_t hi = min(max(upto + 1 - (int32_t)(32 * c), 0), 32), lo = row.pos < a.window ? 0 : min(max(from + 1 - (int32_t)(32 * c), 0), 32);
+              seen[c] = real[c] & (hi == 32 ? ~0u : (1u << hi) - 1u) & (lo == 32 ? 0u : ~0u << lo);
+#pragma unroll
+              for (uint32_t k = 0; k < 32; ++k)
+                if (!(seen[c] >> k & 1u)) x[32 * c + k] = -INFINITY;
+            }
+          }
+          float h4[4] = {x[0], x[1], x[2], x[3]};
+#pragma unroll
+          for (uint32_t k = 4; k < KT - 4; k += 8)
+#pragma unroll
+            for (uint32_t i = 0; i < 4; ++i) h4[i] = max3(h4[i], x[k + i], x[k + 4 + i]);
+#pragma unroll
+          for (uint32_t i = 0; i < 4; ++i) h4[i] = fmaxf(h4[i], x[KT - 4 + i]);
+          float high = fmaxf(max3(h4[0], h4[1], h4[2]), h4[3]);
           high = high == -INFINITY ? high : high * mul;      // (NaN from a poisoned query: its weights are NaN below)
           float soft = 1.f, values = 1.f;
           if (high > ref + kSlack) { soft = exp2_fast(ref - high); ref = high; }
           if (tops.y != v_top) { values = power_of_two(max(v_top - tops.y, -126)); v_top = tops.y; }
           sum *= soft;
           if (u > 0 && __any_sync(0xffffffffu, soft * values != 1.f)) {
-            if (!bar_wait(o_done(t), (turn - 1) & 1, failed)) { ok = false; break; }
+            if (!bar_wait(o_done(n - 1), (n - 1) / 8 & 1, failed)) return false;
             tc_fence_after();
             const float f = soft * values;
 #pragma unroll 1
-            for (uint32_t c = 0; c < DP / 32; ++c) {
-              tensor_read(o_at + 32 * c, x);
+            for (uint32_t c = 0; c < DP / 16; ++c) {
+              float o[16];
+              tensor_read16(o_at + 16 * c, o);
 #pragma unroll
-              for (uint32_t k = 0; k < 32; ++k) x[k] *= f;
-              tensor_write(o_at + 32 * c, x);
+              for (uint32_t k = 0; k < 16; k += 2) mul2(o[k], o[k + 1], f, f);
+              uint32_t bits[16];
+#pragma unroll
+              for (uint32_t k = 0; k < 16; ++k) bits[k] = __float_as_uint(o[k]);
+              tensor_write16(o_at + 16 * c, bits);
             }
           }
           const float less = (float)kWeightBits - (ref == -INFINITY ? 0.f : ref);
-          float sums[2] = {0.f, 0.f};
-#pragma unroll 1
-          for (uint32_t c = 0; c < KT / 32; ++c) {
-            scores(c, x);
-            uint32_t seen = 0xffffffffu;
-            if (!every) {
+          float sums[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-              for (uint32_t k = 0; k < 32; ++k)
-                if (x[k] == -INFINITY) seen &= ~(1u << k);
-            }
+          for (uint32_t c = 0; c < 2; ++c) {
+            float* const y = x + 32 * c;
 #pragma unroll
-            for (uint32_t k = 0; k < 32; k += 2) fma2(x[k], x[k + 1], mul, less);
+            for (uint32_t k = 0; k < 32; k += 2) fma2(y[k], y[k + 1], mul, less);
 #pragma unroll
-            for (uint32_t k = 0; k < 32; ++k) x[k] = exp2_fast(x[k]);
+            for (uint32_t k = 0; k < 32; ++k) y[k] = exp2_fast(y[k]);
 #pragma unroll
-            for (uint32_t k = 0; k < 32; k += 2) add2(sums[0], sums[1], x[k], x[k + 1]);
+            for (uint32_t k = 0; k < 32; k += 4) { add2(sums[0], sums[1], y[k], y[k + 1]); add2(sums[2], sums[3], y[k + 2], y[k + 3]); }
             if (!MX) {
 #pragma unroll
               for (uint32_t k = 0; k < 8; ++k) {
                 const float4 f = v_scale[8 * c + k];
-                mul2(x[4 * k], x[4 * k + 1], f.x, f.y);
-                mul2(x[4 * k + 2], x[4 * k + 3], f.z, f.w);
+                mul2(y[4 * k], y[4 * k + 1], f.x, f.y);
+                mul2(y[4 * k + 2], y[4 * k + 3], f.z, f.w);
               }
-              if (!every) {
+              if constexpr (!EVERY) {
 #pragma unroll
                 for (uint32_t k = 0; k < 32; ++k)
-                  if (!(seen >> k & 1u)) x[k] = 0.f;         // not zero times a poisoned scale
+                  if (!(seen[c] >> k & 1u)) y[k] = 0.f;      // not zero times a poisoned scale
               }
-            } else if (poisoned) {
-              const uint32_t nan = bad[c] & seen;
+            } else if (!EVERY && poisoned) {
+              const uint32_t nan = bad[c] & seen[c];
 #pragma unroll
               for (uint32_t k = 0; k < 32; ++k)
-                if (nan >> k & 1u) x[k] = __uint_as_float(0x7fc00000u);
+                if (nan >> k & 1u) y[k] = __uint_as_float(0x7fc00000u);
             }
             uint32_t h[16];
 #pragma unroll
-            for (uint32_t k = 0; k < 16; ++k) h[k] = pack_half(x[2 * k], x[2 * k + 1]);
+            for (uint32_t k = 0; k < 16; ++k) h[k] = pack_half(y[2 * k], y[2 * k + 1]);
             tensor_write16(s_at + 16 * c, h);
           }
-          sum += sums[0] + sums[1];
+          sum += (sums[0] + sums[1]) + (sums[2] + sums[3]);
           tensor_write_wait();
           tc_fence_before();
-          __syncwarp();
-          if (lane == 0) bar_arrive(p_full(t));
+          return true;
+        };
+        if (row.part) {
+          if (every && !poisoned) ok = weights(std::true_type());
+          else ok = weights(std::false_type());
+          if (!ok) break;
         }
-        if (!ok) break;
+        __syncwarp();
+        if (lane == 0) bar_arrive(p_full(n));                // (a query tile without rows says so, too)
       }
-      tiles_before += n_units;
+      if (!ok) break;
     }
   } else if (warp < kFirstScout) {
     // ---------------------------------------------------------------------------------- codes into operands
     constexpr uint32_t TOK = F::TOK, LOADS = F::LOADS, HIGH = F::HIGH;
     const uint32_t first = (warp - 8) * TOK;                                 // this warp's tokens of a tile
     const uint32_t row_bytes = MX ? 16 * ((a.c.dim + 31) / 32) : a.c.dim;
-    uint4 code[2][LOADS];
+    uint4 code[2][2][LOADS];                                                 // of this tile and the next: [tile][keys, values]
     auto at_load = [&](uint32_t i, uint32_t* in, uint32_t* piece) {          // token of the tile, 16-byte piece of its row
       *in = first + (i % (TOK / HIGH)) * HIGH + lane % HIGH;
       *piece = (i / (TOK / HIGH)) * F::WIDE + lane / HIGH;
     };
-    auto fetch = [&](int w, const uint8_t* m) {
+    auto fetch = [&](uint4 (&code)[LOADS], int w, uint32_t n) {
+      const uint8_t* const m = meta + n % F::INFO * F::META;
 #pragma unroll
       for (uint32_t i = 0; i < LOADS; ++i) {
         uint32_t in, piece;
         at_load(i, &in, &piece);
         const int64_t row = reinterpret_cast<const int64_t*>(m)[in];
-        code[w][i] = make_uint4(0, 0, 0, 0);
-        if (row >= 0 && 16 * piece < row_bytes && (MX || p.vec_codes)) code[w][i] = __ldg(reinterpret_cast<const uint4*>(a.c.codes[w] + row + 16 * piece));
+        code[i] = make_uint4(0, 0, 0, 0);
+        if (row >= 0 && 16 * piece < row_bytes && (MX || p.vec_codes)) code[i] = __ldg(reinterpret_cast<const uint4*>(a.c.codes[w] + row + 16 * piece));
       }
       if constexpr (MX) return;
       else if (p.vec_codes) return;
@@ -581,21 +609,26 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
 #pragma unroll
           for (uint32_t k = 0; k < 4; ++k) if (b / 4 == k) v[k] |= byte;
         }
-        code[w][i] = make_uint4(v[0], v[1], v[2], v[3]);
+        code[i] = make_uint4(v[0], v[1], v[2], v[3]);
       }
     };
     bool ok = bar_wait(m_full(0), 0, failed);
-    if (ok) { fetch(0, meta); fetch(1, meta); }
-#pragma unroll 1
-    for (uint32_t n = 0; ok; ++n) {
-      const uint32_t s = n % F::STAGES, phase = (n / F::STAGES & 1) ^ 1;
+    auto last = [&](uint32_t n) { return (*reinterpret_cast<const int32_t*>(meta + n % F::INFO * F::META + F::AT_BITS + 40) & 4) != 0; };
+    if (ok) {
+      fetch(code[0][0], 0, 0); fetch(code[0][1], 1, 0);
+      if (!last(0)) {
+        ok = bar_wait(m_full(1), 0, failed);
+        if (ok) { fetch(code[1][0], 0, 1); fetch(code[1][1], 1, 1); }
+      }
+    }
+    // One tile; its registers take the codes of the next but one as soon as they are free.  false: that was the last, or a wait gave up.
+    auto convert = [&](uint32_t n, uint4 (&code)[2][LOADS]) -> bool {
+      const uint32_t s = n % F::STAGES, before = n - F::STAGES;              // the tile that had this stage
       const uint8_t* const m = meta + n % F::INFO * F::META;
-      const uint8_t* const m_next = meta + (n + 1) % F::INFO * F::META;
-      const bool more = !(*reinterpret_cast<const int32_t*>(m + F::AT_BITS + 40) & 4);
+      const bool more = !last(n), far = more && !last(n + 1);
 #pragma unroll
       for (int w = 0; w < 2; ++w) {
-        ok = ok && bar_wait(w ? v_empty(s) : k_empty(s), phase, failed);
-        if (!ok) break;
+        if (n >= F::STAGES && !bar_wait(w ? o_done(before) : s_done(before), before / 8 & 1, failed)) return false;
         const uint32_t tile = (w ? v_at : k_at) + s * F::KV_TILE;
 #pragma unroll
         for (uint32_t i = 0; i < LOADS; ++i) {
@@ -625,13 +658,16 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
         if (lane == 0) bar_arrive(w ? v_full(s) : k_full(s));
-        if (more) {
-          if (w == 0) ok = bar_wait(m_full((n + 1) % F::INFO), (n + 1) / F::INFO & 1, failed);
-          if (ok) fetch(w, m_next);
+        if (far) {
+          if (w == 0 && !bar_wait(m_full(n + 2), (n + 2) / 8 & 1, failed)) return false;
+          fetch(code[w], w, n + 2);
         }
       }
-      if (!more) break;
-    }
+      return more;
+    };
+    if (ok)
+#pragma unroll 1
+      for (uint32_t n = 0; convert(n, code[0]) && convert(n + 1, code[1]); n += 2) {}
   } else if (warp < kProducts) {
     // ---------------------------------------------------------------------------------- tokens
     constexpr uint32_t PER = KT / (32 * kScout), WORDS = F::SCALE_WORDS, PACKS = MX ? (NB + 3) / 4 : 1;
@@ -680,7 +716,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
     bool more = true;
 #pragma unroll 1
     for (uint32_t n = 0; more; ++n) {
-      const uint32_t s = n % F::INFO, phase = (n / F::INFO & 1) ^ 1;
+      const uint32_t s = n % F::INFO;
       float scale[PER][2];
       uint32_t bytes[PER][2][PACKS], high_byte[PER][2], real[PER], poisoned[PER];      // 4 bits: scales of the blocks, and the largest
       int64_t here[PER];
@@ -730,7 +766,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
 #pragma unroll
         for (uint32_t q = 0; q < PER; ++q) fetch_scales(u, q);
       }
-      if (!all_scouts(bar_wait(m_empty(s), phase, failed))) break;
+      if (!all_scouts(n < F::INFO || bar_wait(o_done(n - F::INFO), (n - F::INFO) / 8 & 1, failed))) break;
       int k_top = 1, any_flag = 0;
 #pragma unroll
       for (uint32_t k = 0; k < kScout; ++k) {
@@ -772,55 +808,55 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
     }
   } else {
     // ---------------------------------------------------------------------------------- products
-    uint32_t n = 0, q_turn[2] = {0, 0}, p_turn[2] = {0, 0};
-    auto scores = [&](uint32_t t, uint32_t s) {                              // by one lane
-#pragma unroll
-      for (uint32_t k = 0; k < DP / 16; ++k)
-        tensor_product(tmem + t * KT, rows_desc(q_at + t * F::Q_TILE + (k / 4) * F::Q_PANEL) + 2 * (k % 4), rows_desc(k_at + s * F::KV_TILE + (k / 4) * F::PANEL) + 2 * (k % 4),
-                       F::S_IDESC, k > 0);
-      tensor_commit(s_full(t));
-    };
-    auto results = [&](uint32_t t, uint32_t s, bool add) {
-#pragma unroll
-      for (uint32_t k = 0; k < KT / 16; ++k)
-        tensor_product_from(tmem + F::O_COL + t * DP, tmem + t * KT + 8 * k, columns_desc(v_at + s * F::KV_TILE, F::PANEL) + 128 * k, F::O_IDESC, add || k > 0);
-      tensor_commit(o_done(t));
-    };
+    // Scores run two tiles of tokens ahead of the results, so that a softmax finds the next ones ready.  Descriptors are made once and moved by
+    // constants (in units of 16 bytes): the one warp that issues is soon the slowest.
+    uint32_t n = 0, items = 0;
+    const uint64_t q_desc = rows_desc(q_at), k_desc = rows_desc(k_at), v_desc = columns_desc(v_at, F::PANEL);
     bool ok = true;
     do {
-      const uint32_t n_units = at.unit1 - at.unit, nt = QT == 2 && at.t.row1 - at.t.row0 > 128 ? 2 : 1;
-      for (uint32_t t = 0; ok && t < nt; ++t) { ok = bar_wait(q_full(t), q_turn[t] & 1, failed); ++q_turn[t]; }
-      ok = ok && bar_wait(k_full(n % 2), n / 2 & 1, failed);
-      if (!ok) break;
-      tc_fence_after();
-      if (elect_one()) {
-        for (uint32_t t = 0; t < nt; ++t) scores(t, n % 2);
-        tensor_commit(k_empty(n % 2));
-      }
-      __syncwarp();
-#pragma unroll 1
-      for (uint32_t u = 0; u < n_units; ++u, ++n) {
-        const bool more = u + 1 < n_units;
-        if (!bar_wait(v_full(n % 2), n / 2 & 1, failed)) { ok = false; break; }
-        for (uint32_t t = 0; t < nt; ++t) {
-          if (!bar_wait(p_full(t), p_turn[t] & 1, failed)) { ok = false; break; }
-          ++p_turn[t];
-          tc_fence_after();
-          if (elect_one()) {
-            results(t, n % 2, u > 0);
-            if (t + 1 == nt) { tensor_commit(v_empty(n % 2)); tensor_commit(m_empty(n % F::INFO)); }
-          }
-          __syncwarp();
-          if (!more) continue;
-          if (t == 0 && !bar_wait(k_full((n + 1) % 2), (n + 1) / 2 & 1, failed)) { ok = false; break; }
-          if (t == 0) tc_fence_after();
-          if (elect_one()) {
-            scores(t, (n + 1) % 2);
-            if (t + 1 == nt) tensor_commit(k_empty((n + 1) % 2));
-          }
-          __syncwarp();
+      const uint32_t n_units = at.unit1 - at.unit;
+      const bool both = QT == 2 && at.t.row1 - at.t.row0 > 128;
+      auto scores = [&](uint32_t m) {                                        // of tile m
+        const uint32_t s = m % F::STAGES;
+        ok = ok && bar_wait(k_full(s), m / F::STAGES & 1, failed);
+        if (!ok) return;
+        tc_fence_after();
+        if (elect_one()) {
+          const uint64_t kd = k_desc + s * (F::KV_TILE >> 4);
+          const uint32_t to = tmem + (m & 1) * KT;
+#pragma unroll
+          for (uint32_t t = 0; t < QT; ++t)
+            if (t == 0 || both)
+#pragma unroll
+              for (uint32_t k = 0; k < DP / 16; ++k)
+                tensor_product(to + 2 * t * KT, q_desc + ((t * F::Q_TILE + (k / 4) * F::Q_PANEL) >> 4) + 2 * (k % 4), kd + ((k / 4) * F::PANEL >> 4) + 2 * (k % 4),
+                               F::S_IDESC, k > 0);
+          tensor_commit(s_done(m));
         }
+        __syncwarp();
+      };
+      ok = bar_wait(q_full, items++ & 1, failed);
+      scores(n);
+      if (n_units > 1) scores(n + 1);
+#pragma unroll 1
+      for (uint32_t u = 0; ok && u < n_units; ++u, ++n) {
+        const uint32_t s = n % F::STAGES;
+        ok = bar_wait(v_full(s), n / F::STAGES & 1, failed) && bar_wait(p_full(n), n / 2 & 1, failed);
         if (!ok) break;
+        tc_fence_after();
+        if (elect_one()) {
+          const uint64_t vd = v_desc + s * (F::KV_TILE >> 4);
+          const uint32_t from = tmem + (n & 1) * KT, add = u > 0;
+#pragma unroll
+          for (uint32_t t = 0; t < QT; ++t)
+            if (t == 0 || both)
+#pragma unroll
+              for (uint32_t k = 0; k < KT / 16; ++k)
+                tensor_product_from(tmem + F::O_COL + t * DP, from + 2 * t * KT + 8 * k, vd + 128 * k, F::O_IDESC, k > 0 ? 1u : add);
+          tensor_commit(o_done(n));
+        }
+        __syncwarp();
+        if (u + 2 < n_units) scores(n + 2);
       }
     } while (ok && at.next(p));
     if (*failed) {                                                           // leave no product in flight
