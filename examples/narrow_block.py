@@ -1,7 +1,8 @@
 """A transformer block run in 4 bits: how far each of its outputs is from FP32, and which layers to leave there.
 
 A block of random weights (attention over a quantized paged cache, then a layer of experts) decodes a few tokens after a
-prompt, once in FP32 with plain torch operations and once through the 4-bit layers and the cache.  The framework's own
+prompt, once in FP32 with plain torch operations and once through the 4-bit layers and the cache: pages and positions planned
+on the GPU, heads normalized and rotated, keys and values rounded into their slots, attention straight over those.  The framework's own
 metrics then compare every stage's output, and its ranking says which layers lose most.
 
     python examples/narrow_block.py [--cache mx4|i8]
@@ -31,6 +32,14 @@ def attention(x, k, v, lens):
         out[row: row + new] = torch.einsum("thgs,shd->thgd", s, vs).reshape(new, HEADS * DIM)
         at, row = at + total, row + new
     return out
+
+
+def rotate(x, positions, freqs):
+    """x [tokens, heads, DIM]: RMS norm of every head, then the pairs (i, i + DIM / 2) turned by position * frequency."""
+    x = x * (x.square().mean(-1, keepdim=True) + 1e-6).rsqrt()
+    t = (positions.double()[:, None] * freqs.double())[:, None]
+    c, s, (a, b) = t.cos().float(), t.sin().float(), x.split(DIM // 2, -1)
+    return torch.cat((a * c - b * s, b * c + a * s), -1)
 
 
 class Block:
@@ -66,27 +75,30 @@ def run(ctx, cache_format=q.KV_MX4, prompts=(70, 33, 1, 128), steps=3, seed=0):
     block = Block(ctx, seed)
     g = torch.Generator(device="cuda").manual_seed(seed + 1)
     pages = [-(-(p + steps) // PAGE) for p in prompts]
-    ids = torch.randperm(sum(pages), device="cuda", generator=g).to(torch.int32)
-    table = torch.zeros(len(prompts), max(pages), dtype=torch.int32, device="cuda")
-    for i, n in enumerate(pages):
-        table[i, :n] = ids[sum(pages[:i]): sum(pages[: i + 1])]
+    free = torch.randperm(sum(pages), device="cuda", generator=g).to(torch.int32)       # pages that no sequence has yet, and how many
+    left = torch.tensor([sum(pages)], device="cuda")
+    table = torch.full((len(prompts), max(pages)), -1, dtype=torch.int32, device="cuda")
+    held = torch.zeros(len(prompts), dtype=torch.int64, device="cuda")
+    freqs = 10000.0 ** (-torch.arange(0, DIM, 2, device="cuda") / DIM)
+    ones = torch.ones(DIM, device="cuda")
     cache = ctx.kv_empty(sum(pages), PAGE, KV_HEADS, DIM, cache_format)
     past = [torch.empty(0, 2 * KV_HEADS, DIM, device="cuda") for _ in prompts]          # FP32 keys and values
     lens = [0] * len(prompts)
     for step in range(steps + 1):
         new = list(prompts) if step == 0 else [1] * len(prompts)
         x = torch.randn(sum(new), WIDTH, device="cuda", generator=g)
-        slots = torch.cat([table[i, torch.arange(n, n + c, device="cuda") // PAGE].long() * PAGE + torch.arange(n, n + c, device="cuda") % PAGE
-                           for i, (n, c) in enumerate(zip(lens, new))])
+        plan = ctx.kv_plan(held, torch.tensor(new, device="cuda"), PAGE, table, free, left, sum(new))
+        held, left = plan.lens, plan.free_count
         lens = [n + c for n, c in zip(lens, new)]
-        starts = torch.tensor([sum(lens[:i]) for i in range(len(lens) + 1)], device="cuda")
         both = list(zip(lens, new))
 
         qkv = x @ block.w["qkv"].T
-        kv = qkv[:, HEADS * DIM:].view(-1, 2 * KV_HEADS, DIM)
+        heads = qkv.view(-1, HEADS + 2 * KV_HEADS, DIM)
+        turned = rotate(heads[:, : HEADS + KV_HEADS], plan.positions, freqs)
+        kv = torch.cat((turned[:, HEADS:], heads[:, HEADS + KV_HEADS:]), 1)
         past = [torch.cat((p, part)) for p, part in zip(past, kv.split(new))]
         every = torch.cat(past)
-        att = attention(qkv[:, : HEADS * DIM], every[:, :KV_HEADS], every[:, KV_HEADS:], both)
+        att = attention(turned[:, :HEADS].reshape(-1, HEADS * DIM), every[:, :KV_HEADS], every[:, KV_HEADS:], both)
         out = att @ block.w["out"].T
 
         def plain(name, rows, offsets):
@@ -96,11 +108,11 @@ def run(ctx, cache_format=q.KV_MX4, prompts=(70, 33, 1, 128), steps=3, seed=0):
 
         h = x.bfloat16()
         nqkv = ctx.mx_linear(h, block.narrow["qkv"])
-        nkv = nqkv[:, HEADS * DIM:].unflatten(1, (2 * KV_HEADS, DIM))
-        ctx.kv_write(cache, nkv[:, :KV_HEADS], nkv[:, KV_HEADS:], slots)
-        k, v = ctx.kv_read(cache, table, starts, sum(lens))
-        natt = attention(nqkv[:, : HEADS * DIM].float(), k.float(), v.float(), both)
-        nout = ctx.mx_linear(natt.bfloat16(), block.narrow["out"])
+        nheads = nqkv.unflatten(1, (HEADS + 2 * KV_HEADS, DIM))
+        nq, nk = ctx.norm_rotate(nheads[:, :HEADS], nheads[:, HEADS: HEADS + KV_HEADS], plan.positions, freqs, ones, ones)
+        ctx.kv_write(cache, nk, nheads[:, HEADS + KV_HEADS:], plan.slots)
+        natt = ctx.kv_attend(cache, nq, plan.q_starts, plan.lens, table, max_new=max(new))
+        nout = ctx.mx_linear(natt.flatten(1), block.narrow["out"])
         # the experts of the FP32 pass, so that a token that changes sides does not drown the layers' own error
         rows = (h + nout)[order // TOP]
         nup = ctx.mx_linear_grouped(rows, offsets, block.narrow["up"])

@@ -572,7 +572,8 @@ int qv2_mx_matmul(qv2_ctx* ctx, const qv2_mx_matrix* a, const qv2_mx_matrix* w, 
                   const int64_t* offsets, void* y, uint32_t y_type, uint64_t y_ld);
 
 /* A product's kernel does not wait for its own copies for ever: after 2 seconds it gives up, its result is not valid, and the
- * next call that rounds, multiplies or uses the cache below returns QV2_ERR_TIMEOUT and does nothing.  qv2_check_waits asks
+ * next call that rounds, multiplies or uses the cache below returns QV2_ERR_TIMEOUT and does nothing; the same holds for the
+ * attention over the cache and what stands with it.  qv2_check_waits asks
  * without such a call: it waits for the context's stream and returns QV2_ERR_TIMEOUT if a product, or a replay of a
  * captured one, has given up since the last call that said so.  Replays on other streams are the caller's to wait
  * for.  QV2_ERR_UNSUPPORTED while the stream is capturing. */
