@@ -18,12 +18,13 @@ namespace qv2 {
 namespace {
 
 constexpr uint32_t kDepth = 2;                             // stages of a warp's ring
+constexpr uint32_t kBegin = 3;                             // what an item costs besides its units, in units
 constexpr int kWeightBits = 13;                            // weights stand 2^13 above p * scale / (largest scale)
 constexpr int kFactorBits = 12;                            // 4 bits: block factors stand 2^12 above scale / (largest of the row)
 
 __device__ __forceinline__ uint32_t shared_at(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, uint32_t bytes) {      // the rest of the 16 becomes zeros
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ void copy4(uint32_t dst, const void* src, bool there) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(there ? 4 : 0) : "memory");
@@ -84,6 +85,8 @@ struct RowsArgs {
   uint32_t hw, hw_log;                                     // key heads of a CTA (a power of two), warps / hw warps share the tokens
   uint32_t row_limit;                                      // sequences of more rows are not this kernel's
   uint32_t vec_q, vec_codes, vec_out;                      // queries and codes by 16 bytes, results by four elements
+  uint32_t quick;                                          // ... and rows of scales are whole aligned words
+  uint32_t token_codes, token_scales;                      // bytes of a token's codes and scales, all heads
   float* parts;
   AttendPiece* pieces;
 };
@@ -118,7 +121,7 @@ __global__ void __launch_bounds__(F::THREADS, 1) attend_rows_kernel(const RowsAr
     if (s >= a.seqs) return 0;
     uint32_t units, tiles;
     units_of<F>(p, attend_seq(a, s), &units, &tiles);
-    return (uint64_t)units * tiles * groups;
+    return (uint64_t)(units + kBegin) * tiles * groups;
   };
   uint64_t all = 0;
   for (uint32_t base = 0; base < a.seqs; base += kThreads) all += units_in(base + tid);
@@ -167,10 +170,13 @@ __global__ void __launch_bounds__(F::THREADS, 1) attend_rows_kernel(const RowsAr
     AttendSeq s = attend_seq(a, seq);
     uint32_t units, tiles;
     units_of<F>(p, s, &units, &tiles);
-    const uint64_t in_seq = (uint64_t)units * tiles * groups;
+    const uint32_t cost = units + kBegin;
+    const uint64_t in_seq = (uint64_t)cost * tiles * groups;
     if (at_unit - seq_begin >= in_seq) { seq_begin += in_seq; ++seq; continue; }
-    const uint32_t item = (uint32_t)((at_unit - seq_begin) / units), unit0 = (uint32_t)((at_unit - seq_begin) % units);
-    const uint32_t unit1 = (uint32_t)min((uint64_t)units, unit0 + (u_end - at_unit));
+    const uint32_t item = (uint32_t)((at_unit - seq_begin) / cost), x0 = (uint32_t)((at_unit - seq_begin) % cost);
+    const uint32_t x1 = (uint32_t)min((uint64_t)cost, x0 + (u_end - at_unit));
+    const uint32_t unit0 = max(x0, kBegin) - kBegin, unit1 = max(x1, kBegin) - kBegin;
+    if (unit0 == unit1) { at_unit += x1 - x0; continue; }                       // (of the setup alone there is nothing to do)
     const uint32_t tile = item / groups, hg = item % groups, kv = (hg << p.hw_log) + head_in;
     const uint32_t rows = s.n * a.group, row0 = tile * ROWS, row1 = min(rows, row0 + ROWS);
     const int32_t pos0 = s.len - (int32_t)s.n;                                  // position of the sequence's first query
@@ -179,7 +185,91 @@ __global__ void __launch_bounds__(F::THREADS, 1) attend_rows_kernel(const RowsAr
     const uint32_t j1 = max(min((uint32_t)(max(p_last, -1) + 1), a.room), j0);
     const int32_t* const pages = a.table + seq * a.table_ld;
 
-    // ---- queries: as operands, with what brings their scores back (to powers of two unless they are capped)
+    // ---- tokens: stage k of this warp begins at j0 + (first + k * parts) * TOK
+    const uint32_t n_stages = unit1 - unit0;
+    auto stage_token = [&](uint32_t k) { return (uint64_t)j0 + (uint64_t)((unit0 + k) * parts + part) * TOK; };
+    auto page_of = [&](uint32_t k) -> int32_t {                                  // of token `lane` of a stage; negative: no such token
+      const uint64_t j = stage_token(k) + lane;
+      if (k >= n_stages || lane >= TOK || j >= j1) return -1;
+      const int32_t id = __ldg(pages + p.page.div((uint32_t)j));
+      return id >= 0 && (uint32_t)id < a.c.pages ? id : -1;
+    };
+    constexpr uint32_t CH = F::RB / 16, PER = 32 / CH;                           // 16-byte pieces of a row, rows of one instruction
+    const uint32_t c16 = 16 * (lane % CH), tok0 = lane / CH;
+    const bool piece = c16 < row_bytes;
+    const uint32_t piece_bytes = piece ? 16 : 0;
+    const uint64_t row_in_token = (uint64_t)kv * row_bytes;
+    const uint8_t *const k_src = a.c.codes[0] + row_in_token + c16, *const v_src = a.c.codes[1] + row_in_token + c16;
+    const uint32_t k_dst = tok0 * F::KS + c16, v_dst = TOK * F::KS + tok0 * F::VS + c16;
+    const uint32_t scale_bytes = MX ? blocks : 4;                                // of a row
+    const uint8_t *const ks_src = a.c.scales[0] + (uint64_t)kv * scale_bytes, *const vs_src = a.c.scales[1] + (uint64_t)kv * scale_bytes;
+    auto fetch = [&](uint32_t k, int32_t id) {                                   // codes and scales of a stage into its place of the ring
+      const uint32_t place = (k % kDepth) * F::STAGE;
+      if (k < n_stages) {
+        const uint32_t j = (uint32_t)stage_token(k) + lane, off = j - p.page.div(j) * p.page.d;
+        const uint64_t token = (uint64_t)(uint32_t)max(id, 0) * p.page.d + (id < 0 ? 0 : off);      // in the cache
+        const int64_t bytes = (int64_t)(token * p.token_codes);
+        const uint32_t raw = place + TOK * (F::KS + F::VS), where = ring + place;
+        if (p.quick && __all_sync(0xffffffffu, id >= 0 || lane >= TOK)) {          // whole aligned words and pieces, and every token is there
+#pragma unroll
+          for (uint32_t i = 0; i < TOK / PER; ++i) {
+            const int64_t row = __shfl_sync(0xffffffffu, bytes, i * PER + tok0);
+            copy16(where + k_dst + i * PER * F::KS, k_src + row, piece_bytes);
+            copy16(where + v_dst + i * PER * F::VS, v_src + row, piece_bytes);
+          }
+          if (lane < TOK) {
+            const uint64_t first = token * p.token_scales;
+#pragma unroll
+            for (uint32_t i = 0; i < (MX ? (NB + 3) / 4 : 1); ++i)
+              if (!MX || 4 * i + 4 <= blocks) {
+                copy4(ring + raw + lane * F::RAW + 4 * i, ks_src + first + 4 * i, true);
+                copy4(ring + raw + TOK * F::RAW + lane * F::RAW + 4 * i, vs_src + first + 4 * i, true);
+              }
+            *reinterpret_cast<uint32_t*>(mine + raw + 2 * TOK * F::RAW + 4 * lane) = 0u;
+          }
+        } else {
+          const int64_t known = id < 0 ? -1 : bytes;
+#pragma unroll 1
+          for (uint32_t i = 0; i < TOK / PER; ++i) {
+            const int64_t row = __shfl_sync(0xffffffffu, known, i * PER + tok0);
+            const bool there = row >= 0 && piece;
+            const uint64_t from = there ? (uint64_t)row : 0;
+            if (MX || p.vec_codes) {
+              copy16(where + k_dst + i * PER * F::KS, k_src + from, there ? 16 : 0);
+              copy16(where + v_dst + i * PER * F::VS, v_src + from, there ? 16 : 0);
+            } else
+              for (uint32_t b = 0; b < 16; ++b) {
+                const bool has = there && c16 + b < row_bytes;
+                mine[place + k_dst + i * PER * F::KS + b] = has ? __ldg(k_src + from + b) : (uint8_t)0;
+                mine[place + v_dst + i * PER * F::VS + b] = has ? __ldg(v_src + from + b) : (uint8_t)0;
+              }
+          }
+          if (lane < TOK) {
+            const uint64_t first = token * p.token_scales;
+            uint32_t skip = 0;
+#pragma unroll
+            for (int w = 0; w < 2; ++w) {                                        // whole words, each of which holds a wanted byte
+              const uintptr_t from = (uintptr_t)(w ? vs_src : ks_src) + first;
+              const uint32_t lead = (uint32_t)(from & 3u);
+              skip |= lead << (8 * w);
+#pragma unroll
+              for (uint32_t i = 0; i < F::RAW / 4; ++i)
+                if (4 * i < lead + scale_bytes) copy4(ring + raw + w * TOK * F::RAW + lane * F::RAW + 4 * i, (const void*)((from & ~(uintptr_t)3u) + 4 * i), id >= 0);
+            }
+            *reinterpret_cast<uint32_t*>(mine + raw + 2 * TOK * F::RAW + 4 * lane) = id >= 0 ? skip : ~0u;
+          }
+        }
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    int32_t next_id = page_of(0);
+#pragma unroll 1
+    for (uint32_t k = 0; k < kDepth; ++k) {
+      const int32_t id = next_id;
+      next_id = page_of(k + 1);
+      fetch(k, id);
+    }
+    // ---- queries, while the first stages are on their way: as operands, with what brings their scores back (to powers of two unless they are capped)
     uint32_t qf[TERMS][NT][4 * NB];
     float back[NT][2];
     int32_t pos[NT][2];
@@ -253,72 +343,6 @@ __global__ void __launch_bounds__(F::THREADS, 1) attend_rows_kernel(const RowsAr
         for (int k = 0; k < 4; ++k) o[n][m][k] = 0.f;
     }
 
-    // ---- tokens: stage k of this warp begins at j0 + (first + k * parts) * TOK
-    const uint32_t n_stages = unit1 - unit0;
-    auto stage_token = [&](uint32_t k) { return (uint64_t)j0 + (uint64_t)((unit0 + k) * parts + part) * TOK; };
-    auto page_of = [&](uint32_t k) -> int32_t {                                  // of token `lane` of a stage; negative: no such token
-      const uint64_t j = stage_token(k) + lane;
-      if (k >= n_stages || lane >= TOK || j >= j1) return -1;
-      const int32_t id = __ldg(pages + p.page.div((uint32_t)j));
-      return id >= 0 && (uint32_t)id < a.c.pages ? id : -1;
-    };
-    constexpr uint32_t CH = F::RB / 16, PER = 32 / CH;                           // 16-byte pieces of a row, rows of one instruction
-    const uint32_t c16 = 16 * (lane % CH), tok0 = lane / CH;
-    const bool piece = c16 < row_bytes;
-    const uint8_t *const k_src = a.c.codes[0] + c16, *const v_src = a.c.codes[1] + c16;
-    const uint32_t k_dst = tok0 * F::KS + c16, v_dst = TOK * F::KS + tok0 * F::VS + c16;
-    auto fetch = [&](uint32_t k, int32_t id) {                                   // codes and scales of a stage into its place of the ring
-      const uint32_t place = (k % kDepth) * F::STAGE;
-      if (k < n_stages) {
-        const uint32_t j = (uint32_t)stage_token(k) + lane, off = j - p.page.div(j) * p.page.d;
-        const uint64_t at = id < 0 ? 0 : ((uint64_t)(uint32_t)id * p.page.d + off) * a.c.heads + kv;
-        const int64_t bytes = id < 0 ? -1 : (int64_t)(at * row_bytes);
-#pragma unroll
-        for (uint32_t i = 0; i < TOK / PER; ++i) {
-          const int64_t row = __shfl_sync(0xffffffffu, bytes, i * PER + tok0);
-          const bool there = row >= 0 && piece;
-          const uint64_t from = there ? (uint64_t)row : 0;
-          if (MX || p.vec_codes) {
-            copy16(ring + place + k_dst + i * PER * F::KS, k_src + from, there);
-            copy16(ring + place + v_dst + i * PER * F::VS, v_src + from, there);
-          } else
-            for (uint32_t b = 0; b < 16; ++b) {
-              const bool has = there && c16 + b < row_bytes;
-              mine[place + k_dst + i * PER * F::KS + b] = has ? __ldg(k_src + from + b) : (uint8_t)0;
-              mine[place + v_dst + i * PER * F::VS + b] = has ? __ldg(v_src + from + b) : (uint8_t)0;
-            }
-        }
-        const uint32_t raw = place + TOK * (F::KS + F::VS);
-        if (lane < TOK) {
-          if (MX) {
-            const uint64_t first = at * blocks;
-            uint32_t skip = 0;
-#pragma unroll
-            for (int w = 0; w < 2; ++w) {                                        // whole words, each of which holds a wanted byte
-              const uintptr_t from = (uintptr_t)a.c.scales[w] + first;
-              const uint32_t lead = (uint32_t)(from & 3u);
-              skip |= lead << (8 * w);
-#pragma unroll
-              for (uint32_t i = 0; i < F::RAW / 4; ++i)
-                if (4 * i < lead + blocks) copy4(ring + raw + w * TOK * F::RAW + lane * F::RAW + 4 * i, (const void*)((from & ~(uintptr_t)3u) + 4 * i), id >= 0);
-            }
-            *reinterpret_cast<uint32_t*>(mine + raw + 2 * TOK * F::RAW + 4 * lane) = id >= 0 ? skip : ~0u;
-          } else {
-#pragma unroll
-            for (int w = 0; w < 2; ++w) copy4(ring + raw + w * TOK * F::RAW + 4 * lane, reinterpret_cast<const float*>(a.c.scales[w]) + at, id >= 0);
-            *reinterpret_cast<uint32_t*>(mine + raw + 2 * TOK * F::RAW + 4 * lane) = id >= 0 ? 0u : ~0u;
-          }
-        }
-      }
-      asm volatile("cp.async.commit_group;" ::: "memory");
-    };
-    int32_t next_id = page_of(0);
-#pragma unroll 1
-    for (uint32_t k = 0; k < kDepth; ++k) {
-      const int32_t id = next_id;
-      next_id = page_of(k + 1);
-      fetch(k, id);
-    }
 #pragma unroll 1
     for (uint32_t k = 0; k < n_stages; ++k) {
       asm volatile("cp.async.wait_group %0;" ::"n"(kDepth - 1) : "memory");
@@ -596,7 +620,7 @@ __global__ void __launch_bounds__(F::THREADS, 1) attend_rows_kernel(const RowsAr
     float* const to_part = p.parts + ((uint64_t)blockIdx.x * 2 + place) * p.hw * F::PIECE;
     if (!whole && place == 1 && tid == 0) {
       // the item's last unit is among those of CTA c where c * all / ctas <= last < (c + 1) * all / ctas
-      const uint64_t last = at_unit + units - 1;
+      const uint64_t last = at_unit - x0 + cost - 1;
       uint32_t c = (uint32_t)(last * ctas / all);
       while (all * c / ctas > last) --c;
       while (all * (c + 1) / ctas <= last) ++c;
@@ -625,7 +649,7 @@ __global__ void __launch_bounds__(F::THREADS, 1) attend_rows_kernel(const RowsAr
       }
     }
     __syncthreads();
-    at_unit += unit1 - unit0;
+    at_unit += x1 - x0;
   }
 }
 
@@ -781,7 +805,9 @@ AttendRun plan_kv_attend(const AttendArgs& a, int sm_count) {
   r.dp = a.c.dim <= 64 ? 64 : a.c.dim <= 128 ? 128 : 256;
   r.terms = a.dtype == kF32 ? 2 : 1;
   const uint64_t most = (uint64_t)a.max_new * a.group;             // query rows of a sequence and key head
-  r.rows = r.dp <= 128 && most > 8 ? 16 : 8;
+  // Sixteen rows to an item where sequences have more than eight (drafts), or a single token has; where long chunks are mixed with single
+  // tokens, which the latter get eight (attend 24 sequences of 12 heads over 4, half of them single tokens: 39 us for those with sixteen, see below).
+  r.rows = r.dp <= 128 && most > 8 && (most <= 16 || a.group > 8) ? 16 : 8;
   // Sequences of more than 16 rows go to the tensor cores' tiles of 128 rows, which binary32 has no operands for.
   r.few = r.terms == 2 || most <= 16 ? 0xffffffffu : a.seqs == 1 ? 0 : 16;
   r.hw_log = 0;
@@ -807,6 +833,10 @@ cudaError_t launch_kv_attend(const Launch& l, const AttendArgs& a, const AttendR
     p.a = a; p.page = FastDiv(a.c.page_size); p.group = FastDiv(a.group);
     p.hw = 1u << run.hw_log; p.hw_log = run.hw_log; p.row_limit = run.few;
     p.vec_codes = a.c.dim % 16 == 0 && ((uintptr_t)a.c.codes[0] | (uintptr_t)a.c.codes[1]) % 16 == 0;
+    const uint32_t blocks = (a.c.dim + 31) / 32;
+    const bool mx = a.c.format == QV2_KV_MX4;
+    p.token_codes = a.c.heads * (mx ? 16 * blocks : a.c.dim); p.token_scales = a.c.heads * (mx ? blocks : 4);
+    p.quick = (mx || p.vec_codes) && (!mx || blocks % 4 == 0) && ((uintptr_t)a.c.scales[0] | (uintptr_t)a.c.scales[1]) % 4 == 0;
     p.vec_q = a.c.dim % 8 == 0 && ((uintptr_t)a.q | a.q_token_ld * dtype_size(a.dtype) | a.q_head_ld * dtype_size(a.dtype)) % 16 == 0;
     p.vec_out = attend_vec_out(a);
     cudaError_t e = a.c.format == QV2_KV_MX4 ? launch_dim<QV2_KV_MX4>(l, p, run, launches) : launch_dim<QV2_KV_I8>(l, p, run, launches);
