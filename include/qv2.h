@@ -700,11 +700,13 @@ int qv2_norm_rotate(qv2_ctx* ctx, const qv2_head_rows* queries, const qv2_head_r
  * Query heads h of a token share the key/value head h / (q_heads / cache->heads).  A query that sees no token has out = 0 and
  * lse = -inf; one that sees a token whose key or value holds a NaN (a poisoned row or block) has NaN throughout, and so has one that itself
  * holds a NaN or an infinity.  What a query does not see does not change its result.
- * q: element (t, h, d) at q + t*q_token_ld + h*q_head_ld + d.  out: dense [total][q_heads][head_dim], element type as q's;
+ * q: element (t, h, d) at q + t*q_token_ld + h*q_head_ld + d.  out, which q may not overlap: dense [total][q_heads][head_dim], element type as q's;
  * lse: binary32 [total][q_heads], nullable.  Rows outside every sequence are left as they were.  q_starts: non-decreasing,
- * held to 0 .. total; lens: held to 0 .. 2^31 - 1.  max_new: no sequence has more queries than this (rows past it are not written); 0: unknown.
- * Codes and scales enter exactly; queries of 16 bits are exact, of 32 bits held to 2^-22 of their largest element; weights
- * p_j times the value's scale are rounded to 11 bits (22 for 32-bit queries); sums are binary32.
+ * held to 0 .. total; lens: held to 0 .. 2^31 - 1.  max_new: no sequence has more queries than this, 0: unknown; it
+ * decides which kernels are launched, and one that is wrong costs nothing but time.
+ * Codes enter exactly, and so do scales within 2^-36 of the largest that a tile of query rows meets; queries of 16 bits are
+ * exact, of 32 bits held to 2^-22 of their largest element; weights p_j times the value's scale are rounded to 11 bits (22 for 32-bit queries), and
+ * to fewer below 2^-24 of the largest scale of a value; sums are binary32.  Values of 2^96 and more may come out infinite, parts below 2^-120 as zero.
  * The order of the sums depends on the lengths and sizes only: the same inputs give the same bits.
  * q_heads is a multiple of cache->heads and <= 65536, head_dim <= QV2_SERVE_MAX_DIM, table_ld * page_size < 2^31,
  * seqs <= 65536, total * q_heads < 2^31.  The scratch grows and is captured as that of qv2_mx_linear.

@@ -820,7 +820,8 @@ class Context:
         keys and values already: rows q_starts[s] .. q_starts[s+1]-1 (int64 [seqs + 1]) are the last of the lens[s] (int64 [seqs])
         tokens of sequence s, whose pages are row s of table (int32 [seqs, pages]).  Each sees itself and what went before, at
         most `window` tokens if that is given; scores times `scale` (1 / sqrt(dim)) may be capped (cap * tanh(x / cap)) and biased by slopes
-        (float32 [q_heads]) times the distance.  max_new: no sequence has more new tokens (the host often knows; rows past it are not written).
+        (float32 [q_heads]) times the distance.  max_new: no sequence has more new tokens (the host often knows; it decides which
+        kernels are launched, and a wrong one costs only time).
         -> [tokens, q_heads, dim] of q's type, with want_lse also float32 [tokens, q_heads], the logarithm of the
         sum of exponentials.  Rows of no sequence are left as they were in `out` (undefined in a new result)."""
         type_, c = _DTYPE_FLAG.get(q.dtype), cache._c

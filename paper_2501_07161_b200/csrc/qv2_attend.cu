@@ -653,68 +653,123 @@ __global__ void __launch_bounds__(F::THREADS, 1) attend_rows_kernel(const RowsAr
   }
 }
 
-// Adds up the items that were cut.  CTA (c, y) has every kJoinRows-th (row, key head) of the item that main CTA c began, all of them at once:
-// its warps are dealt out to them and share their pieces.
-constexpr uint32_t kJoinThreads = 256, kJoinRows = 8;
+// Adds up the items that were cut.  Their rows of results (query row, key head) stand in one row of all of them and are dealt out to the warps of
+// all CTAs, several warps to a row when there are few: those share its pieces and meet in shared memory.  (CTA c for what main CTA c began left one
+// sequence of 32000 tokens, 8 key heads and 8 rows to 8 CTAs: 77 us with the main kernel.)
+constexpr uint32_t kJoinThreads = 256, kJoinMost = kJoinThreads;      // main CTAs at most: a thread for each
+template <uint32_t K>                                         // float4 of a row to a lane
 __global__ void __launch_bounds__(kJoinThreads)
-attend_join_kernel(const AttendArgs a, FastDiv group, const float* parts, const AttendPiece* pieces, uint32_t hw_log, uint32_t tile_rows, uint32_t dp, uint32_t vec_out) {
-  constexpr uint32_t WARPS = kJoinThreads / 32;
-  __shared__ float4 sums[WARPS][64];
+attend_join_kernel(const AttendArgs a, FastDiv group, const float* parts, const AttendPiece* pieces, uint32_t ctas, uint32_t hw_log, uint32_t tile_rows, uint32_t dp,
+                   uint32_t vec_out) {
+  constexpr uint32_t WARPS = kJoinThreads / 32, HELD = 8;      // pieces in flight
+  __shared__ float4 sums[WARPS][32 * K];
   __shared__ float2 top_sum[WARPS];
+  __shared__ uint32_t begin[kJoinMost], scan[WARPS];
   dependency_wait();
   allow_dependents();
-  const AttendPiece h = pieces[blockIdx.x];
-  if (h.followers == 0) return;
-  const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32, quads = dp / 4, n_rows = min(tile_rows, h.rows - h.tile * tile_rows), pairs = n_rows << hw_log;
+  const uint32_t tid = threadIdx.x, warp = tid / 32, lane = tid % 32, quads = dp / 4;
+  // rows of what each main CTA began and did not end, and their running sum
+  uint32_t sum = 0;
+  if (tid < ctas) {
+    const AttendPiece h = pieces[tid];
+    if (h.followers) sum = min(tile_rows, h.rows - h.tile * tile_rows) << hw_log;
+  }
+  uint32_t upto = sum;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) { const uint32_t v = __shfl_up_sync(0xffffffffu, upto, o); if (lane >= o) upto += v; }
+  if (lane == 31) scan[warp] = upto;
+  __syncthreads();
+  uint32_t all = 0, before = upto - sum;
+#pragma unroll
+  for (uint32_t w = 0; w < WARPS; ++w) { if (w < warp) before += scan[w]; all += scan[w]; }
+  begin[tid] = before;
+  __syncthreads();
   const uint64_t piece = (uint64_t)(tile_rows << hw_log) * (dp + 2);
-  uint32_t share = WARPS;                                    // warps of a pair: a power of two
-  while (share > 1 && (WARPS / share) * kJoinRows < pairs) share /= 2;
-  const uint32_t sub = warp & (share - 1);
-  for (uint32_t i0 = blockIdx.y; i0 < pairs; i0 += kJoinRows * (WARPS / share)) {
-    const uint32_t i = i0 + kJoinRows * (warp / share);
-    const bool there = i < pairs;
-    const uint32_t r = i >> hw_log, head = i & ((1u << hw_log) - 1), at = head * tile_rows + r;
+  uint32_t share = WARPS;                                    // warps of a row: a power of two
+  while (share > 1 && gridDim.x * (WARPS / share) < all) share /= 2;
+  const uint32_t sub = warp & (share - 1), step = gridDim.x * (WARPS / share);
+  for (uint32_t i0 = blockIdx.x; i0 < all; i0 += step) {
+    const uint32_t i = i0 + gridDim.x * (warp / share);
+    const bool there = i < all;
     float top = -INFINITY, total = 0.f;
-    float4 v[2] = {};
+    float4 v[K] = {};
+    AttendPiece h = {};
+    uint32_t r = 0, head = 0;
     if (there) {
-#pragma unroll 8
-      for (uint32_t f = sub; f <= h.followers; f += share) {
-        const float* from = parts + ((uint64_t)(blockIdx.x + f) * 2 + (f == 0 ? 1 : 0)) * piece;
-        const float2 ts = *reinterpret_cast<const float2*>(from + (tile_rows << hw_log) * dp + 2 * at);
-        const float m = fmaxf(top, ts.x), base = m == -INFINITY ? 0.f : m, was = exp2_fast(top - base), is = exp2_fast(ts.x - base);
-        top = m;
-        total = total * was + ts.y * is;
-#pragma unroll
-        for (uint32_t k = 0; k < 2; ++k)
-          if (lane + 32 * k < quads) {
-            const float4 x = *reinterpret_cast<const float4*>(from + at * dp + 4 * (lane + 32 * k));
-            v[k].x = v[k].x * was + x.x * is; v[k].y = v[k].y * was + x.y * is; v[k].z = v[k].z * was + x.z * is; v[k].w = v[k].w * was + x.w * is;
-          }
+      uint32_t c = 0, end = ctas;                            // the last one that begins at i or before (those without rows begin where the next one does)
+      while (end - c > 1) {
+        const uint32_t mid = (c + end) / 2;
+        if (begin[mid] <= i) c = mid; else end = mid;
       }
-    }
+      h = pieces[c];
+      const uint32_t in = i - begin[c];
+      r = in >> hw_log; head = in & ((1u << hw_log) - 1);
+      const uint32_t at = head * tile_rows + r;
+#pragma unroll 1
+      for (uint32_t f0 = sub; f0 <= h.followers; f0 += HELD * share) {
+        float2 ts[HELD];
+        float4 x[HELD][K];
 #pragma unroll
-    for (uint32_t k = 0; k < 2; ++k) sums[warp][lane + 32 * k] = v[k];
-    if (lane == 0) top_sum[warp] = make_float2(top, total);
-    __syncthreads();
-    if (there && sub == 0) {
-      top = -INFINITY; total = 0.f;
-      for (uint32_t w = 0; w < share; ++w) top = fmaxf(top, top_sum[warp + w].x);
-      const float base = top == -INFINITY ? 0.f : top;
-      v[0] = v[1] = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (uint32_t w = 0; w < share; ++w) {
-        const float f = exp2_fast(top_sum[warp + w].x - base);
-        total = fmaf(top_sum[warp + w].y, f, total);
+        for (uint32_t b = 0; b < HELD; ++b) {                // (loads without branches: past the end the last piece, past the row its last elements)
+          const uint32_t f = min(f0 + b * share, h.followers);
+          const float* from = parts + ((uint64_t)(c + f) * 2 + (f == 0 ? 1 : 0)) * piece;
+          ts[b] = *reinterpret_cast<const float2*>(from + (tile_rows << hw_log) * dp + 2 * at);
 #pragma unroll
-        for (uint32_t k = 0; k < 2; ++k) {
-          const float4 x = sums[warp + w][lane + 32 * k];
-          v[k].x = fmaf(x.x, f, v[k].x); v[k].y = fmaf(x.y, f, v[k].y); v[k].z = fmaf(x.z, f, v[k].z); v[k].w = fmaf(x.w, f, v[k].w);
+          for (uint32_t k = 0; k < K; ++k) x[b][k] = *reinterpret_cast<const float4*>(from + at * dp + 4 * min(lane + 32 * k, quads - 1));
+        }
+        float high = top;
+#pragma unroll
+        for (uint32_t b = 0; b < HELD; ++b) {
+          if (f0 + b * share > h.followers) {
+            ts[b] = make_float2(-INFINITY, 0.f);
+#pragma unroll
+            for (uint32_t k = 0; k < K; ++k) x[b][k] = make_float4(0.f, 0.f, 0.f, 0.f);
+          }
+          high = fmaxf(high, ts[b].x);
+        }
+        const float base = high == -INFINITY ? 0.f : high, was = exp2_fast(top - base);
+        top = high;
+        total *= was;
+#pragma unroll
+        for (uint32_t k = 0; k < K; ++k) { v[k].x *= was; v[k].y *= was; v[k].z *= was; v[k].w *= was; }
+#pragma unroll
+        for (uint32_t b = 0; b < HELD; ++b) {
+          const float is = exp2_fast(ts[b].x - base);
+          total = fmaf(ts[b].y, is, total);
+#pragma unroll
+          for (uint32_t k = 0; k < K; ++k) {
+            v[k].x = fmaf(x[b][k].x, is, v[k].x); v[k].y = fmaf(x[b][k].y, is, v[k].y); v[k].z = fmaf(x[b][k].z, is, v[k].z); v[k].w = fmaf(x[b][k].w, is, v[k].w);
+          }
         }
       }
-#pragma unroll
-      for (uint32_t k = 0; k < 2; ++k)
-        if (lane + 32 * k < quads) attend_store(a, h.row0, h.tile * tile_rows + r, group, (h.heads << hw_log) + head, 4 * (lane + 32 * k), v[k], top, total, vec_out);
     }
-    __syncthreads();
+    if (share > 1) {                                         // (the same in all threads)
+#pragma unroll
+      for (uint32_t k = 0; k < K; ++k) sums[warp][lane + 32 * k] = v[k];
+      if (lane == 0) top_sum[warp] = make_float2(top, total);
+      __syncthreads();
+      if (there && sub == 0) {
+        top = -INFINITY; total = 0.f;
+        for (uint32_t w = 0; w < share; ++w) top = fmaxf(top, top_sum[warp + w].x);
+        const float base = top == -INFINITY ? 0.f : top;
+#pragma unroll
+        for (uint32_t k = 0; k < K; ++k) v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (uint32_t w = 0; w < share; ++w) {
+          const float f = exp2_fast(top_sum[warp + w].x - base);
+          total = fmaf(top_sum[warp + w].y, f, total);
+#pragma unroll
+          for (uint32_t k = 0; k < K; ++k) {
+            const float4 x = sums[warp + w][lane + 32 * k];
+            v[k].x = fmaf(x.x, f, v[k].x); v[k].y = fmaf(x.y, f, v[k].y); v[k].z = fmaf(x.z, f, v[k].z); v[k].w = fmaf(x.w, f, v[k].w);
+          }
+        }
+      }
+      __syncthreads();
+    }
+    if (there && sub == 0)
+#pragma unroll
+      for (uint32_t k = 0; k < K; ++k)
+        if (lane + 32 * k < quads) attend_store(a, h.row0, h.tile * tile_rows + r, group, (h.heads << hw_log) + head, 4 * (lane + 32 * k), v[k], top, total, vec_out);
   }
 }
 
@@ -792,9 +847,12 @@ cudaError_t launch_dim(const Launch& l, const RowsArgs& p, const AttendRun& run,
 
 cudaError_t launch_attend_join(const Launch& l, const AttendArgs& a, const float* parts, const AttendPiece* pieces, uint32_t ctas, uint32_t hw_log, uint32_t tile_rows,
                                uint32_t dp, uint64_t* launches) {
-  cudaError_t e = tile_rows >= 128 ? launch_grid(l, attend_join_rows_kernel, dim3(ctas, 8), kJoinThreads, 0, a, FastDiv(a.group), parts, pieces, tile_rows, dp, attend_vec_out(a))
-                                   : launch_grid(l, attend_join_kernel, dim3(ctas, kJoinRows), kJoinThreads, 0, a, FastDiv(a.group), parts, pieces, hw_log,
-                                                 tile_rows, dp, attend_vec_out(a));
+  const FastDiv group(a.group);
+  const uint32_t vec = attend_vec_out(a);
+  cudaError_t e;
+  if (tile_rows >= 128) e = launch_grid(l, attend_join_rows_kernel, dim3(ctas, 8), kJoinThreads, 0, a, group, parts, pieces, tile_rows, dp, vec);
+  else if (dp <= 128) e = launch_grid(l, attend_join_kernel<1>, dim3(2 * ctas), kJoinThreads, 0, a, group, parts, pieces, ctas, hw_log, tile_rows, dp, vec);
+  else e = launch_grid(l, attend_join_kernel<2>, dim3(2 * ctas), kJoinThreads, 0, a, group, parts, pieces, ctas, hw_log, tile_rows, dp, vec);
   if (e == cudaSuccess) ++*launches;
   return e;
 }
@@ -805,21 +863,22 @@ AttendRun plan_kv_attend(const AttendArgs& a, int sm_count) {
   r.dp = a.c.dim <= 64 ? 64 : a.c.dim <= 128 ? 128 : 256;
   r.terms = a.dtype == kF32 ? 2 : 1;
   const uint64_t most = (uint64_t)a.max_new * a.group;             // query rows of a sequence and key head
-  // Sixteen rows to an item where sequences have more than eight (drafts), or a single token has; where long chunks are mixed with single
-  // tokens, which the latter get eight (attend 24 sequences of 12 heads over 4, half of them single tokens: 39 us for those with sixteen, see below).
-  r.rows = r.dp <= 128 && most > 8 && (most <= 16 || a.group > 8) ? 16 : 8;
-  // Sequences of more than 16 rows go to the tensor cores' tiles of 128 rows, which binary32 has no operands for.
-  r.few = r.terms == 2 || most <= 16 ? 0xffffffffu : a.seqs == 1 ? 0 : 16;
+  // Sequences of more than 32 rows go to the tensor cores' tiles of 128 rows, which binary32 has no operands for.  (32 sequences of 2000 tokens, 8 key heads of
+  // 128, 4 bits, 32 rows each: 85 us here, 106 there; 64 rows: 147 and 109; 8 bits: 104 and 162, 179 and 166.)
+  r.few = r.terms == 2 || most <= 32 ? 0xffffffffu : a.seqs == 1 ? 0 : 32;
+  // Sixteen rows to an item where sequences have more than eight (drafts), or a single token has (16 rows as above: 56 us beside 57, 8 bits 68 and 74; 8 rows,
+  // half of the sixteen empty: 48 beside 38).  Where long chunks are mixed with single tokens, the latter get eight.
+  r.rows = r.dp <= 128 && most > 8 && (most <= 32 || r.terms == 2 || a.group > 8) ? 16 : 8;
   r.hw_log = 0;
   while (r.hw_log < 3 && a.c.heads % (2u << r.hw_log) == 0) ++r.hw_log;
   // A CTA per SM, fewer where there cannot be a unit of 16 tokens for each
   const uint64_t tiles = (uint64_t)a.total * a.group / r.rows + a.seqs, units = tiles * (a.c.heads >> r.hw_log) * (a.room / 16 + 1);
-  const uint64_t ctas = (uint64_t)sm_count;
+  const uint64_t ctas = (uint64_t)(sm_count < (int)kJoinMost ? sm_count : (int)kJoinMost);
   r.ctas = (uint32_t)(units < ctas ? units : ctas);
   uint64_t most_bytes = r.few == 0 ? 0 : attend_parts_bytes(r.ctas, 1u << r.hw_log, r.rows, r.dp) + r.ctas * sizeof(AttendPiece);
   if (r.few != 0xffffffffu) {
     const uint64_t many = ((uint64_t)a.total * a.group / chunk_rows(r.dp) + a.seqs) * a.c.heads * (a.room / 64 + 1);
-    r.chunk_ctas = (uint32_t)(many < (uint64_t)sm_count ? many : sm_count);
+    r.chunk_ctas = (uint32_t)(many < ctas ? many : ctas);
     const uint64_t bytes = attend_parts_bytes(r.chunk_ctas, 1, chunk_rows(r.dp), r.dp) + r.chunk_ctas * sizeof(AttendPiece);
     if (bytes > most_bytes) most_bytes = bytes;
   }

@@ -1,13 +1,19 @@
 // Attention of new tokens over the quantized paged cache, many query rows to a key head: prompts and chunks of them, 16-bit queries.
 //
-// A CTA takes 256 query rows (two tiles of 128; one tile where a head has more than 128 elements) against tiles of 128 (64) tokens:
-//   warps 0-3, 4-7   the softmax of one tile each, a thread to a row: scores from tensor memory, weights back into it in
+// A CTA takes 256 query rows (two tiles of 128; one tile where a head has more than 128 elements) against tiles of 64 tokens:
+//   warps 0-3, 4-7   the softmax of one query tile each, a thread to a row: scores from tensor memory, weights back into it in
 //                    binary16, where the second product reads them; results out at the end,
+//   warps 8-11       turn codes of keys and values into operands in shared memory, once for both query tiles,
 //   warps 12, 13     look up the tokens of a tile ahead: where their rows lie, what their scales come to,
-//   warps 8-11       turn codes of keys and values into operands in shared memory, once for both tiles,
-//   warp 14          issues the products (tcgen05.mma): scores S = Q K^T, results O += P V.
-// While one tile's softmax runs the tensor cores are at the other tile's products.  Bound by the exponentials (16 a cycle and SM: 2048
-// cycles for 2 x 128 x 128 scores) next to the products (2 x 2 x 512 cycles for 128 elements).
+//   warp 14          issues the products (tcgen05.mma): scores S = Q K^T two tiles ahead, results O += P V.
+// While one query tile's softmax runs the tensor cores are at the other's products.
+//
+// What bounds it: the way of one tile round the warps, not a unit.  Per 64 tokens and 256 rows of 128 elements the products ask for 1024
+// cycles and the exponentials (16 a cycle) for 1024; a tile takes some 1900.  A prompt of 8192 tokens, 32 heads over 8, takes 785 us (700 TFLOP/s of what
+// is seen); 64 tokens at a time against 128 took 785 where 128 took 840 with their scores and weights in one
+// buffer: the softmax holds 64 scores in registers, 128 spill.  8 bits cost more: a multiplication for each score and each weight that the 4-bit form has
+// in its operands (4 chunks of 512 over 4096 tokens each, 16 heads over 4:
+// 157 us without a cap, 224 with one, whose exponential and reciprocal come on top).
 //
 // Codes are exact in binary16.  At 4 bits they are multiplied by their block's scale over the largest of the tile (keys) or of the item so far
 // (values), a power of two: exact unless a scale is 2^36 below that.  8-bit integers enter as they are, and what is left is one number per
@@ -74,6 +80,11 @@ __device__ __forceinline__ void tensor_write16(uint32_t at, const uint32_t (&v)[
                  "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(at) : "memory");
 }
 __device__ __forceinline__ void tensor_write_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ float4 shared_quad(uint32_t at) {           // (volatile: as plain loads all of a tile's are brought forward, at the price of 72 spilled registers)
+  float4 v;
+  asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at) : "memory");
+  return v;
+}
 __device__ __forceinline__ float reciprocal_fast(float x) { float r; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
 __device__ __forceinline__ float max3(float a, float b, float c) { float r; asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c)); return r; }
 // Whether all threads of the looking-up warps say yes.
@@ -358,7 +369,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
               if (lane / ROUND == r0 / ROUND + k) top = mine;
               const bool there = __shfl_sync(0xffffffffu, (uint32_t)ahead.there, r) != 0;
               const int e = high ? max((int)(high >> 23) - 127, -100) : 0;
-              const float up = there && c8 < a.c.dim ? copysignf(power_of_two(14 - min(e, 127)), a.scale) : 0.f;
+              // (a row that holds a NaN or an infinity becomes NaN throughout: then all of its scores are, and no factor needs to be)
+              const float up = !there || c8 >= a.c.dim ? 0.f : high >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : copysignf(power_of_two(14 - min(e, 127)), a.scale);
               float v[8];
               c[k].widen(v);
               uint32_t h[4];
@@ -373,7 +385,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
         else bring(Chunk8<__half>(), (const __half*)a.q);
         const int e = top ? max((int)(top >> 23) - 127, -100) : 0;
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        ahead.back = top >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : power_of_two(min(e, 127) - 14) * power_of_two(MX ? -kChunkFactor : 0) * fabsf(a.scale) * (!F::PLAIN && a.cap > 0.f ? 1.f : kLog2e);
+        ahead.back = power_of_two(min(e, 127) - 14) * power_of_two(MX ? -kChunkFactor : 0) * fabsf(a.scale) * (!F::PLAIN && a.cap > 0.f ? 1.f : kLog2e);
         ahead.slope = !F::PLAIN && a.slopes ? kLog2e * __ldg(a.slopes + ahead.head) : 0.f;
       }
       __syncwarp();
@@ -436,8 +448,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
 #pragma unroll 1
       for (uint32_t u = 0; u < n_units; ++u, ++n) {
         const uint8_t* const m = meta + n % F::INFO * F::META;
-        const float4* const k_scale = reinterpret_cast<const float4*>(m + F::AT_SCALES);
-        const float4* const v_scale = reinterpret_cast<const float4*>(m + F::AT_SCALES + 4 * KT);
+        const uint32_t k_scale = smem_addr(m + F::AT_SCALES), v_scale = k_scale + 4 * KT;
         const uint32_t* const real = reinterpret_cast<const uint32_t*>(m + F::AT_BITS);
         const uint32_t* const bad = real + 4;
         const uint32_t j = at.t.j0 + (at.unit + u) * KT, s_at = s_tile + (n & 1) * KT;
@@ -459,12 +470,14 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
           if (!MX) {
 #pragma unroll
             for (uint32_t k = 0; k < KT / 4; ++k) {
-              const float4 f = k_scale[k];
+              const float4 f = shared_quad(k_scale + 16 * k);
               mul2(x[4 * k], x[4 * k + 1], f.x, f.y);
               mul2(x[4 * k + 2], x[4 * k + 3], f.z, f.w);
             }
           }
           if (!F::PLAIN) {
+            // the bias of the tile's first token; of the others, `slope` for each token more
+            const float bias = row.slope * (float)(int32_t)(j - (uint32_t)row.pos);
             if (a.cap > 0.f) {                               // cap * tanh(y / cap) = cap - 2 cap / (1 + e^(2 y / cap)), off by some 2^-22 of cap
               const float cap_in = 2.f * kLog2e * unit / a.cap, cap_out = kLog2e * a.cap;
 #pragma unroll
@@ -474,16 +487,15 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
                 x[k + 1] = 1.f + exp2_fast(x[k + 1]);
                 x[k] = reciprocal_fast(x[k]);
                 x[k + 1] = reciprocal_fast(x[k + 1]);
-                fma2(x[k], x[k + 1], -2.f * cap_out, cap_out);
+                fma2(x[k], x[k + 1], -2.f * cap_out, cap_out + bias);
               }
             } else {
 #pragma unroll
-              for (uint32_t k = 0; k < KT; k += 2) mul2(x[k], x[k + 1], unit, unit);
+              for (uint32_t k = 0; k < KT; k += 2) fma2(x[k], x[k + 1], unit, bias);
             }
-            if (a.slopes) {
+            if (a.slopes)
 #pragma unroll
-              for (uint32_t k = 0; k < KT; ++k) x[k] = fmaf(row.slope, (float)(int32_t)(j + k - (uint32_t)row.pos), x[k]);
-            }
+              for (uint32_t k = 1; k < KT; ++k) x[k] = fmaf(row.slope, (float)k, x[k]);
           }
           uint32_t seen[2] = {~0u, ~0u};
           if constexpr (!EVERY) {
@@ -506,7 +518,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
 #pragma unroll
           for (uint32_t i = 0; i < 4; ++i) h4[i] = fmaxf(h4[i], x[KT - 4 + i]);
           float high = fmaxf(max3(h4[0], h4[1], h4[2]), h4[3]);
-          high = high == -INFINITY ? high : high * mul;      // (NaN from a poisoned query: its weights are NaN below)
+          high = high == -INFINITY ? high : high * mul;      // (NaN scores are not seen here: their weights are NaN below)
           float soft = 1.f, values = 1.f;
           if (high > ref + kSlack) { soft = exp2_fast(ref - high); ref = high; }
           if (tops.y != v_top) { values = power_of_two(max(v_top - tops.y, -126)); v_top = tops.y; }
@@ -541,14 +553,9 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
             if (!MX) {
 #pragma unroll
               for (uint32_t k = 0; k < 8; ++k) {
-                const float4 f = v_scale[8 * c + k];
+                const float4 f = shared_quad(v_scale + 16 * (8 * c + k));
                 mul2(y[4 * k], y[4 * k + 1], f.x, f.y);
                 mul2(y[4 * k + 2], y[4 * k + 3], f.z, f.w);
-              }
-              if constexpr (!EVERY) {
-#pragma unroll
-                for (uint32_t k = 0; k < 32; ++k)
-                  if (!(seen[c] >> k & 1u)) y[k] = 0.f;      // not zero times a poisoned scale
               }
             } else if (!EVERY && poisoned) {
               const uint32_t nan = bad[c] & seen[c];
@@ -558,7 +565,10 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
             }
             uint32_t h[16];
 #pragma unroll
-            for (uint32_t k = 0; k < 16; ++k) h[k] = pack_half(y[2 * k], y[2 * k + 1]);
+            for (uint32_t k = 0; k < 16; ++k) {
+              h[k] = pack_half(y[2 * k], y[2 * k + 1]);
+              if (!MX && !EVERY) h[k] &= (0u - (seen[c] >> 2 * k & 1u) & 0xffffu) | (0u - (seen[c] >> (2 * k + 1) & 1u) & 0xffff0000u);      // not zero times a poisoned scale
+            }
             tensor_write16(s_at + 16 * c, h);
           }
           sum += (sums[0] + sums[1]) + (sums[2] + sums[3]);
@@ -596,20 +606,21 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
         code[i] = make_uint4(0, 0, 0, 0);
         if (row >= 0 && 16 * piece < row_bytes && (MX || p.vec_codes)) code[i] = __ldg(reinterpret_cast<const uint4*>(a.c.codes[w] + row + 16 * piece));
       }
-      if constexpr (MX) return;
-      else if (p.vec_codes) return;
+      if constexpr (!MX) {
+        if (p.vec_codes) return;
 #pragma unroll
-      for (uint32_t i = 0; i < LOADS; ++i) {                                 // rows on any address
-        uint32_t in, piece, v[4] = {0, 0, 0, 0};
-        at_load(i, &in, &piece);
-        const int64_t row = reinterpret_cast<const int64_t*>(m)[in];
+        for (uint32_t i = 0; i < LOADS; ++i) {                               // rows on any address
+          uint32_t in, piece, v[4] = {0, 0, 0, 0};
+          at_load(i, &in, &piece);
+          const int64_t row = reinterpret_cast<const int64_t*>(m)[in];
 #pragma unroll 1
-        for (uint32_t b = 0; b < 16 && row >= 0 && 16 * piece + b < row_bytes; ++b) {
-          const uint32_t byte = (uint32_t)__ldg(a.c.codes[w] + row + 16 * piece + b) << (8 * (b % 4));
+          for (uint32_t b = 0; b < 16 && row >= 0 && 16 * piece + b < row_bytes; ++b) {
+            const uint32_t byte = (uint32_t)__ldg(a.c.codes[w] + row + 16 * piece + b) << (8 * (b % 4));
 #pragma unroll
-          for (uint32_t k = 0; k < 4; ++k) if (b / 4 == k) v[k] |= byte;
+            for (uint32_t k = 0; k < 4; ++k) if (b / 4 == k) v[k] |= byte;
+          }
+          code[i] = make_uint4(v[0], v[1], v[2], v[3]);
         }
-        code[i] = make_uint4(v[0], v[1], v[2], v[3]);
       }
     };
     bool ok = bar_wait(m_full(0), 0, failed);
@@ -744,7 +755,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
         }
         // the largest exponents: 4 bits, of the tile's keys, as bytes; of the values (8 bits: finite scales are positive)
         const uint32_t field = MX ? (high_byte[q][1] == 255u ? 0u : high_byte[q][1]) : (__float_as_uint(scale[q][1]) >> 23 & 255u);
-        if (field != 255u) v_most = max(v_most, min((int)field - 127, 126));
+        if (field != 255u) v_most = max(v_most, min((int)field - 127, MX ? 127 : 126));
         if (high_byte[q][0] != 255u) k_most = max(k_most, high_byte[q][0]);
         poisoned[q] = __ballot_sync(0xffffffffu, MX && high_byte[q][1] == 255u);
         flags |= (real[q] != 0xffffffffu) | (poisoned[q] != 0) << 1;         // some token is not there; some value is poisoned

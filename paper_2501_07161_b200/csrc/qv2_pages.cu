@@ -4,6 +4,10 @@
 // 1024 sequences at a time, and then serves its own part of the tokens and pages by searching it, so that one launch does it
 // all and no CTA waits for another.  The arrays that may be an input and an output at once are written by the CTA that
 // arrives last, when all have read them.
+//
+// Bound by latency.  64 sequences with a token each: 15 us a call, nearly all of it the host's.  1500 sequences with up to 700 new
+// tokens (9 MB, 1.4 us at the copy rate) take 23 to 26 us: the running sums over two rounds of 1024 sequences, then a search of ten steps and a chain of
+// look-ups for each token, four tokens of a thread at a time so that their steps overlap.
 #include "qv2_serve.cuh"
 
 namespace qv2 {

@@ -6,6 +6,9 @@
 // them, and the time that those take: 129 us for 16384 tokens of 40 heads x 128 in 16 bits.)  A CTA takes all heads of a few
 // tokens and works out the sines and cosines of those tokens once for all heads: the angle is a product of binary64, reduced there to
 // a part of a turn, and only then narrowed, so that positions in the millions keep their phase.
+//
+// 16384 tokens of 32 + 8 heads x 128 in 16 bits (336 MB) take 67 us, 5.0 TB/s: a copy of as much takes 51.  One token of a few sequences is the call's
+// host time (14 us).
 #include "qv2_serve.cuh"
 
 namespace qv2 {

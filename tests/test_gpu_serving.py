@@ -342,6 +342,38 @@ def test_attend_scales_far_apart(ctx, news, dtype, fmt):
     check_attend(ctx, held, x, news, dtype)
 
 
+@pytest.mark.parametrize("fmt", list(FORMATS))
+@pytest.mark.parametrize("options", [dict(), dict(cap=5.0)], ids=str)
+@pytest.mark.parametrize("lens,news", [([4, 8], [9, 12]), ([4, 70], [40, 75])])
+def test_attend_poisoned_queries_that_see_nothing(ctx, lens, news, options, fmt):
+    """They give zeros, like any that see nothing (padding may hold anything); those that see a token give NaN."""
+    held = Held(ctx, fmt, lens, 2, 64, 16, seed=10)
+    x = randn(sum(news), 4, 64, seed=7, dtype="bf16")
+    x[0, 0, 3], x[1, 1, 0], x[2, :, 63] = float("nan"), float("inf"), -float("inf")
+    x[news[0] - 1, 2, 5], x[news[0], 3, 7], x[news[0] + 6, 0, 1] = float("inf"), float("nan"), float("nan")
+    check_attend(ctx, held, x.cuda(), news, "bf16", **options)
+
+
+@pytest.mark.parametrize("fmt", list(FORMATS))
+@pytest.mark.parametrize("tokens,news,q_heads", [(32000, [4], 32), (3000, [31, 33, 1], 8)])
+def test_attend_pieces_of_many_rows(ctx, tokens, news, q_heads, fmt):
+    """Few sequences cut into many pieces, of which each has many rows of results to add up."""
+    held = Held(ctx, fmt, [tokens] * len(news), 8, 64, 64, seed=11)
+    check_attend(ctx, held, randn(sum(news), q_heads, 64, seed=8, dtype="bf16").cuda(), news, "bf16")
+
+
+@pytest.mark.parametrize("fmt", list(FORMATS))
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("lens,news", [([300], [1]), ([300], [40]), ([700, 30], [1, 30])])
+@pytest.mark.parametrize("power", [90, -90])
+def test_attend_values_far_from_one(ctx, power, lens, news, dtype, fmt):
+    """Values times 2^90 and 2^-90: weights are held against the largest scale of a value, whatever that is."""
+    def write(k, v, held):
+        v *= 2.0 ** power
+    held = Held(ctx, fmt, lens, 2, 128, 16, seed=9, write=write)
+    check_attend(ctx, held, randn(sum(news), 4, 128, seed=6, dtype=dtype).cuda(), news, dtype)
+
+
 def test_attend_cache_past_32_bits(ctx):
     """Rows of one head whose byte offsets pass 2^32; the pages in between are never touched."""
     heads, dim, page = 8, 128, 64

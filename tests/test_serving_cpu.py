@@ -1,8 +1,11 @@
 """CPU: struct layouts of the calls around the cache, and the reference that they are tested against on worked examples."""
 import ctypes as C
 import math
+import os
+import re
 
 import numpy as np
+import pytest
 
 import serving_reference as ref
 from paper_2501_07161_b200 import binding as B
@@ -43,3 +46,16 @@ def test_reference_attention_by_hand():
     assert np.allclose(out[:, 0], [[5, 6], [10 / 3, 13 / 3]]) and np.allclose(lse[:, 0], np.log([2, 3]))
     out, lse, _, _ = ref.attend(np.ones((2, 1, 2)), k, v, [3], [0, 2], np.array([[1, -1]]), 2, 1.0, window=1)
     assert np.allclose(out[0, 0], [6, 7]) and (out[1, 0] == 0).all() and lse[1, 0] == -np.inf
+
+
+CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2501_07161_b200", "csrc")
+
+
+@pytest.mark.parametrize("name", ["qv2_pages.cu", "qv2_rotate.cu", "qv2_attend.cuh", "qv2_attend.cu", "qv2_attend_chunk.cu"])
+def test_global_loads_stay_behind_the_wait_for_the_kernel_before(name):
+    """As for the other operators: inline loads and copies are volatile, every kernel waits for the one before it, and multicast
+    loads are not used."""
+    text = re.sub(r"//[^\n]*", "", open(os.path.join(CSRC, name)).read())
+    loads = re.findall(r"\basm\b(\s*volatile)?\s*\(\s*\"[^\"]*\b(?:ld\.(?:global|shared)|cp\.async)", text)
+    assert all(loads) and "ld_stream" not in text and "multicast::cluster" not in text
+    assert text.count("__global__") == len(re.findall(r"dependency_wait\(\);", text))
