@@ -343,6 +343,24 @@ def test_attend_scales_far_apart(ctx, news, dtype, fmt):
 
 
 @pytest.mark.parametrize("fmt", list(FORMATS))
+@pytest.mark.parametrize("max_new", [1, 5, 70, 100, 1 << 40])
+def test_attend_whatever_most_is_said(ctx, max_new, fmt):
+    """max_new chooses kernels; results do not depend on its being right."""
+    held = Held(ctx, fmt, [150, 40, 130], 2, 64, 16, seed=12)
+    check_attend(ctx, held, randn(111, 4, 64, seed=9, dtype="f16").cuda(), [100, 1, 10], "f16", max_new=max_new)
+
+
+@pytest.mark.parametrize("fmt", list(FORMATS))
+def test_attend_thousands_of_sequences(ctx, fmt):
+    """More sequences than threads, many without new tokens, some of them in chunks."""
+    lens = [(7 * s) % 23 for s in range(2600)]
+    news = [40 if s in (700, 2599) else (0 if s % 5 == 0 else 1 + (s % 97 == 0)) for s in range(2600)]
+    lens[700], lens[2599] = 60, 40
+    held = Held(ctx, fmt, lens, 1, 32, 8, seed=13)
+    check_attend(ctx, held, randn(sum(news), 2, 32, seed=9, dtype="bf16").cuda(), news, "bf16")
+
+
+@pytest.mark.parametrize("fmt", list(FORMATS))
 @pytest.mark.parametrize("options", [dict(), dict(cap=5.0)], ids=str)
 @pytest.mark.parametrize("lens,news", [([4, 8], [9, 12]), ([4, 70], [40, 75])])
 def test_attend_poisoned_queries_that_see_nothing(ctx, lens, news, options, fmt):
@@ -374,7 +392,8 @@ def test_attend_values_far_from_one(ctx, power, lens, news, dtype, fmt):
     check_attend(ctx, held, randn(sum(news), 4, 128, seed=6, dtype=dtype).cuda(), news, dtype)
 
 
-def test_attend_cache_past_32_bits(ctx):
+@pytest.mark.parametrize("new", [1, 60])
+def test_attend_cache_past_32_bits(ctx, new):
     """Rows of one head whose byte offsets pass 2^32; the pages in between are never touched."""
     heads, dim, page = 8, 128, 64
     pages = (1 << 32) // (page * heads * dim) + 9
@@ -383,10 +402,10 @@ def test_attend_cache_past_32_bits(ctx):
     k, v = randn(3 * page, heads, dim, seed=1), randn(3 * page, heads, dim, seed=2)
     slots = torch.cat([torch.arange(page) + page * i for i in used]).cuda()
     ctx.kv_write(cache, k.cuda(), v.cuda(), slots)
-    x = randn(1, 16, dim, seed=3, dtype="bf16").cuda()
+    x = randn(new, 16, dim, seed=3, dtype="bf16").cuda()
     small = ctx.kv_empty(3, page, heads, dim, q.KV_I8)
     ctx.kv_write(small, k.cuda(), v.cuda(), torch.arange(3 * page, device="cuda"))
-    args = (ints([0, 1]), ints([3 * page - 5]))
+    args = (ints([0, new]), ints([3 * page - 5]))
     big = ctx.kv_attend(cache, x, *args, torch.tensor([used], dtype=torch.int32, device="cuda"))
     assert torch.equal(big, ctx.kv_attend(small, x, *args, torch.tensor([[0, 1, 2]], dtype=torch.int32, device="cuda")))
 
