@@ -591,7 +591,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
     constexpr uint32_t TOK = F::TOK, LOADS = F::LOADS, HIGH = F::HIGH;
     const uint32_t first = (warp - 8) * TOK;                                 // this warp's tokens of a tile
     const uint32_t row_bytes = MX ? 16 * ((a.c.dim + 31) / 32) : a.c.dim;
-    uint4 code[2][2][LOADS];                                                 // of this tile and the next: [tile][keys, values]
+    uint4 code[2][LOADS];                                                    // of keys and of values
     auto at_load = [&](uint32_t i, uint32_t* in, uint32_t* piece) {          // token of the tile, 16-byte piece of its row
       *in = first + (i % (TOK / HIGH)) * HIGH + lane % HIGH;
       *piece = (i / (TOK / HIGH)) * F::WIDE + lane / HIGH;
@@ -626,17 +626,13 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
     bool ok = bar_wait(m_full(0), 0, failed);
     auto last = [&](uint32_t n) { return (*reinterpret_cast<const int32_t*>(meta + n % F::INFO * F::META + F::AT_BITS + 40) & 4) != 0; };
     if (ok) {
-      fetch(code[0][0], 0, 0); fetch(code[0][1], 1, 0);
-      if (!last(0)) {
-        ok = bar_wait(m_full(1), 0, failed);
-        if (ok) { fetch(code[1][0], 0, 1); fetch(code[1][1], 1, 1); }
-      }
+      fetch(code[0], 0, 0); fetch(code[1], 1, 0);
     }
-    // One tile; its registers take the codes of the next but one as soon as they are free.  false: that was the last, or a wait gave up.
-    auto convert = [&](uint32_t n, uint4 (&code)[2][LOADS]) -> bool {
+    // One tile; its registers take the codes of the next as soon as they are free.  false: that was the last, or a wait gave up.
+    auto convert = [&](uint32_t n) -> bool {
       const uint32_t s = n % F::STAGES, before = n - F::STAGES;              // the tile that had this stage
       const uint8_t* const m = meta + n % F::INFO * F::META;
-      const bool more = !last(n), far = more && !last(n + 1);
+      const bool more = !last(n);
 #pragma unroll
       for (int w = 0; w < 2; ++w) {
         if (n >= F::STAGES && !bar_wait(w ? o_done(before) : s_done(before), before / 8 & 1, failed)) return false;
@@ -645,9 +641,10 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
         for (uint32_t i = 0; i < LOADS; ++i) {
           uint32_t in, piece;
           at_load(i, &in, &piece);
-          const uint32_t to = tile + in * 128;
-          auto put = [&](uint32_t d, uint32_t x, uint32_t y, uint32_t z, uint32_t t) {
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + (d / 64) * F::PANEL + (((d / 8) ^ in) & 7) * 16), "r"(x), "r"(y), "r"(z), "r"(t) : "memory");
+          // 16 bytes of operands after 16: where they lie differs from the first in bits that the swizzle turns over
+          const uint32_t d = (MX ? 32 : 16) * piece, to = tile + in * 128 + (d / 64) * F::PANEL + (((d / 8) ^ in) & 7) * 16;
+          auto put = [&](uint32_t k, uint32_t x, uint32_t y, uint32_t z, uint32_t t) {
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to ^ 16 * k), "r"(x), "r"(y), "r"(z), "r"(t) : "memory");
           };
           const uint32_t word[4] = {code[w][i].x, code[w][i].y, code[w][i].z, code[w][i].w};
           if (MX) {
@@ -656,29 +653,29 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
             for (uint32_t k = 0; k < 4; ++k) {
               uint32_t c[4];
               four_bits(word[k], c);
-              put(32 * piece + 8 * k, half_mul(c[0], factor), half_mul(c[1], factor), half_mul(c[2], factor), half_mul(c[3], factor));
+              put(k, half_mul(c[0], factor), half_mul(c[1], factor), half_mul(c[2], factor), half_mul(c[3], factor));
             }
           } else {
 #pragma unroll
             for (uint32_t k = 0; k < 4; k += 2) {
               const uint32_t x = word[k] ^ 0x80808080u, y = word[k + 1] ^ 0x80808080u;
-              put(16 * piece + 4 * k, eight_bits<0x4140>(x), eight_bits<0x4342>(x), eight_bits<0x4140>(y), eight_bits<0x4342>(y));
+              put(k / 2, eight_bits<0x4140>(x), eight_bits<0x4342>(x), eight_bits<0x4140>(y), eight_bits<0x4342>(y));
             }
           }
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
         if (lane == 0) bar_arrive(w ? v_full(s) : k_full(s));
-        if (far) {
-          if (w == 0 && !bar_wait(m_full(n + 2), (n + 2) / 8 & 1, failed)) return false;
-          fetch(code[w], w, n + 2);
+        if (more) {
+          if (w == 0 && !bar_wait(m_full(n + 1), (n + 1) / 8 & 1, failed)) return false;
+          fetch(code[w], w, n + 1);
         }
       }
       return more;
     };
     if (ok)
 #pragma unroll 1
-      for (uint32_t n = 0; convert(n, code[0]) && convert(n + 1, code[1]); n += 2) {}
+      for (uint32_t n = 0; convert(n); ++n) {}
   } else if (warp < kProducts) {
     // ---------------------------------------------------------------------------------- tokens
     constexpr uint32_t PER = KT / (32 * kScout), WORDS = F::SCALE_WORDS, PACKS = MX ? (NB + 3) / 4 : 1;
