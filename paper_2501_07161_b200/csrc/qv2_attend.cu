@@ -5,6 +5,10 @@
 // come by cp.async into its own ring in shared memory, go through registers as operands of mma.sync (16 tokens x 8 query rows
 // for the scores, transposed probabilities for the values), and the softmax runs along (running maximum and sum).
 //
+// Measured: 8 sequences of up to 32000 tokens, 32 heads over 8 of 128 elements, 4 bits (231 MB, all that is read): 77 us, 3.0 TB/s; 64 sequences of
+// up to 2000 at 8 bits (208 MB): 61 us, 3.4 TB/s.  What bounds it is issue: 2.5 instructions a cycle and SM, of them 23 % for turning codes of values into
+// operands and multiplying them, 10 % for scales, 9 % for the softmax.
+//
 // Codes enter as they are: 4-bit codes and 8-bit integers are exact in binary16.  Scales of keys multiply the scores of their block
 // (32 columns: two products), or of the row; scales of values are split into the row's (multiplied into its weight) and
 // a power of two per block (multiplied into the codes, exactly).  Queries are brought to the top of binary16's range by

@@ -8,12 +8,13 @@
 //   warp 14          issues the products (tcgen05.mma): scores S = Q K^T two tiles ahead, results O += P V.
 // While one query tile's softmax runs the tensor cores are at the other's products.
 //
-// What bounds it: the way of one tile round the warps, not a unit.  Per 64 tokens and 256 rows of 128 elements the products ask for 1024
-// cycles and the exponentials (16 a cycle) for 1024; a tile takes some 1900.  A prompt of 8192 tokens, 32 heads over 8, takes 785 us (700 TFLOP/s of what
-// is seen); 64 tokens at a time against 128 took 785 where 128 took 840 with their scores and weights in one
-// buffer: the softmax holds 64 scores in registers, 128 spill.  8 bits cost more: a multiplication for each score and each weight that the 4-bit form has
-// in its operands (4 chunks of 512 over 4096 tokens each, 16 heads over 4:
-// 157 us without a cap, 224 with one, whose exponential and reciprocal come on top).
+// What bounds it: instructions and their latencies, not a unit.  Per 64 tokens and 256 rows of 128 elements the products are 512 cycles at the
+// full rate and the exponentials 1024 (16 a cycle); a tile takes some 3000, the tensor cores are active 25 % of the time, special functions 25 %, and leaving out all exponentials
+// was worth 3 %.  A prompt of 8192 tokens, 32 heads over 8, takes 740 us (744 TFLOP/s of what is seen).  Steps that told: two bodies of the softmax,
+// one of them without masks, so that it need not jump over what it does not use; half the code of the converting warps (785 -> 740 us: a quarter of what
+// a warp waits for is the next instruction); 64 tokens to a tile, since 128 scores of a row do not fit in registers (840 us with 128).
+// 8 bits cost more: a multiplication for each score and each weight that the 4-bit form has in its operands (4 chunks of 512 over 4096 tokens
+// each, 16 heads over 4: 154 us without a cap, 210 with one, whose exponential and reciprocal come on top).
 //
 // Codes are exact in binary16.  At 4 bits they are multiplied by their block's scale over the largest of the tile (keys) or of the item so far
 // (values), a power of two: exact unless a scale is 2^36 below that.  8-bit integers enter as they are, and what is left is one number per
